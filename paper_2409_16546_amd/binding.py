@@ -1,4 +1,4 @@
-"""ctypes binding of the C ABI in ``include/akv.h`` and ``include/akw.h`` -- argument marshalling only.
+"""ctypes binding of the C ABI in ``include/akv.h``, ``include/akw.h`` and ``include/akb.h`` -- argument marshalling only.
 
 Every function has the name of its C entry point and hands torch device pointers and the current
 HIP stream to it; no step of the path runs here.  If ``libakv.so`` has not been built the import of
@@ -28,6 +28,10 @@ EXPORTS = ["akv_version", "akv_last_error", "akv_layout_sizes", "akv_cache_reset
            "akv_fp16_path", "akv_stream_read",
            "akw_layout_sizes", "akw_workspace_init", "akw_pack", "akw_unpack", "akw_gemv"]
 AKW_MAX_B = 4
+AKB_EXPORTS = ["akb_layout_sizes", "akb_cache_reset", "akb_append", "akb_attention_workspace", "akb_attention", "akb_evict_workspace", "akb_evict",
+               "akb_unpack"]
+AKB_TB, AKB_MAX_G = 64, 16
+AKB_DTYPES = {torch.float16: 0, torch.bfloat16: 1}
 
 
 class AkvError(RuntimeError):
@@ -74,6 +78,22 @@ class akw_sizes(C.Structure):
 
 class akw_params(C.Structure):
     _fields_ = [("guard_bits", C.c_int32), ("force_level", C.c_int32), ("lvl_out", C.c_void_p)]
+
+
+class akb_shape(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("B", "Hq", "Hkv", "D", "Ncap", "dtype")]
+
+
+class akb_cache(C.Structure):
+    _fields_ = [("shape", akb_shape)] + [(n, C.c_void_p) for n in ("k8", "v8", "exps", "k_tail", "v_tail", "score", "lens", "flags")]
+
+
+class akb_sizes(C.Structure):
+    _fields_ = [(n, C.c_size_t) for n in ("k8", "v8", "exps", "k_tail", "v_tail", "score", "lens", "flags")]
+
+
+class akb_params(C.Structure):
+    _fields_ = [("scale", C.c_float), ("out_dtype", C.c_int32), ("accumulate", C.c_int32), ("max_len", C.c_int32)]
 
 
 _lib = None
@@ -130,6 +150,23 @@ def lib() -> C.CDLL:
         L.akw_gemv.restype = C.c_int
         L.akw_gemv.argtypes = [C.POINTER(akw_weights), C.c_void_p, C.c_int32, C.c_void_p, C.POINTER(akw_params), C.c_void_p,
                                C.c_size_t, C.c_void_p]
+        L.akb_layout_sizes.restype = C.c_int
+        L.akb_layout_sizes.argtypes = [C.POINTER(akb_shape), C.POINTER(akb_sizes)]
+        L.akb_cache_reset.restype = C.c_int
+        L.akb_cache_reset.argtypes = [C.POINTER(akb_cache), C.c_void_p]
+        L.akb_append.restype = C.c_int
+        L.akb_append.argtypes = [C.POINTER(akb_cache), C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p]
+        L.akb_attention_workspace.restype = C.c_size_t
+        L.akb_attention_workspace.argtypes = [C.POINTER(akb_shape), C.c_int32, C.c_int32]
+        L.akb_attention.restype = C.c_int
+        L.akb_attention.argtypes = [C.POINTER(akb_cache), C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.POINTER(akb_params), C.c_void_p, C.c_size_t,
+                                    C.c_void_p]
+        L.akb_evict_workspace.restype = C.c_size_t
+        L.akb_evict_workspace.argtypes = [C.POINTER(akb_shape), C.c_int32]
+        L.akb_evict.restype = C.c_int
+        L.akb_evict.argtypes = [C.POINTER(akb_cache), C.POINTER(akb_cache), C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
+        L.akb_unpack.restype = C.c_int
+        L.akb_unpack.argtypes = [C.POINTER(akb_cache), C.c_void_p, C.c_void_p, C.c_void_p]
         _lib = L
     return _lib
 
@@ -441,3 +478,129 @@ def akw_gemv(w: Weights, x: torch.Tensor, y: torch.Tensor | None = None, *, guar
         p = C.byref(akw_params(guard_bits, force_level, _ptr(lvl_out)))
     _check(lib().akw_gemv(C.byref(w.struct()), _ptr(x), B, _ptr(y), p, _ptr(ws), ws.numel(), _stream()))
     return y
+
+
+# ---------------------------------------------------------------------------------- block-scaled 8-bit cache (akb.h)
+
+def akb_layout_sizes(B: int, Hq: int, Hkv: int, D: int, Ncap: int, dtype: torch.dtype = torch.float16) -> akb_sizes:
+    shp, out = akb_shape(B, Hq, Hkv, D, Ncap, AKB_DTYPES[dtype]), akb_sizes()
+    _check(lib().akb_layout_sizes(C.byref(shp), C.byref(out)))
+    return out
+
+
+@dataclass
+class BlockCache:
+    """Caller-owned device buffers of one block-scaled 8-bit cache (torch owns the memory; include/akb.h has the layout).  The tensors may be given
+    in any shape of the right number of bytes, or be made by ``allocate``."""
+    B: int
+    Hq: int
+    Hkv: int
+    D: int
+    Ncap: int
+    dtype: torch.dtype
+    k8: torch.Tensor = field(repr=False)
+    v8: torch.Tensor = field(repr=False)
+    exps: torch.Tensor = field(repr=False)
+    k_tail: torch.Tensor = field(repr=False)
+    v_tail: torch.Tensor = field(repr=False)
+    lens: torch.Tensor = field(repr=False)
+    flags: torch.Tensor = field(repr=False)
+    score: torch.Tensor | None = field(repr=False, default=None)
+    workspace: torch.Tensor = field(repr=False, default=None)
+    _struct: akb_cache = field(repr=False, default=None)
+
+    def __post_init__(self):
+        sz = akb_layout_sizes(self.B, self.Hq, self.Hkv, self.D, self.Ncap, self.dtype)
+        for name, _ in akb_sizes._fields_:
+            t = getattr(self, name)
+            if t is None and name == "score":
+                continue
+            want = {"k_tail": self.dtype, "v_tail": self.dtype, "lens": torch.int32, "flags": torch.int32, "score": torch.float32, "exps": torch.int8}.get(name, torch.uint8)
+            assert t.dtype == want and t.numel() * t.element_size() == getattr(sz, name), f"{name}: {getattr(sz, name)} bytes of {want} are wanted"
+            assert t.device == self.k8.device, "one device for all buffers"
+
+    @staticmethod
+    def allocate(B: int, Hq: int, Hkv: int, D: int, Ncap: int, dtype: torch.dtype = torch.float16, *, score: bool = False, n: int = 1,
+                 device="cuda:0") -> "BlockCache":
+        """An empty cache; score: with room for accumulated attention weights; n: query tokens per call that the workspace is for."""
+        sz = akb_layout_sizes(B, Hq, Hkv, D, Ncap, dtype)
+        new = lambda bytes_, dt: torch.empty(bytes_ // torch.empty(0, dtype=dt).element_size(), dtype=dt, device=device)
+        c = BlockCache(B, Hq, Hkv, D, Ncap, dtype, new(sz.k8, torch.uint8), new(sz.v8, torch.uint8), new(sz.exps, torch.int8), new(sz.k_tail, dtype),
+                       new(sz.v_tail, dtype), new(sz.lens, torch.int32), new(sz.flags, torch.int32), new(sz.score, torch.float32) if score else None)
+        akb_cache_reset(c)
+        return c.reserve(n)
+
+    def struct(self) -> akb_cache:
+        if self._struct is None:   # the tensors never change after allocation
+            self._struct = akb_cache(akb_shape(self.B, self.Hq, self.Hkv, self.D, self.Ncap, AKB_DTYPES[self.dtype]), _ptr(self.k8), _ptr(self.v8),
+                                     _ptr(self.exps), _ptr(self.k_tail), _ptr(self.v_tail), _ptr(self.score), _ptr(self.lens), _ptr(self.flags))
+        return self._struct
+
+    def reserve(self, n: int = 1, keep: int = 0) -> "BlockCache":
+        """Make the workspace large enough for attention of up to n query tokens and, where keep > 0, for evictions down to `keep` tokens."""
+        shp = self.struct().shape
+        need = lib().akb_attention_workspace(C.byref(shp), n, int(self.score is not None))
+        need_evict = lib().akb_evict_workspace(C.byref(shp), keep) if keep > 0 else 1
+        if not need or not need_evict:
+            _check(AKV_EINVAL)
+        need = max(need, need_evict)
+        if self.workspace is None or self.workspace.numel() < need:
+            self.workspace = torch.empty(need, dtype=torch.uint8, device=self.k8.device)
+        return self
+
+
+def _here(*tensors) -> None:
+    """The calls go to the current stream of the current device: every tensor has to lie there."""
+    dev = torch.cuda.current_device()
+    assert all(t is None or t.device.index == dev for t in tensors), f"tensors of the current device (cuda:{dev}) only"
+
+
+def akb_cache_reset(cache: BlockCache) -> None:
+    _here(cache.k8)
+    _check(lib().akb_cache_reset(C.byref(cache.struct()), _stream()))
+
+
+def akb_append(cache: BlockCache, k_new: torch.Tensor, v_new: torch.Tensor, n_new: torch.Tensor | None = None) -> None:
+    """k_new, v_new: [B, Hkv, n, D] of the cache's type on the device; n_new: int32 [B] on the device or None."""
+    n = k_new.shape[2]
+    assert k_new.dtype == v_new.dtype == cache.dtype and tuple(k_new.shape) == (cache.B, cache.Hkv, n, cache.D) == tuple(v_new.shape)
+    assert n_new is None or (n_new.dtype == torch.int32 and tuple(n_new.shape) == (cache.B,))
+    _here(cache.k8, k_new, v_new, n_new)
+    _check(lib().akb_append(C.byref(cache.struct()), _ptr(k_new), _ptr(v_new), _ptr(n_new), n, _stream()))
+
+
+def akb_attention(cache: BlockCache, q: torch.Tensor, out: torch.Tensor | None = None, *, n_q: torch.Tensor | None = None, scale: float = 0.0,
+                  accumulate: bool = False, max_len: int = 0, workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """q: [B, Hq, n, D] (or [B, Hq, D]: one query token) of the cache's type; out: float32 or the cache's type, q's shape (float32 if None).
+    n_q: int32 [B] query tokens of each sequence (rows behind them are left as they were), or None for n.  accumulate: add the weights to the
+    cache's score.  The cache's workspace has to be large enough for n (``BlockCache.reserve``)."""
+    n = 1 if q.dim() == 3 else q.shape[2]
+    assert q.dtype == cache.dtype and tuple(q.shape) in ((cache.B, cache.Hq, n, cache.D), (cache.B, cache.Hq, cache.D))
+    assert n_q is None or (n_q.dtype == torch.int32 and tuple(n_q.shape) == (cache.B,))
+    if out is None:
+        out = (torch.empty if n_q is None else torch.zeros)(q.shape, dtype=torch.float32, device=q.device)
+    assert out.dtype in (torch.float32, cache.dtype) and out.shape == q.shape
+    ws = cache.workspace if workspace is None else workspace
+    _here(cache.k8, q, out, n_q, ws)
+    p = akb_params(scale, 0 if out.dtype == torch.float32 else 1, int(accumulate), max_len)
+    _check(lib().akb_attention(C.byref(cache.struct()), _ptr(q), _ptr(n_q), n, _ptr(out), C.byref(p), _ptr(ws), ws.numel() * ws.element_size(), _stream()))
+    return out
+
+
+def akb_evict(src: BlockCache, dst: BlockCache, keep: int, recent: int = 0, *, kept: torch.Tensor | None = None,
+              workspace: torch.Tensor | None = None) -> None:
+    """Bring every (sequence, KV head) of src down to its `keep` best tokens, in dst.  kept: int32 [B, Hkv, keep] receiving their places in src, or
+    None (then a workspace: src's has to be large enough for `keep`, ``BlockCache.reserve``)."""
+    assert kept is None or (kept.dtype == torch.int32 and tuple(kept.shape) == (src.B, src.Hkv, keep))
+    ws = src.workspace if workspace is None else workspace
+    _here(src.k8, dst.k8, kept, ws)
+    _check(lib().akb_evict(C.byref(src.struct()), C.byref(dst.struct()), keep, recent, _ptr(kept), _ptr(ws), ws.numel() * ws.element_size(), _stream()))
+
+
+def akb_unpack(cache: BlockCache) -> tuple[torch.Tensor, torch.Tensor]:
+    """The values as they are read, [B, Hkv, Ncap, D] of the cache's type; zeros behind a sequence's length."""
+    _here(cache.k8)
+    k = torch.empty(cache.B, cache.Hkv, cache.Ncap, cache.D, dtype=cache.dtype, device=cache.k8.device)
+    v = torch.empty_like(k)
+    _check(lib().akb_unpack(C.byref(cache.struct()), _ptr(k), _ptr(v), _stream()))
+    return k, v
