@@ -1,10 +1,13 @@
 // Eviction from the block-scaled 8-bit cache by accumulated attention weight (rules and layout: include/akb.h).
-#include "akb_common.h"
+#include "akb_pack.h"
 
 namespace akb {
 
 constexpr int kSelThreads = 1024;
 constexpr int kBins = 2048;
+constexpr int kCopies = 4;   // of the counts: many scores are alike, and counts of one value in one place are taken one after the other
+constexpr int kPer = 8;      // neighbouring scores per thread and turn
+constexpr int kTurns = 4;    // turns whose scores are asked for together
 
 // order of binary32 numbers as unsigned integers; zeros of either sign are equal, a NaN is the largest
 __device__ __forceinline__ uint32_t order_key(float f)
@@ -32,12 +35,36 @@ __device__ __forceinline__ int block_scan(int v, int* wave_s, int* sum)
     return x + before;
 }
 
+// The scores of the first n tokens in turns of kPer neighbouring ones per thread, kTurns turns asked for together (a workgroup is alone with its head, and
+// a trip to memory per turn is what it would wait for): f(turn's first token of this thread, its keys), every thread takes every turn
+template <class F> __device__ __forceinline__ void for_scores(const float* score, int n, F f)
+{
+    for (int base = 0; base < n; base += kTurns * kPer * kSelThreads) {
+        f32x4_t v[kTurns][kPer / 4];
+#pragma unroll
+        for (int k = 0; k < kTurns; ++k)
+#pragma unroll
+            for (int i = 0; i < kPer / 4; ++i) {   // rows are whole blocks long: a piece that begins below n can be read
+                const int t = base + (k * kSelThreads + int(threadIdx.x)) * kPer + 4 * i;
+                v[k][i] = t < n ? *reinterpret_cast<const f32x4_t*>(score + t) : f32x4_t{0, 0, 0, 0};
+            }
+#pragma unroll
+        for (int k = 0; k < kTurns; ++k) {
+            if (base + k * kSelThreads * kPer >= n) break;
+            uint32_t key[kPer];
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) key[i] = order_key(v[k][i >> 2][i & 3]);
+            f(base + (k * kSelThreads + int(threadIdx.x)) * kPer, key);
+        }
+    }
+}
+
 // Which tokens of a (sequence, KV head) stay: one workgroup each.  The place among the sorted scores is found 11, 11 and 10 bits at a
 // time (counts of each value of the bits among the scores that agree in the bits above), then one pass writes the kept tokens' places in
 // their order: those above the threshold, of those at it the first.
 __global__ __launch_bounds__(kSelThreads) void select_kernel(akb_cache c, akb_cache d, int keep, int recent, int32_t* __restrict__ kept)
 {
-    __shared__ int hist[kBins];
+    __shared__ int hist[kCopies * kBins];
     __shared__ int wave_s[kSelThreads / 64];
     __shared__ int found_s[2];
     const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x;
@@ -50,15 +77,23 @@ __global__ __launch_bounds__(kSelThreads) void select_kernel(akb_cache c, akb_ca
     if (need < pool && need > 0) {
         for (int pass = 0; pass < 3; ++pass) {
             const int shift = pass == 0 ? 21 : (pass == 1 ? 10 : 0), bits = pass == 2 ? 10 : 11;
-            for (int i = tid; i < kBins; i += kSelThreads) hist[i] = 0;
+            for (int i = tid; i < kCopies * kBins; i += kSelThreads) hist[i] = 0;
             __syncthreads();
-            for (int t = tid; t < pool; t += kSelThreads) {
-                const uint32_t k = order_key(score[t]);
-                if (pass == 0 || (k >> (shift + bits)) == prefix) atomicAdd(&hist[(k >> shift) & ((1u << bits) - 1)], 1);
-            }
+            int* mine = hist + (tid % kCopies) * kBins;
+            for_scores(score, pool, [&](int t0, const uint32_t (&key)[kPer]) {
+#pragma unroll
+                for (int i = 0; i < kPer; ++i)
+                    if (t0 + i < pool && (pass == 0 || (key[i] >> (shift + bits)) == prefix)) atomicAdd(&mine[(key[i] >> shift) & ((1u << bits) - 1)], 1);
+            });
             __syncthreads();
             // from the largest value down: thread i has values 2 i, 2 i + 1 counted from the top
-            const int top = kBins - 1 - 2 * tid, h0 = hist[top], h1 = hist[top - 1];
+            const int top = kBins - 1 - 2 * tid;
+            int h0 = 0, h1 = 0;
+#pragma unroll
+            for (int k = 0; k < kCopies; ++k) {
+                h0 += hist[k * kBins + top];
+                h1 += hist[k * kBins + top - 1];
+            }
             int all;
             const int upto = block_scan(h0 + h1, wave_s, &all), before = upto - h0 - h1;
             if (before < need && need <= upto) {
@@ -72,111 +107,122 @@ __global__ __launch_bounds__(kSelThreads) void select_kernel(akb_cache c, akb_ca
             __syncthreads();
         }
     }
-    const bool all_stay = count - sure >= pool, none = count - sure <= 0;
     int32_t* out = kept + bh * keep;
-    int done = 0, ties = 0;               // written; tokens at the threshold passed
-    if (all_stay) {
+    if (count - sure >= pool) {           // all stay
         for (int t = tid; t < count; t += kSelThreads) out[t] = t;
     } else {
-        if (!none)
-            for (int base = 0; base < pool; base += kSelThreads) {
-                const int t = base + tid;
-                const uint32_t k = t < pool ? order_key(score[t]) : 0u;
-                const int tie = t < pool && k == prefix ? 1 : 0;
-                int all_ties, all_keep;
-                const int rank = block_scan(tie, wave_s, &all_ties);
-                const int stays = t < pool && (k > prefix || (tie && ties + rank <= need)) ? 1 : 0;
-                const int at = block_scan(stays, wave_s, &all_keep);
-                if (stays) out[done + at - 1] = t;
-                done += all_keep;
-                ties += all_ties;
+        // written so far, and tokens at the threshold passed so far; a thread has kPer neighbouring tokens and counts those above the threshold
+        // (low half of the word that is summed up over the workgroup) and those at it (high half)
+        int above = 0, ties = 0;
+        for_scores(score, count > sure ? pool : 0, [&](int t0, const uint32_t (&key)[kPer]) {
+            int mine = 0;
+#pragma unroll
+            for (int i = 0; i < kPer; ++i)
+                if (t0 + i < pool) mine += key[i] > prefix ? 1 : (key[i] == prefix ? 1 << 16 : 0);
+            int all;
+            const int upto = block_scan(mine, wave_s, &all) - mine;
+            int a = above + (upto & 0xFFFF), e = ties + (upto >> 16);
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) {
+                if (t0 + i >= pool) continue;
+                if (key[i] > prefix || (key[i] == prefix && e < need)) out[a + min(e, need)] = t0 + i;
+                a += key[i] > prefix ? 1 : 0;
+                e += key[i] == prefix ? 1 : 0;
             }
+            above += all & 0xFFFF;
+            ties += all >> 16;
+        });
         for (int i = tid; i < sure; i += kSelThreads) out[count - sure + i] = len - sure + i;
     }
     for (int i = count + tid; i < keep; i += kSelThreads) out[i] = -1;
     if (h == 0 && tid == 0) d.lens[b] = count;
 }
 
-// one stored value of channel ch of token t, exact
-template <class T, int D> __device__ __forceinline__ float stored(const akb_cache& c, size_t bh, int len, int t, int ch, bool is_v)
-{
-    const int blk = t / kTB, s = t % kTB;
-    if (blk < len / kTB) {
-        const size_t block = bh * (c.shape.Ncap / kTB) + blk;
-        const uint32_t code = is_v ? c.v8[block * (kTB * D) + ch * kTB + v_place(s)] : c.k8[block * (kTB * D) + k_place<D>(s, ch)];
-        return T::lo(T::template cvt2<false>(code, pow2(c.exps[block * 2 + (is_v ? 1 : 0)])));
-    }
-    return T::to_float(is_v ? c.v_tail[(bh * D + ch) * kTB + v_place(s)] : c.k_tail[(bh * kTB + s) * D + ch]);
-}
-
-// A block of the destination: one workgroup of 2 D threads per (block, side, KV head, sequence); a thread has the four tokens of a
-// dword of V's order in eight channels, as in the append.
+// A block of the destination: one workgroup of 2 D threads per (block, side, KV head, sequence), as in the append.  K: a token's codes are runs of 64
+// bytes, read where they lie.  V: a token is one byte in each channel's 64 (read where they lie, a wave's byte loads touched 64 lines each, 4 of
+// 5 parts of the time), so the source blocks that hold a kept token are read whole, one after the other, into LDS (rows padded to 17 dwords,
+// so that a token's bytes lie in different banks), and the kept tokens' bytes go token-major to where the threads take them from.
 template <class T, int D>
 __global__ __launch_bounds__(2 * D) void gather_kernel(akb_cache c, akb_cache d, int keep, const int32_t* __restrict__ kept)
 {
-    constexpr int kOct = D / 8, kWaves = 2 * D / 64;
-    __shared__ uint32_t max_s[kWaves];
+    constexpr int kStride = PackLds<D>::kStride, kRow = D + 8;   // bytes of a token's row: shifted by two dwords from token to token
+    __shared__ PackLds<D> lds;   // the source block in its place, before the block is packed
+    __shared__ __align__(16) uint8_t rows_s[kTB * kRow];
     __shared__ int from_s[kTB];
-    const int tid = threadIdx.x, h = blockIdx.y, b = blockIdx.z, blk = blockIdx.x >> 1;
+    __shared__ float scale_s[kTB];
+    const int tid = threadIdx.x, lane = tid & 63, h = blockIdx.y, b = blockIdx.z, blk = blockIdx.x >> 1;
     const bool is_v = blockIdx.x & 1;
-    const size_t bh = size_t(b) * c.shape.Hkv + h;
-    const int len = seq_len(c, b), count = min(len, keep);
+    const size_t bh = size_t(b) * c.shape.Hkv + h, block0 = bh * (c.shape.Ncap / kTB);
+    const int len = seq_len(c, b), count = min(len, keep), whole = len / kTB;
     if (blk * kTB >= count) return;
     if (tid < kTB) {
         const int i = blk * kTB + tid, t = i < count ? kept[bh * keep + i] : -1;
         from_s[tid] = t;
+        scale_s[tid] = t >= 0 && t / kTB < whole ? pow2(c.exps[(block0 + t / kTB) * 2 + (is_v ? 1 : 0)]) : 0.f;
         if (!is_v && d.score && t >= 0) d.score[bh * d.shape.Ncap + i] = c.score[bh * c.shape.Ncap + t];
     }
     __syncthreads();
-    const int oct = tid % kOct, grp = tid / kOct, t0 = (grp & 3) * 16 + (grp >> 2) * 4;
-    float x[4][8];
-    float mx = 0.f;
+    const BlockLane<D> at(tid);
+    u32x4_t x[4] = {};
+    int token[4];
+    bool in_tail[4], stays[4];
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-        const int t = from_s[t0 + r];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            x[r][e] = t >= 0 ? stored<T, D>(c, bh, len, t, oct * 8 + e, is_v) : 0.f;
-            const float a = fabsf(x[r][e]);
-            if (a < __builtin_inff()) mx = fmaxf(mx, a);
-        }
+        const int t = from_s[at.t0 + r];
+        stays[r] = t >= 0;
+        in_tail[r] = stays[r] && t / kTB >= whole;
+        token[r] = t;
     }
-    if ((blk + 1) * kTB <= count) {
-        mx = akv::wave_max(mx);
-        if ((tid & 63) == 0) max_s[tid >> 6] = float_bits(mx);
-        __syncthreads();
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) mx = fmaxf(mx, bits_float(max_s[w]));
-        const int e = scale_exponent(mx);
-        const float inv = pow2(-e), most = most_code<T>(e);
-        const size_t block = bh * (d.shape.Ncap / kTB) + blk;
+    if (!is_v) {
+        u32x2_t w[4] = {};
 #pragma unroll
         for (int r = 0; r < 4; ++r)
+            if (stays[r] && !in_tail[r]) w[r] = *reinterpret_cast<const u32x2_t*>(c.k8 + (block0 + token[r] / kTB) * (kTB * D) + k_place<D>(token[r] % kTB, at.oct * 8));
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[r][i] = to_code<T>(x[r][i], inv, most);
-        if (!is_v) {
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-                *reinterpret_cast<u32x2_t*>(d.k8 + block * (kTB * D) + k_place<D>(t0 + r, oct * 8)) =
-                    u32x2_t{pack_codes(x[r][0], x[r][1], x[r][2], x[r][3]), pack_codes(x[r][4], x[r][5], x[r][6], x[r][7])};
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) *reinterpret_cast<uint32_t*>(d.v8 + block * (kTB * D) + (oct * 8 + i) * kTB + grp * 4) = pack_codes(x[0][i], x[1][i], x[2][i], x[3][i]);
-        }
-        if (tid == 0) d.exps[block * 2 + (is_v ? 1 : 0)] = (int8_t)e;
+        for (int r = 0; r < 4; ++r) x[r] = cvt8<T>(w[r][0], w[r][1], scale_s[at.t0 + r]);
     } else {
+        // lane i of every wave: source block of token i; `starts`: the first token of each source block
+        const int t = from_s[lane], src = t >= 0 && t / kTB < whole ? t / kTB : -1;
+        const int before = __shfl_up(src, 1);
+        uint64_t starts = __ballot(src >= 0 && (lane == 0 || before != src));
+        const int used = __popcll(__ballot(src >= 0));   // tokens of whole blocks: the first ones, as the places ascend
+        u32x4_t piece[2];
+        auto fetch = [&](int first) {
+            const uint8_t* p = c.v8 + (block0 + __builtin_amdgcn_readlane(src, first)) * (kTB * D) + tid * 16;
+            piece[0] = *reinterpret_cast<const u32x4_t*>(p);
+            piece[1] = *reinterpret_cast<const u32x4_t*>(p + 2 * D * 16);
+        };
+        if (starts) fetch(0);
+        while (starts) {
+            const int first = __builtin_ctzll(starts);
+            starts &= starts - 1;
+            const int end = starts ? __builtin_ctzll(starts) : used;
+            __syncthreads();   // the block before has been read
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            if (from_s[t0 + r] < 0) continue;
-            if (!is_v) {
-                *reinterpret_cast<u32x4_t*>(d.k_tail + (bh * kTB + t0 + r) * D + oct * 8) =
-                    u32x4_t{T::pack(x[r][0], x[r][1]), T::pack(x[r][2], x[r][3]), T::pack(x[r][4], x[r][5]), T::pack(x[r][6], x[r][7])};
-            } else {
+            for (int k = 0; k < 2; ++k)
 #pragma unroll
-                for (int i = 0; i < 8; ++i) d.v_tail[(bh * D + oct * 8 + i) * kTB + grp * 4 + r] = (uint16_t)T::from_float(x[r][i]);
-            }
+                for (int i = 0; i < 4; ++i) lds.codes[((tid + k * 2 * D) >> 2) * kStride + (tid & 3) * 4 + i] = piece[k][i];
+            if (starts) fetch(end);
+            __syncthreads();
+            const uint8_t* raw = reinterpret_cast<const uint8_t*>(lds.codes) + (tid % D) * (4 * kStride);
+            for (int i = first + tid / D; i < end; i += 2) rows_s[i * kRow + tid % D] = raw[v_place(from_s[i] % kTB)];
         }
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            if (stays[r] && !in_tail[r]) {
+                const u32x2_t w = *reinterpret_cast<const u32x2_t*>(rows_s + (at.t0 + r) * kRow + at.oct * 8);
+                x[r] = cvt8<T>(w[0], w[1], scale_s[at.t0 + r]);
+            }
     }
+    if (in_tail[0] || in_tail[1] || in_tail[2] || in_tail[3]) {
+        int slot[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) slot[r] = token[r] % kTB;
+        load_tail<D, false>(c, bh, is_v, x, in_tail, slot);
+    }
+    if ((blk + 1) * kTB <= count) pack_block<T, D>(d, bh * (d.shape.Ncap / kTB) + blk, is_v, x, lds);
+    else store_tail<D>(d, bh, is_v, x, stays);
 }
 
 hipError_t launch_evict(const akb_cache& src, const akb_cache& dst, int keep, int recent, int32_t* kept, hipStream_t st)

@@ -1,0 +1,121 @@
+// A block of 64 tokens x D channels in the registers of a workgroup of 2 D threads: a thread holds the four tokens 16 t + 4 g .. + 3 (a dword of V's
+// order) of eight channels, as 16-bit numbers.  What the append and the eviction do with it.
+#pragma once
+
+#include "akb_common.h"
+
+namespace akb {
+
+template <int D> struct BlockLane {
+    int oct, grp, t0;   // channels 8 oct .. + 7; dword grp of a V channel: tokens t0 .. t0 + 3
+    __device__ __forceinline__ BlockLane(int tid) : oct(tid % (D / 8)), grp(tid / (D / 8)), t0((grp & 3) * 16 + (grp >> 2) * 4) {}
+};
+template <int D> struct PackLds {
+    static constexpr int kStride = kTB / 4 + 1;   // of a V channel, padded by a dword
+    uint32_t codes[D * kStride];
+    uint32_t max[2 * D / 64];
+};
+
+// A complete block: maximum over the workgroup, e, codes.  K leaves straight from the registers (8 bytes of a token's 64-channel run), V through LDS,
+// so that its 16-byte pieces are stored by neighbouring lanes.
+template <class T, int D>
+__device__ __forceinline__ void pack_block(const akb_cache& c, size_t block, bool is_v, const u32x4_t (&x)[4], PackLds<D>& lds)
+{
+    constexpr int kStride = PackLds<D>::kStride;
+    const int tid = threadIdx.x;
+    const BlockLane<D> at(tid);
+    uint32_t mx = 0;
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) mx = max(mx, max(finite_mag<T>(x[r][i] & 0xFFFFu), finite_mag<T>(x[r][i] >> 16)));
+    mx = akv::wave_max_int(int(mx));
+    if ((tid & 63) == 0) lds.max[tid >> 6] = mx;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < 2 * D / 64; ++w) mx = max(mx, lds.max[w]);
+    const int e = scale_exponent(T::to_float(mx));
+    const float inv = pow2(-e), most = most_code<T>(e);
+    float y[4][8];
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            y[r][2 * i] = to_code<T>(T::lo(x[r][i]), inv, most);
+            y[r][2 * i + 1] = to_code<T>(T::hi(x[r][i]), inv, most);
+        }
+    if (!is_v) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            *reinterpret_cast<u32x2_t*>(c.k8 + block * (kTB * D) + k_place<D>(at.t0 + r, at.oct * 8)) =
+                u32x2_t{pack_codes(y[r][0], y[r][1], y[r][2], y[r][3]), pack_codes(y[r][4], y[r][5], y[r][6], y[r][7])};
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) lds.codes[(at.oct * 8 + i) * kStride + at.grp] = pack_codes(y[0][i], y[1][i], y[2][i], y[3][i]);
+        __syncthreads();
+        for (int p = tid; p < D * 4; p += 2 * D) {   // 16-byte pieces
+            const uint32_t* s = lds.codes + (p >> 2) * kStride + (p & 3) * 4;
+            *reinterpret_cast<u32x4_t*>(c.v8 + block * (kTB * D) + p * 16) = u32x4_t{s[0], s[1], s[2], s[3]};
+        }
+    }
+    if (tid == 0) c.exps[block * 2 + (is_v ? 1 : 0)] = (int8_t)e;
+}
+
+// Tokens of the incomplete block: those of the thread's four that `store` names
+template <int D>
+__device__ __forceinline__ void store_tail(const akb_cache& c, size_t bh, bool is_v, const u32x4_t (&x)[4], const bool (&store)[4])
+{
+    const BlockLane<D> at(threadIdx.x);
+    uint16_t* tail = (is_v ? c.v_tail : c.k_tail) + bh * kTB * D;
+    if (is_v && store[0] && store[1] && store[2] && store[3]) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const uint32_t sel = e & 1 ? 0x07060302u : 0x05040100u;
+            *reinterpret_cast<u32x2_t*>(tail + (at.oct * 8 + e) * kTB + at.grp * 4) =
+                u32x2_t{__builtin_amdgcn_perm(x[1][e >> 1], x[0][e >> 1], sel), __builtin_amdgcn_perm(x[3][e >> 1], x[2][e >> 1], sel)};
+        }
+        return;
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        if (!store[r]) continue;
+        if (!is_v) {
+            *reinterpret_cast<u32x4_t*>(tail + (at.t0 + r) * D + at.oct * 8) = x[r];
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) tail[(at.oct * 8 + e) * kTB + at.grp * 4 + r] = (uint16_t)(x[r][e >> 1] >> (16 * (e & 1)));
+        }
+    }
+}
+
+// ... and those that `want` names, read back into x; RUN: token[r] = t0 + r, a dword pair of V's order
+template <int D, bool RUN>
+__device__ __forceinline__ void load_tail(const akb_cache& c, size_t bh, bool is_v, u32x4_t (&x)[4], const bool (&want)[4], const int (&token)[4])
+{
+    const BlockLane<D> at(threadIdx.x);
+    const uint16_t* tail = (is_v ? c.v_tail : c.k_tail) + bh * kTB * D;
+    if (RUN && is_v) {
+        u32x2_t w[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[e] = *reinterpret_cast<const u32x2_t*>(tail + (at.oct * 8 + e) * kTB + at.grp * 4);
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)   // half r % 2 of dword r / 2 of channels 2 i, 2 i + 1
+                if (want[r]) x[r][i] = __builtin_amdgcn_perm(w[2 * i + 1][r >> 1], w[2 * i][r >> 1], r & 1 ? 0x07060302u : 0x05040100u);
+        return;
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        if (!want[r]) continue;
+        if (!is_v) {
+            x[r] = *reinterpret_cast<const u32x4_t*>(tail + token[r] * D + at.oct * 8);
+        } else {
+            const uint16_t* p = tail + at.oct * 8 * kTB + v_place(token[r]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[r][i] = p[2 * i * kTB] | uint32_t(p[(2 * i + 1) * kTB]) << 16;
+        }
+    }
+}
+
+}  // namespace akb

@@ -1,22 +1,18 @@
 // The block-scaled 8-bit cache: tokens stored, and given back as 16-bit values (rules and layout: include/akb.h).
-#include "akb_common.h"
+#include "akb_pack.h"
 
 namespace akb {
 
-// One workgroup of 2 D threads per (block that the call touches, side, KV head, sequence).  A thread holds the four tokens 16 t + 4 g .. + 3
-// of eight channels (16 bytes of four rows; the lanes of a wave cover whole rows), which is what a dword of V's order takes.
-//   complete block: tokens that the tail held and new ones; maximum over the workgroup, e, codes.  K leaves straight from the
-//   registers (8 bytes of a token's 64-channel run), V through LDS, so that its 16-byte pieces are stored by neighbouring lanes.
-//   the incomplete last block goes to the tail, by the workgroups of the first block alone: they are the ones that read the tail.
+// One workgroup of 2 D threads per (block that the call touches, side, KV head, sequence); the lanes of a wave read whole rows.
+//   A complete block takes the tokens that the tail held and new ones.
+//   The incomplete last block goes to the tail, by the workgroups of the first block alone: they are the ones that read the tail.
 // Who moves the length: with few workgroups the last of the sequence by ticket (every one has read the old length by then), as in the
 // append of the 16-bit cache; otherwise a launch behind this one.
 template <class T, int D>
 __global__ __launch_bounds__(2 * D) void append_kernel(akb_cache c, const uint16_t* __restrict__ k_new, const uint16_t* __restrict__ v_new,
                                                        const int32_t* __restrict__ n_new, int n, int ticketed)
 {
-    constexpr int kOct = D / 8, kWaves = 2 * D / 64, kStride = kTB / 4 + 1;
-    __shared__ uint32_t codes_s[D * kStride];   // V: channel-major, padded by a dword
-    __shared__ uint32_t max_s[kWaves];
+    __shared__ PackLds<D> lds;
     const int tid = threadIdx.x, h = blockIdx.y, b = blockIdx.z;
     const bool is_v = blockIdx.x & 1;
     const int j = blockIdx.x >> 1;
@@ -36,91 +32,33 @@ __global__ __launch_bounds__(2 * D) void append_kernel(akb_cache c, const uint16
     const size_t bh = size_t(b) * Hkv + h;
     const int first = len / kTB, had = len % kTB, total = had + cnt;   // counted from the start of block `first`
     const uint16_t* fresh = (is_v ? v_new : k_new) + bh * n * D;
-    uint16_t* tail = (is_v ? c.v_tail : c.k_tail) + bh * kTB * D;
-    const int oct = tid % kOct, grp = tid / kOct;         // channels 8 oct .. + 7; dword grp of a V channel: tokens t0 .. t0 + 3
-    const int t0 = (grp & 3) * 16 + (grp >> 2) * 4;
+    const BlockLane<D> at(tid);
     auto load_fresh = [&](int w) -> u32x4_t {             // token w counted from the start of block `first`
-        return w >= had && w < total ? *reinterpret_cast<const u32x4_t*>(fresh + size_t(w - had) * D + oct * 8) : u32x4_t{0, 0, 0, 0};
+        return w >= had && w < total ? *reinterpret_cast<const u32x4_t*>(fresh + size_t(w - had) * D + at.oct * 8) : u32x4_t{0, 0, 0, 0};
     };
+    const int t0 = at.t0;
     if ((j + 1) * kTB <= total) {
         u32x4_t x[4];
 #pragma unroll
         for (int r = 0; r < 4; ++r) x[r] = load_fresh(j * kTB + t0 + r);
         if (j == 0 && had > 0) {
-            if (!is_v) {
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    if (t0 + r < had) x[r] = *reinterpret_cast<const u32x4_t*>(tail + (t0 + r) * D + oct * 8);
-            } else {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const u32x2_t w = *reinterpret_cast<const u32x2_t*>(tail + (oct * 8 + e) * kTB + grp * 4);
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const uint32_t half = (w[r >> 1] >> (16 * (r & 1))) & 0xFFFFu, sh = 16 * (e & 1);
-                        if (t0 + r < had) x[r][e >> 1] = (x[r][e >> 1] & ~(0xFFFFu << sh)) | (half << sh);
-                    }
-                }
-            }
+            const bool old[4] = {t0 < had, t0 + 1 < had, t0 + 2 < had, t0 + 3 < had};
+            const int token[4] = {t0, t0 + 1, t0 + 2, t0 + 3};
+            load_tail<D, true>(c, bh, is_v, x, old, token);
         }
-        uint32_t mx = 0;
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) mx = max(mx, max(finite_mag<T>(x[r][i] & 0xFFFFu), finite_mag<T>(x[r][i] >> 16)));
-        mx = akv::wave_max_int(int(mx));
-        if ((tid & 63) == 0) max_s[tid >> 6] = mx;
-        __syncthreads();
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) mx = max(mx, max_s[w]);
-        const int e = scale_exponent(T::to_float(mx));
-        const float inv = pow2(-e), most = most_code<T>(e);
-        const size_t block = bh * (Ncap / kTB) + first + j;
-        float y[4][8];
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                y[r][2 * i] = to_code<T>(T::lo(x[r][i]), inv, most);
-                y[r][2 * i + 1] = to_code<T>(T::hi(x[r][i]), inv, most);
-            }
-        if (!is_v) {
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const u32x2_t w = {pack_codes(y[r][0], y[r][1], y[r][2], y[r][3]), pack_codes(y[r][4], y[r][5], y[r][6], y[r][7])};
-                *reinterpret_cast<u32x2_t*>(c.k8 + block * (kTB * D) + k_place<D>(t0 + r, oct * 8)) = w;
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) codes_s[(oct * 8 + i) * kStride + grp] = pack_codes(y[0][i], y[1][i], y[2][i], y[3][i]);
-            __syncthreads();
-            for (int p = tid; p < D * 4; p += 2 * D) {   // 16-byte pieces
-                const uint32_t* s = codes_s + (p >> 2) * kStride + (p & 3) * 4;
-                *reinterpret_cast<u32x4_t*>(c.v8 + block * (kTB * D) + p * 16) = u32x4_t{s[0], s[1], s[2], s[3]};
-            }
-        }
-        if (tid == 0) c.exps[block * 2 + (is_v ? 1 : 0)] = (int8_t)e;
+        pack_block<T, D>(c, bh * (Ncap / kTB) + first + j, is_v, x, lds);
     }
     if (j == 0 && total % kTB) {   // the incomplete block: its new tokens go to the tail (what of the old ones is needed has been read)
         __syncthreads();
         const int last = total / kTB * kTB;
         u32x4_t x[4];
-#pragma unroll
-        for (int r = 0; r < 4; ++r) x[r] = load_fresh(last + t0 + r);
         bool store[4];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) store[r] = last + t0 + r >= had && last + t0 + r < total;
-        if (!is_v) {
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-                if (store[r]) *reinterpret_cast<u32x4_t*>(tail + (t0 + r) * D + oct * 8) = x[r];
-        } else if (store[0] || store[1] || store[2] || store[3]) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    if (store[r]) tail[(oct * 8 + e) * kTB + grp * 4 + r] = (uint16_t)(x[r][e >> 1] >> (16 * (e & 1)));
+        for (int r = 0; r < 4; ++r) {
+            x[r] = load_fresh(last + t0 + r);
+            store[r] = last + t0 + r >= had && last + t0 + r < total;
         }
+        store_tail<D>(c, bh, is_v, x, store);
     }
     if (c.score && !is_v && tid < kTB) {   // the new tokens' scores
         const int w = j * kTB + tid;
