@@ -109,7 +109,15 @@ __device__ __forceinline__ uint32_t pack_codes(float a, float b, float c, float 
     return uint32_t(__builtin_amdgcn_cvt_pk_fp8_f32(c, d, __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false), true));
 }
 
-// tokens of sequence b, and its query tokens
+// A barrier for data in LDS alone: loads from memory that are in flight stay so (__syncthreads waits for them)
+__device__ __forceinline__ void lds_barrier()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
+// tokens of sequence b
 __device__ __forceinline__ int seq_len(const akb_cache& c, int b) { return min(max(c.lens[b], 0), c.shape.Ncap); }
 #endif
 

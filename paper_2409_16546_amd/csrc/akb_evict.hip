@@ -183,7 +183,8 @@ __global__ __launch_bounds__(2 * D) void gather_kernel(akb_cache c, akb_cache d,
     } else {
         // lane i of every wave: source block of token i; `starts`: the first token of each source block
         const int t = from_s[lane], src = t >= 0 && t / kTB < whole ? t / kTB : -1;
-        const int before = __shfl_up(src, 1);
+        const int place = v_place(max(t, 0) % kTB), before = __shfl_up(src, 1);
+        const int half = __builtin_amdgcn_readfirstlane(tid / D);   // which of two neighbouring tokens the wave moves
         uint64_t starts = __ballot(src >= 0 && (lane == 0 || before != src));
         const int used = __popcll(__ballot(src >= 0));   // tokens of whole blocks: the first ones, as the places ascend
         u32x4_t piece[2];
@@ -197,15 +198,22 @@ __global__ __launch_bounds__(2 * D) void gather_kernel(akb_cache c, akb_cache d,
             const int first = __builtin_ctzll(starts);
             starts &= starts - 1;
             const int end = starts ? __builtin_ctzll(starts) : used;
-            __syncthreads();   // the block before has been read
+            lds_barrier();   // the block before has been read
 #pragma unroll
             for (int k = 0; k < 2; ++k)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) lds.codes[((tid + k * 2 * D) >> 2) * kStride + (tid & 3) * 4 + i] = piece[k][i];
             if (starts) fetch(end);
-            __syncthreads();
+            lds_barrier();
             const uint8_t* raw = reinterpret_cast<const uint8_t*>(lds.codes) + (tid % D) * (4 * kStride);
-            for (int i = first + tid / D; i < end; i += 2) rows_s[i * kRow + tid % D] = raw[v_place(from_s[i] % kTB)];
+            for (int i = first + half; i < end; i += 8) {   // four of the wave's tokens at a time
+                uint8_t code[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) code[k] = raw[__builtin_amdgcn_readlane(place, min(i + 2 * k, end - 1))];
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    if (i + 2 * k < end) rows_s[(i + 2 * k) * kRow + tid % D] = code[k];
+            }
         }
         __syncthreads();
 #pragma unroll
