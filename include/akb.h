@@ -107,11 +107,15 @@ typedef struct akb_params {
 size_t akb_attention_workspace(const akb_shape *shape, int32_t n, int32_t accumulate);
 size_t akb_evict_workspace(const akb_shape *shape, int32_t keep);
 
+/* Prepare a workspace: zero its control words (arrival counters at its front, which every call leaves at zero again and evictions do not touch).
+ * Once on every workspace before its first use, and again if anything else wrote to it; a single small fill kernel. */
+akv_status akb_workspace_init(void *workspace, size_t workspace_bytes, void *stream);
+
 /*
  * Attention of n query tokens per sequence.  q: device [B][Hq][n][D] of the shape's type.  n_q: device int32 [B] with the
  * number of leading query tokens (0..n) of each sequence, or NULL for n.  out: device [B][Hq][n][D] of params->out_dtype;
  * rows i >= n_q[b] are left as they were; a query token that sees nothing yields zeros.  workspace: device scratch, 256-B
- * aligned; calls that overlap need distinct ones.  It holds nothing between calls and needs no preparation.  params may be
+ * aligned, prepared by akb_workspace_init; calls that overlap need distinct ones, and it holds nothing between calls.  params may be
  * NULL (float32 out, no accumulation).  The same call gives the same bits.
  */
 akv_status akb_attention(const akb_cache *cache, const uint16_t *q, const int32_t *n_q, int32_t n, void *out, const akb_params *params,

@@ -28,7 +28,7 @@ EXPORTS = ["akv_version", "akv_last_error", "akv_layout_sizes", "akv_cache_reset
            "akv_fp16_path", "akv_stream_read",
            "akw_layout_sizes", "akw_workspace_init", "akw_pack", "akw_unpack", "akw_gemv"]
 AKW_MAX_B = 4
-AKB_EXPORTS = ["akb_layout_sizes", "akb_cache_reset", "akb_append", "akb_attention_workspace", "akb_attention", "akb_evict_workspace", "akb_evict",
+AKB_EXPORTS = ["akb_layout_sizes", "akb_cache_reset", "akb_append", "akb_attention_workspace", "akb_workspace_init", "akb_attention", "akb_evict_workspace", "akb_evict",
                "akb_unpack"]
 AKB_TB, AKB_MAX_G = 64, 16
 AKB_DTYPES = {torch.float16: 0, torch.bfloat16: 1}
@@ -158,6 +158,8 @@ def lib() -> C.CDLL:
         L.akb_append.argtypes = [C.POINTER(akb_cache), C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p]
         L.akb_attention_workspace.restype = C.c_size_t
         L.akb_attention_workspace.argtypes = [C.POINTER(akb_shape), C.c_int32, C.c_int32]
+        L.akb_workspace_init.restype = C.c_int
+        L.akb_workspace_init.argtypes = [C.c_void_p, C.c_size_t, C.c_void_p]
         L.akb_attention.restype = C.c_int
         L.akb_attention.argtypes = [C.POINTER(akb_cache), C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.POINTER(akb_params), C.c_void_p, C.c_size_t,
                                     C.c_void_p]
@@ -546,6 +548,7 @@ class BlockCache:
         need = max(need, need_evict)
         if self.workspace is None or self.workspace.numel() < need:
             self.workspace = torch.empty(need, dtype=torch.uint8, device=self.k8.device)
+            akb_workspace_init(self.workspace)
         return self
 
 
@@ -558,6 +561,12 @@ def _here(*tensors) -> None:
 def akb_cache_reset(cache: BlockCache) -> None:
     _here(cache.k8)
     _check(lib().akb_cache_reset(C.byref(cache.struct()), _stream()))
+
+
+def akb_workspace_init(workspace: torch.Tensor) -> None:
+    """Zero the control words of a workspace (once per workspace, before its first use)."""
+    _here(workspace)
+    _check(lib().akb_workspace_init(_ptr(workspace), workspace.numel() * workspace.element_size(), _stream()))
 
 
 def akb_append(cache: BlockCache, k_new: torch.Tensor, v_new: torch.Tensor, n_new: torch.Tensor | None = None) -> None:

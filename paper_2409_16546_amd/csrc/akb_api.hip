@@ -96,6 +96,12 @@ size_t akb_attention_workspace(const akb_shape* shape, int32_t n, int32_t accumu
     return akb::attention_workspace(*shape, n, accumulate != 0);
 }
 
+akv_status akb_workspace_init(void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (akv_status st = check_workspace(workspace, workspace_bytes, akb::attention_tickets())) return st;
+    return hip_result(akv::launch_zero(workspace, akb::attention_tickets(), static_cast<hipStream_t>(stream)), "zero launch");
+}
+
 akv_status akb_attention(const akb_cache* cache, const uint16_t* q, const int32_t* n_q, int32_t n, void* out, const akb_params* params, void* workspace,
                          size_t workspace_bytes, void* stream)
 {
@@ -124,7 +130,7 @@ size_t akb_evict_workspace(const akb_shape* shape, int32_t keep)
         fail(AKV_EINVAL, "bad shape, or keep below 1");
         return 0;
     }
-    return akv::align256(size_t(shape->B) * shape->Hkv * size_t(keep) * sizeof(int32_t));
+    return akv::align256(akb::attention_tickets()) + akv::align256(size_t(shape->B) * shape->Hkv * size_t(keep) * sizeof(int32_t));
 }
 
 akv_status akb_evict(const akb_cache* src, const akb_cache* dst, int32_t keep, int32_t recent, int32_t* kept, void* workspace, size_t workspace_bytes, void* stream)
@@ -150,7 +156,7 @@ akv_status akb_evict(const akb_cache* src, const akb_cache* dst, int32_t keep, i
     if (!aligned(kept, 4)) return fail(AKV_EINVAL, "kept must be 4-byte aligned");
     if (!kept) {
         if (akv_status st = check_workspace(workspace, workspace_bytes, akb_evict_workspace(&s, keep))) return st;
-        kept = static_cast<int32_t*>(workspace);
+        kept = reinterpret_cast<int32_t*>(static_cast<char*>(workspace) + akv::align256(akb::attention_tickets()));
     }
     return hip_result(akb::launch_evict(*src, *dst, keep, recent, kept, static_cast<hipStream_t>(stream)), "evict launch");
 }

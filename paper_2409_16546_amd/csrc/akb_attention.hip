@@ -12,278 +12,512 @@ namespace akb {
 // In 16 bits the weights of fp16 caches would lose bits below 2^-14: they are taken relative to 2^-14 of the maximum (up to 2^14).
 constexpr float kWeightBits = 14.f;
 constexpr int kWaves = 4;
+constexpr int kTileRows = 16;
 
-// what one row tile of one split of the tokens gives: O [16][D], then (maximum, sum) per row
-template <int D> constexpr int part_floats() { return 16 * D + 32; }
+// What one split of a row group leaves for the workgroup that joins them: per row (maximum, sum), padded to 16 bytes, then O [row][D]
+__host__ __device__ constexpr int part_head(int rows) { return (2 * rows + 3) / 4 * 4; }
+__host__ __device__ constexpr int part_floats(int rows, int D) { return part_head(rows) + rows * D; }
 
+constexpr int kMostCut = 256;   // sequences whose lengths every workgroup looks through
+
+// How the walks over the blocks (one per row group) are shared out.  `slots` workgroups run at a time, two per compute unit (three or four per unit measured
+// behind: their fixed costs, parts to write and join, outweigh what more loads in flight give; 8 x 8 pairs of 4096 tokens 15.6 / 18.3 / 19.4 us).  Where there
+// are fewer walks than that, each is cut into parts.  The host knows a bound of the lengths only.  Calls of several long sequences with few walks are cut
+// by the device, which looks through the lengths: parts of about equal length, all in one round (4 sequences of 32768 to 131072 tokens, 8 heads each: 139 ->
+// 123 us).  Elsewhere every walk is cut into the same number of parts: a short call would wait for the lengths (8.0 -> 9.9 us), and with many walks the
+// parts that are not full cost what they even out (16 x 32 pairs of 2048 to 8192 tokens 131 -> 145 us).
 struct AttentionPlan {
-    int groups;   // row tiles of a (sequence, KV head)
-    int splits;   // parts its blocks are cut into
-    size_t parts, stats, total;   // offsets into the workspace
+    int tiles;      // row tiles of a row group: 1, 2
+    int groups;     // row groups of a (sequence, KV head)
+    int splits;     // parts of a walk, or 0: cut by the device
+    int grid;       // workgroups at most
+    bool ticketed;  // the last workgroup of a row group joins its parts; otherwise a launch does
+    size_t tickets, parts, logits, stats, total;   // offsets into the workspace
 };
-// (a call has more than one split only where there are fewer row tiles than 2 workgroups per unit, and then at most twice as many parts)
+// Row tiles that share a walk over K and V.
+static int tiles_for(long rows) { return rows <= 16 ? 1 : 2; }
 static AttentionPlan plan(const akb_shape& s, int n, int max_len, bool accumulate)
 {
     AttentionPlan p;
-    p.groups = (int)((long(n) * (s.Hq / s.Hkv) + 15) / 16);
-    const long items = long(s.B) * s.Hkv * p.groups, blocks = (max_len + kTB - 1) / kTB;
-    const long want = (2L * akv::compute_units() + items - 1) / items;
-    p.splits = (int)std::max(1L, std::min(want, (blocks + kWaves - 1) / kWaves));
-    p.parts = 0;
-    p.stats = align256(size_t(4) * akv::compute_units() * (16 * s.D + 32) * sizeof(float));
-    p.total = p.stats + (accumulate ? align256(size_t(items) * 32 * sizeof(float)) : 0);
+    const long slots = 2L * akv::compute_units(), rows = long(n) * (s.Hq / s.Hkv), pairs = long(s.B) * s.Hkv;
+    p.tiles = tiles_for(rows);
+    p.groups = (int)((rows + 16 * p.tiles - 1) / (16 * p.tiles));
+    const long items = pairs * p.groups, blocks = (max_len + kTB - 1) / kTB;
+    const long splits = items >= slots ? 1 : std::max(1L, std::min((slots + items - 1) / items, (blocks + kWaves - 1) / kWaves));
+    p.splits = s.B > 1 && s.B <= kMostCut && items * 4 <= slots && blocks >= 8 * kWaves * splits ? 0 : (int)splits;
+    p.grid = (int)(p.splits ? items * p.splits : slots);
+    // Joined by the last workgroup where that has little to read (a launch less), by a launch of one workgroup per row where it has much: rows x parts per row
+    // group 4 7.4 / 11.0 us, 48 11.6 / 14.4, 64 40.5 / 45.1; 128 23.2 / 20.9, 350 29.7 / 25.9, 512 27.9 / 19.3 (last workgroup / launch).
+    p.ticketed = std::min(rows, 16L * p.tiles) * splits <= 64;
+    // (calls of fewer query tokens fit into what is laid out for more: fewer than `2 slots` parts of up to 32 rows, and as many tickets)
+    p.tickets = 0;
+    p.parts = align256(size_t(2 * slots) * sizeof(int32_t));
+    p.logits = p.parts + align256(size_t(2 * slots) * part_floats((int)std::min(rows, 32L), s.D) * sizeof(float));
+    p.stats = p.logits + (accumulate ? align256(size_t(pairs) * std::min(rows, 16L) * s.Ncap * sizeof(float)) : 0);
+    p.total = p.stats + (accumulate ? align256(size_t(pairs) * rows * 2 * sizeof(float)) : 0);
     return p;
 }
-size_t attention_workspace(const akb_shape& s, int n, bool accumulate)
-{
-    return plan(s, n, s.Ncap, accumulate).total;
-}
+size_t attention_workspace(const akb_shape& s, int n, bool accumulate) { return plan(s, std::max(n, 1), s.Ncap, accumulate).total; }
+size_t attention_tickets() { return size_t(4) * akv::compute_units() * sizeof(int32_t); }
 
 struct RowArgs {
     akb_cache c;
     const uint16_t* q;
     const int32_t* n_q;
-    int n, groups, splits, out_dtype;
+    int n, groups, splits, slots, out_dtype;
     void* out;
     float c2;
-    float *parts, *stats;   // stats: (maximum, 1 / sum) per row, or NULL
+    int32_t* tickets;   // [sequence, KV head, row group]: splits that have arrived, zero between calls; NULL: join_kernel follows
+    float *parts, *logits, *stats;   // logits: q . k of the one row group, [sequence, KV head][block][tile][row][16]; stats: (maximum, 1 / sum) per row; or NULL
 };
 
 // The tokens that rows see: row r (its query token r / G of m) the first `limit`
 __device__ __forceinline__ int row_limit(int row, int G, int m, int len) { return row < m * G ? len - m + row / G + 1 : 0; }
 
-// A block of K as the operand of S^T: lane (token t % 16, quarter g of 64 channels), [tile][64 channels]: 16 codes
-template <int D> struct Codes {
-    u32x4_t k[4][D / 64], v[D / 16];
-    float ks, vs;
+// How the walks of a call are cut: the same in every wave that asks.  Lane l has sequences l, l + 64, ..
+struct Cut {
+    unsigned w;        // this workgroup's number among those that have work
+    int b, splits;     // its sequence, the parts of its walks
+    unsigned first;    // the sequence's first workgroup
+    // An XCD has one stretch of the work, so that the row groups and parts of a (sequence, KV head) share its L2 (workgroups are dealt to the XCDs in turn):
+    // false where none is left.
+    __device__ __forceinline__ bool stretch(unsigned n)
+    {
+        const unsigned per = (n + akv::kXcds - 1) / akv::kXcds, x = blockIdx.x % akv::kXcds, i = blockIdx.x / akv::kXcds;
+        w = x * per + i;
+        return i < per && w < n;
+    }
+    // OF: of sequence `of`; otherwise of this workgroup; false where there is no work for it
+    template <bool OF> __device__ __forceinline__ bool find(const RowArgs& a, int of)
+    {
+        const int B = a.c.shape.B, walks = a.c.shape.Hkv * a.groups, lane = threadIdx.x & 63;   // walks: per sequence
+        splits = a.splits;
+        if (splits) {
+            if (!OF && !stretch(unsigned(B) * walks * splits)) return false;
+            b = OF ? of : int(w / unsigned(walks * splits));
+            first = unsigned(b) * walks * splits;
+            return true;
+        }
+        constexpr int kTurns = kMostCut / 64;
+        int nb[kTurns];   // blocks of sequence 64 i + lane
+#pragma unroll
+        for (int i = 0; i < kTurns; ++i) {
+            const int s = 64 * i + lane;
+            nb[i] = s < B && (!a.n_q || a.n_q[s] > 0) ? (seq_len(a.c, s) + kTB - 1) / kTB : 0;
+        }
+        unsigned total = 0;   // fewer than 2^25: at most 128 walks of 65536 blocks (and at least one part per walk in the `slots`)
+#pragma unroll
+        for (int i = 0; i < kTurns; ++i)
+            if (64 * i < B) total += akv::wave_read(akv::wave_scan_add(nb[i]), 63);
+        // the sum of all ceil(blocks / q) is below total / q + walks, so it fits the slots
+        const unsigned most = a.slots - B * walks, q = max(unsigned(kWaves), (total * walks + most - 1) / most);
+        auto parts = [&](int i) { return 64 * i + lane < B ? max(int((nb[i] + q - 1) / q), 1) : 0; };
+        unsigned n = 0, before = 0;
+#pragma unroll
+        for (int i = 0; i < kTurns; ++i)
+            if (64 * i < B) n += akv::wave_read(akv::wave_scan_add(parts(i)), 63);
+        if (!OF && !stretch(n * walks)) return false;
+        b = B;
+#pragma unroll
+        for (int i = 0; i < kTurns; ++i) {
+            if (64 * i >= B || b < B) continue;
+            const int mine = parts(i), upto = akv::wave_scan_add(mine);
+            const bool here = 64 * i + lane < B && (OF ? 64 * i + lane == of : (before + unsigned(upto)) * walks > w);
+            if (const uint64_t past = __ballot(here)) {
+                const int l = __builtin_ctzll(past);
+                b = 64 * i + l;
+                splits = akv::wave_read(mine, l);
+                first = (before + unsigned(akv::wave_read(upto, l)) - splits) * walks;
+            }
+            before += akv::wave_read(upto, 63);
+        }
+        return true;
+    }
+};
+
+// A block of K or V as the matrix instructions take it: lane (token t % 16 or channel % 16, quarter): 16 codes
+template <int D> struct KCodes {
+    u32x4_t w[4][D / 64];
+    float s;
     __device__ __forceinline__ void load(const akb_cache& c, size_t block, int lane)
     {
-        const size_t at = block * (kTB * D) + (lane & 15) * 64 + (lane >> 4) * 16;
-        const uint8_t *kp = c.k8 + at, *vp = c.v8 + at;
+        const uint8_t* p = c.k8 + block * (kTB * D) + (lane & 15) * 64 + (lane >> 4) * 16;
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
-            for (int i = 0; i < D / 64; ++i) k[t][i] = *reinterpret_cast<const u32x4_t*>(kp + t * (16 * D) + i * 1024);
-#pragma unroll
-        for (int i = 0; i < D / 16; ++i) v[i] = *reinterpret_cast<const u32x4_t*>(vp + i * 1024);
-        ks = pow2(c.exps[block * 2]);
-        vs = pow2(c.exps[block * 2 + 1]);
+            for (int i = 0; i < D / 64; ++i) w[t][i] = *reinterpret_cast<const u32x4_t*>(p + t * (16 * D) + i * 1024);
+        s = pow2(c.exps[block * 2]);
     }
 };
+template <int D> struct VCodes {
+    u32x4_t w[D / 16];
+    float s;
+    __device__ __forceinline__ void load(const akb_cache& c, size_t block, int lane)
+    {
+        const uint8_t* p = c.v8 + block * (kTB * D) + (lane & 15) * 64 + (lane >> 4) * 16;
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) w[i] = *reinterpret_cast<const u32x4_t*>(p + i * 1024);
+        s = pow2(c.exps[block * 2 + 1]);
+    }
+};
+
+// A query row as the operand of S^T: step k of 32 channels, lane group g: channels 64 (k / 2) + 16 g + 8 (k % 2) .. + 7 (the order in which K's codes come)
+template <int D> __device__ __forceinline__ void load_query(u32x4_t (&q)[D / 32], const uint16_t* row, int lane)
+{
+#pragma unroll
+    for (int k = 0; k < D / 32; ++k) q[k] = row ? *reinterpret_cast<const u32x4_t*>(row + 64 * (k >> 1) + 16 * (lane >> 4) + 8 * (k & 1)) : u32x4_t{0, 0, 0, 0};
+}
 
 // Running state of a row tile in one wave: lane (row l % 16, g): channels 16 i + 4 g .. + 3 of O, the row's maximum, its share of the sum
 template <class T, int D> struct RowState {
     u32x4_t q[D / 32];
     f32x4_t o[D / 16];
     float m, z;
-    // channel order of the first product: step s of 32 channels, lane group g: 64 (s / 2) + 16 g + 8 (s % 2) .. + 7
-    __device__ __forceinline__ void init(const uint16_t* qrow, int lane)
+    int limit;
+    __device__ __forceinline__ void init(const uint16_t* qrow, int lim, int lane)
     {
-        const int g = lane >> 4;
-#pragma unroll
-        for (int s = 0; s < D / 32; ++s) q[s] = qrow ? *reinterpret_cast<const u32x4_t*>(qrow + 64 * (s >> 1) + 16 * g + 8 * (s & 1)) : u32x4_t{0, 0, 0, 0};
+        load_query<D>(q, qrow, lane);
 #pragma unroll
         for (int i = 0; i < D / 16; ++i) o[i] = f32x4_t{0, 0, 0, 0};
         m = -__builtin_inff();
         z = 0.f;
+        limit = lim;
     }
-    // S^T of 64 tokens -> weights; p[u]: tokens 32 u + .. as the operand of the second product (its high parts, and what they lack)
-    template <bool EXACT> __device__ __forceinline__ void weights(const f32x4_t (&s)[4], int first, int limit, bool masked, float c2, int lane, u32x4_t (&ph)[2], u32x4_t (&pl)[2])
+    // S^T of 64 tokens -> weights; ph[u]: tokens 32 u .. + 31 as the operand of the second product, pl: what 16 bits lack of them
+    template <bool EXACT> __device__ __forceinline__ void weights(f32x4_t (&s)[4], int first, bool masked, float c2, int lane, u32x4_t (&ph)[2], u32x4_t (&pl)[2])
     {
-        float x[4][4];
-        const int g = lane >> 4;
         float mx = -__builtin_inff();
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                x[t][r] = s[t][r] * c2;
-                if (masked && first + 16 * t + 4 * g + r >= limit) x[t][r] = -__builtin_inff();
-                mx = fmaxf(mx, x[t][r]);
+                if (masked && first + 16 * t + 4 * (lane >> 4) + r >= limit) s[t][r] = -__builtin_inff();
+                mx = fmaxf(mx, s[t][r]);
             }
-        mx = fmaxf(mx, __shfl_xor(mx, 16));
-        mx = fmaxf(mx, __shfl_xor(mx, 32));
-        const float m_new = fmaxf(m, mx - kWeightBits);
+        mx = max_lane32(max_lane16(mx));
+        const float m_new = fmaxf(m, fmaf(mx, c2, -kWeightBits));
         const float base = m_new == -__builtin_inff() ? 0.f : m_new;   // nothing seen yet: all weights are 2^-inf
-        const float a = __builtin_amdgcn_exp2f(m - base);
-        m = m_new;
+        if (__any(m_new != m)) {
+            const float a = __builtin_amdgcn_exp2f(m - base);
+            z *= a;
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i) o[i] *= a;
+            m = m_new;
+        }
         float sum = 0.f;
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                x[t][r] = __builtin_amdgcn_exp2f(x[t][r] - base);
-                sum += x[t][r];
+                s[t][r] = __builtin_amdgcn_exp2f(fmaf(s[t][r], c2, -base));
+                sum += s[t][r];
             }
-        z = fmaf(z, a, sum);
-#pragma unroll
-        for (int i = 0; i < D / 16; ++i) o[i] *= a;
+        z += sum;
 #pragma unroll
         for (int u = 0; u < 2; ++u)
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                const float p0 = x[2 * u + (k >> 1)][2 * (k & 1)], p1 = x[2 * u + (k >> 1)][2 * (k & 1) + 1];
+                const float p0 = s[2 * u + (k >> 1)][2 * (k & 1)], p1 = s[2 * u + (k >> 1)][2 * (k & 1) + 1];
                 ph[u][k] = T::pack(p0, p1);
                 if (EXACT) pl[u][k] = T::pack(p0 - T::lo(ph[u][k]), p1 - T::hi(ph[u][k]));
             }
     }
 };
 
-// One workgroup of four waves per (row tile, split): wave w takes every fourth block of the split, and the four states are put together
-// through LDS.  EXACT: 32-bit results; the weights go into the second product as two 16-bit numbers each (their sum carries 16 bits or more
-// where one carries 8 or 11, which is what a 16-bit result keeps).
-template <class T, int D, bool EXACT>
-__global__ __launch_bounds__(64 * kWaves) void rows_kernel(RowArgs a)
+// q . k of 64 tokens for the score, [tile of 16 tokens][row][16]: a store covers whole lines; lane (row, g) has four runs of four tokens
+__device__ __forceinline__ void store_logits(float* block, const f32x4_t (&s)[4], int rows, int row, int lane)
 {
-    __shared__ float o_s[kWaves][16][D + 4];
-    __shared__ float m_s[kWaves][16], z_s[kWaves][16];
+    if (row >= rows) return;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) __builtin_nontemporal_store(s[t], reinterpret_cast<f32x4_t*>(block + (t * rows + row) * 16 + 4 * (lane >> 4)));
+}
+
+template <class T> __device__ __forceinline__ void store_row(void* out, int out_dtype, size_t at, f32x4_t o)
+{
+    if (out_dtype == 0) *reinterpret_cast<f32x4_t*>(static_cast<float*>(out) + at) = o;
+    else *reinterpret_cast<u32x2_t*>(static_cast<uint16_t*>(out) + at) = u32x2_t{T::pack(o[0], o[1]), T::pack(o[2], o[3])};
+}
+
+// Four channels of a row, put together from parts
+struct Joined {
+    float top = -__builtin_inff(), z = 0.f;
+    f32x4_t o = {0, 0, 0, 0};
+    __device__ __forceinline__ void add(float m1, float z1, f32x4_t o1)
+    {
+        const float up = fmaxf(top, m1), base = up == -__builtin_inff() ? 0.f : up;
+        const float f = __builtin_amdgcn_exp2f(top - base), g = __builtin_amdgcn_exp2f(m1 - base);
+        z = fmaf(z, f, z1 * g);
+        o = o * f + o1 * g;
+        top = up;
+    }
+    __device__ __forceinline__ void put(float (&p)[6]) const
+    {
+        p[0] = top;
+        p[1] = z;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) p[2 + i] = o[i];
+    }
+    __device__ __forceinline__ void add(const float (&p)[6]) { add(p[0], p[1], f32x4_t{p[2], p[3], p[4], p[5]}); }
+    // the row's channels d .. d + 3 at `at` of out, and its statistics
+    template <class T> __device__ __forceinline__ void finish(const RowArgs& a, size_t first_row, int row, size_t at, int d) const
+    {
+        const float inv = z == 0.f ? 0.f : 1.f / z;   // zero: the row sees nothing
+        store_row<T>(a.out, a.out_dtype, at + d, o * inv);
+        if (a.stats && d == 0) {
+            float* p = a.stats + (first_row + row) * 2;
+            p[0] = top == -__builtin_inff() ? 0.f : top;
+            p[1] = inv;
+        }
+    }
+};
+
+// One workgroup of four waves per (row group of RT row tiles, split): wave w takes every fourth block of the split, and the four states are put together
+// through LDS.  Where a row group has several splits, the last of its workgroups to arrive joins them (the parts go through memory with device scope, as
+// the partial results of the 16-bit cache's V kernel do).  EXACT: 32-bit results; the weights go into the second product as two 16-bit numbers each (their
+// sum carries 16 bits or more where one carries 8 or 11, which is what a 16-bit result keeps).
+template <class T, int D, bool EXACT, int RT>
+__global__ __launch_bounds__(64 * kWaves, 2) void rows_kernel(RowArgs a)
+{
+    __shared__ float o_s[kWaves][kTileRows][D + 4];
+    __shared__ float m_s[kWaves][kTileRows], z_s[kWaves][kTileRows];
+    __shared__ int last_s;
+    constexpr int kRows = kTileRows * RT;
     const akb_cache& c = a.c;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int split = blockIdx.x % a.splits, group = blockIdx.x / a.splits, h = blockIdx.y, b = blockIdx.z;
-    const int G = c.shape.Hq / c.shape.Hkv, n = a.n;
+    Cut cut;
+    if (!cut.find<false>(a, 0)) return;
+    const unsigned w = cut.w;
+    const int splits = cut.splits, split = (w - cut.first) % splits, walk = (w - cut.first) / splits;
+    const int group = a.groups - 1 - walk % a.groups;   // the rows that see most go first
+    const int b = cut.b, G = c.shape.Hq / c.shape.Hkv, n = a.n;
+    const size_t pair = size_t(b) * c.shape.Hkv + walk / a.groups;
     const int len = seq_len(c, b), m = a.n_q ? min(max(a.n_q[b], 0), n) : n;
-    const size_t bh = size_t(b) * c.shape.Hkv + h;
-    const size_t item = bh * a.groups + group;
-    const int row = group * 16 + (lane & 15);
-    if (group * 16 >= m * G) return;   // no row of the tile is wanted
-    const int last_row = min(group * 16 + 15, m * G - 1);
-    const int keys = max(row_limit(last_row, G, m, len), 0), nb = (keys + kTB - 1) / kTB;
-    const int all_see = row_limit(group * 16, G, m, len);        // tokens that every row of the tile sees
-    const int limit = row_limit(row, G, m, len);
-    const int lo = (int)(long(nb) * split / a.splits), hi = (int)(long(nb) * (split + 1) / a.splits);
-    const int whole = min(hi, len / kTB);                         // blocks in 8 bits
-    RowState<T, D> st;
-    const int token = row / G, head = row % G;
-    const size_t out_row = (bh * G + head) * n + token;
-    st.init(row < m * G ? a.q + out_row * D : nullptr, lane);
+    const size_t bh = pair, item = bh * a.groups + group;
+    const int row0 = group * kRows, rows = min(kRows, m * G - row0);
+    if (rows <= 0) return;   // no row of the group is wanted (in any split)
+    const int keys = max(row_limit(row0 + rows - 1, G, m, len), 0), nb = (keys + kTB - 1) / kTB;
+    const int all_see = row_limit(row0, G, m, len);               // tokens that every row sees
+    const int lo = (int)(long(nb) * split / splits), hi = (int)(long(nb) * (split + 1) / splits);
+    const int whole = min(hi, len / kTB);                          // blocks in 8 bits
+    auto place = [&](int row) { return ((bh * G + row % G) * n + row / G) * D; };   // of a row in q and out
+    RowState<T, D> st[RT];
+#pragma unroll
+    for (int k = 0; k < RT; ++k) {
+        const int row = row0 + 16 * k + (lane & 15);
+        st[k].init(row < m * G ? a.q + place(row) : nullptr, row_limit(row, G, m, len), lane);
+    }
+    float* logits = RT == 1 && a.logits ? a.logits + bh * min(a.n * G, 16) * c.shape.Ncap : nullptr;
     const size_t block0 = bh * (c.shape.Ncap / kTB);
-    Codes<D> code;
     int blk = lo + wave;
+    KCodes<D> kc;
+    if (blk < whole) kc.load(c, block0 + blk, lane);
     for (; blk < whole; blk += kWaves) {
-        code.load(c, block0 + blk, lane);
-        f32x4_t s[4] = {};
+        VCodes<D> vc;
+        vc.load(c, block0 + blk, lane);
+        f32x4_t s[RT][4];
 #pragma unroll
-        for (int t = 0; t < 4; ++t)
+        for (int t = 0; t < 4; ++t) {
 #pragma unroll
-            for (int i = 0; i < D / 64; ++i) {
-                s[t] = T::mfma16(cvt8<T>(code.k[t][i][0], code.k[t][i][1], code.ks), st.q[2 * i], s[t]);
-                s[t] = T::mfma16(cvt8<T>(code.k[t][i][2], code.k[t][i][3], code.ks), st.q[2 * i + 1], s[t]);
+            for (int k = 0; k < RT; ++k) s[k][t] = f32x4_t{0, 0, 0, 0};
+#pragma unroll
+            for (int i = 0; i < D / 32; ++i) {
+                const u32x4_t x = cvt8<T>(kc.w[t][i >> 1][2 * (i & 1)], kc.w[t][i >> 1][2 * (i & 1) + 1], kc.s);
+#pragma unroll
+                for (int k = 0; k < RT; ++k) s[k][t] = T::mfma16(x, st[k].q[i], s[k][t]);
             }
-        u32x4_t ph[2], pl[2];
-        st.template weights<EXACT>(s, blk * kTB, limit, (blk + 1) * kTB > all_see, a.c2, lane, ph, pl);
+        }
+        if (blk + kWaves < whole) kc.load(c, block0 + blk + kWaves, lane);
+        if (RT == 1 && logits) store_logits(logits + size_t(blk) * kTB * rows, s[0], rows, lane & 15, lane);
+        const bool masked = (blk + 1) * kTB > all_see;
+        u32x4_t ph[RT][2], pl[RT][2];
+#pragma unroll
+        for (int k = 0; k < RT; ++k) st[k].template weights<EXACT>(s[k], blk * kTB, masked, a.c2, lane, ph[k], pl[k]);
 #pragma unroll
         for (int i = 0; i < D / 16; ++i)
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
-                const u32x4_t v = cvt8<T>(code.v[i][2 * u], code.v[i][2 * u + 1], code.vs);
-                st.o[i] = T::mfma16(v, ph[u], st.o[i]);
-                if (EXACT) st.o[i] = T::mfma16(v, pl[u], st.o[i]);
+                const u32x4_t v = cvt8<T>(vc.w[i][2 * u], vc.w[i][2 * u + 1], vc.s);
+#pragma unroll
+                for (int k = 0; k < RT; ++k) {
+                    st[k].o[i] = T::mfma16(v, ph[k][u], st[k].o[i]);
+                    if (EXACT) st[k].o[i] = T::mfma16(v, pl[k][u], st[k].o[i]);
+                }
             }
     }
     if (blk < hi) {   // the incomplete block, in 16 bits
         const uint16_t *kt = c.k_tail + bh * kTB * D, *vt = c.v_tail + bh * kTB * D;
         const int g = lane >> 4, left = len - blk * kTB;
-        f32x4_t s[4] = {};
+        f32x4_t s[RT][4] = {};
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
-            for (int k = 0; k < D / 32; ++k)
-                s[t] = T::mfma16(*reinterpret_cast<const u32x4_t*>(kt + (16 * t + (lane & 15)) * D + 64 * (k >> 1) + 16 * g + 8 * (k & 1)), st.q[k], s[t]);
-        u32x4_t ph[2], pl[2];
-        st.template weights<EXACT>(s, blk * kTB, min(limit, len), true, a.c2, lane, ph, pl);
+            for (int i = 0; i < D / 32; ++i) {
+                const u32x4_t x = *reinterpret_cast<const u32x4_t*>(kt + (16 * t + (lane & 15)) * D + 64 * (i >> 1) + 16 * g + 8 * (i & 1));
+#pragma unroll
+                for (int k = 0; k < RT; ++k) s[k][t] = T::mfma16(x, st[k].q[i], s[k][t]);
+            }
+        if (RT == 1 && logits) store_logits(logits + size_t(blk) * kTB * rows, s[0], rows, lane & 15, lane);
+        u32x4_t ph[RT][2], pl[RT][2];
+#pragma unroll
+        for (int k = 0; k < RT; ++k) st[k].template weights<EXACT>(s[k], blk * kTB, true, a.c2, lane, ph[k], pl[k]);
 #pragma unroll
         for (int i = 0; i < D / 16; ++i)
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
                 u32x4_t v = *reinterpret_cast<const u32x4_t*>(vt + (16 * i + (lane & 15)) * kTB + 16 * g + 8 * u);
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {   // what lies behind the length may be anything: zero, so that a weight of zero makes zero of it
-                    const int t = 16 * (2 * u + (k >> 1)) + 4 * g + 2 * (k & 1);
-                    v[k] = t + 1 < left ? v[k] : (t < left ? v[k] & 0xFFFFu : 0u);
+                for (int e = 0; e < 4; ++e) {   // what lies behind the length may be anything: zero, so that a weight of zero makes zero of it
+                    const int t = 16 * (2 * u + (e >> 1)) + 4 * g + 2 * (e & 1);
+                    v[e] = t + 1 < left ? v[e] : (t < left ? v[e] & 0xFFFFu : 0u);
                 }
-                st.o[i] = T::mfma16(v, ph[u], st.o[i]);
-                if (EXACT) st.o[i] = T::mfma16(v, pl[u], st.o[i]);
+#pragma unroll
+                for (int k = 0; k < RT; ++k) {
+                    st[k].o[i] = T::mfma16(v, ph[k][u], st[k].o[i]);
+                    if (EXACT) st[k].o[i] = T::mfma16(v, pl[k][u], st[k].o[i]);
+                }
             }
     }
-    float z = st.z;
-    z += __shfl_xor(z, 16);
-    z += __shfl_xor(z, 32);
-    if (lane < 16) {
-        m_s[wave][lane] = st.m;
-        z_s[wave][lane] = z;
-    }
+    const int part = part_floats(rows, D);
+    const __amdgpu_buffer_rsrc_t parts = akv::make_rsrc(a.parts + size_t(w - split) * part_floats(min(n * G, kRows), D), uint32_t(splits) * part * 4u);
 #pragma unroll
-    for (int i = 0; i < D / 16; ++i) *reinterpret_cast<f32x4_t*>(&o_s[wave][lane & 15][16 * i + 4 * (lane >> 4)]) = st.o[i];
-    __syncthreads();
-    // four consecutive channels of one row per thread and turn
-    for (int e = threadIdx.x; e < 16 * D / 4; e += 64 * kWaves) {
-        const int r = e / (D / 4), d = e % (D / 4) * 4;
-        float top = m_s[0][r];
-#pragma unroll
-        for (int w = 1; w < kWaves; ++w) top = fmaxf(top, m_s[w][r]);
-        const float base = top == -__builtin_inff() ? 0.f : top;
-        f32x4_t o = {0, 0, 0, 0};
-        float zz = 0.f;
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
-            const float f = __builtin_amdgcn_exp2f(m_s[w][r] - base);
-            zz = fmaf(z_s[w][r], f, zz);
-            o += *reinterpret_cast<const f32x4_t*>(&o_s[w][r][d]) * f;
+    for (int k = 0; k < RT; ++k) {
+        if (16 * k >= rows) break;
+        if (k) __syncthreads();   // the tile before has been put together
+        const float z = akv::add_lane32(akv::add_lane16(st[k].z));
+        if (lane < 16) {
+            m_s[wave][lane] = st[k].m;
+            z_s[wave][lane] = z;
         }
-        if (a.splits > 1) {
-            float* p = a.parts + (item * a.splits + split) * part_floats<D>();
-            *reinterpret_cast<f32x4_t*>(p + r * D + d) = o;
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) *reinterpret_cast<f32x4_t*>(&o_s[wave][lane & 15][16 * i + 4 * (lane >> 4)]) = st[k].o[i];
+        __syncthreads();
+        // four consecutive channels of one row per thread and turn
+        for (int e = threadIdx.x; e < min(16, rows - 16 * k) * (D / 4); e += 64 * kWaves) {
+            const int r = e / (D / 4), d = e % (D / 4) * 4;
+            Joined j;
+            j.top = m_s[0][r];
+#pragma unroll
+            for (int w = 1; w < kWaves; ++w) j.top = fmaxf(j.top, m_s[w][r]);
+            const float base = j.top == -__builtin_inff() ? 0.f : j.top;
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) {
+                const float f = __builtin_amdgcn_exp2f(m_s[w][r] - base);
+                j.z = fmaf(z_s[w][r], f, j.z);
+                j.o += *reinterpret_cast<const f32x4_t*>(&o_s[w][r][d]) * f;
+            }
+            if (splits == 1) {
+                j.template finish<T>(a, bh * n * G, row0 + 16 * k + r, place(row0 + 16 * k + r), d);
+                continue;
+            }
+            const uint32_t at = uint32_t(split) * part;
+            akv::buf_store_b128_agent(__builtin_bit_cast(u32x4_t, j.o), parts, (at + part_head(rows) + (16 * k + r) * D + d) * 4);
             if (d == 0) {
-                p[16 * D + 2 * r] = top;
-                p[16 * D + 2 * r + 1] = zz;
-            }
-        } else if (group * 16 + r < m * G) {
-            const float inv = zz > 0.f || zz != zz ? 1.f / zz : 0.f;
-            o *= inv;
-            const int rr = group * 16 + r;
-            const size_t at = ((bh * G + rr % G) * n + rr / G) * D + d;
-            if (a.out_dtype == 0) *reinterpret_cast<f32x4_t*>(static_cast<float*>(a.out) + at) = o;
-            else *reinterpret_cast<u32x2_t*>(static_cast<uint16_t*>(a.out) + at) = u32x2_t{T::pack(o[0], o[1]), T::pack(o[2], o[3])};
-            if (a.stats && d == 0) {
-                a.stats[(item * 16 + r) * 2] = base;
-                a.stats[(item * 16 + r) * 2 + 1] = inv;
+                __builtin_amdgcn_raw_buffer_store_b32(float_bits(j.top), parts, (at + 2 * (16 * k + r)) * 4, 0, akv::kAuxSc1);
+                __builtin_amdgcn_raw_buffer_store_b32(float_bits(j.z), parts, (at + 2 * (16 * k + r) + 1) * 4, 0, akv::kAuxSc1);
             }
         }
+    }
+    if (splits == 1 || !a.tickets) return;
+    akv::stores_done();
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        const int t = akv::take_ticket(a.tickets + item);
+        last_s = t == splits - 1;
+        if (last_s) akv::store_agent(a.tickets + item, 0);
+    }
+    __syncthreads();
+    if (!last_s) return;
+    // the parts joined: a thread has kPer runs of four channels of a row, all splits; where there are few rows, one run in every `slices`-th split, and
+    // the slices meet in LDS
+    constexpr int kPer = kRows * (D / 4) / (64 * kWaves);
+    const int work_items = rows * (D / 4), slices = 64 * kWaves / work_items;
+    const int step = max(slices, 1), slice = slices > 1 ? int(threadIdx.x) / work_items : 0, e0 = slices > 1 ? int(threadIdx.x) % work_items : int(threadIdx.x);
+    Joined j[kPer];
+    if (slice < step)
+#pragma unroll 4
+        for (int s = slice; s < splits; s += step) {
+            const uint32_t at = uint32_t(s) * part;
+            u32x2_t mz[kPer];
+            u32x4_t x[kPer];
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) {   // (beyond the rows: beyond the buffer, which gives zeros, or another split's numbers; not used)
+                const int e = e0 + 64 * kWaves * i;
+                mz[i] = __builtin_amdgcn_raw_buffer_load_b64(parts, (at + 2 * (e / (D / 4))) * 4, 0, akv::kAuxSc1);
+                x[i] = akv::buf_load_b128_agent(parts, (at + part_head(rows) + e * 4) * 4);
+            }
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) j[i].add(bits_float(mz[i].x), bits_float(mz[i].y), __builtin_bit_cast(f32x4_t, x[i]));
+        }
+    if (slices > 1) {
+        float(*mine)[6] = reinterpret_cast<float(*)[6]>(&o_s[0][0][0]);
+        j[0].put(mine[threadIdx.x]);
+        __syncthreads();
+        if (int(threadIdx.x) < work_items)
+            for (int s = 1; s < slices; ++s) j[0].add(mine[threadIdx.x + s * work_items]);
+    }
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        const int e = int(threadIdx.x) + 64 * kWaves * i, r = e / (D / 4);
+        if (e < work_items) j[i].template finish<T>(a, bh * n * G, row0 + r, place(row0 + r), e % (D / 4) * 4);
     }
 }
 
-// The parts of a row tile put together: one workgroup per row tile.
+// The parts joined by a launch of their own: one workgroup of 256 threads per row, a thread with four channels of every eighth (D = 128; sixteenth) split.
 template <class T, int D>
-__global__ __launch_bounds__(256) void join_kernel(RowArgs a)
+__global__ __launch_bounds__(256) void join_kernel(RowArgs a, int group_rows)
+{
+    constexpr int kSlices = 256 / (D / 4);
+    __shared__ float x_s[256][6];
+    const akb_cache& c = a.c;
+    const int G = c.shape.Hq / c.shape.Hkv, n = a.n;
+    const unsigned pair = blockIdx.y;
+    const int b = pair / c.shape.Hkv, row = blockIdx.x;
+    const int m = a.n_q ? min(max(a.n_q[b], 0), n) : n;
+    if (row >= m * G) return;
+    Cut cut;
+    cut.find<true>(a, b);
+    const int splits = cut.splits;
+    if (splits == 1) return;   // its rows are there already
+    const int group = row / group_rows, r = row % group_rows, rows = min(group_rows, m * G - group * group_rows), part = part_floats(rows, D);
+    const unsigned walk = (pair % c.shape.Hkv) * a.groups + a.groups - 1 - group;   // as the rows kernel counts them
+    const float* parts = a.parts + (size_t(cut.first) + size_t(walk) * splits) * part_floats(min(n * G, group_rows), D);
+    const int d = threadIdx.x % (D / 4) * 4, slice = threadIdx.x / (D / 4);
+    Joined j;
+#pragma unroll 8
+    for (int s = slice; s < splits; s += kSlices) {
+        const float* p = parts + size_t(s) * part;
+        j.add(p[2 * r], p[2 * r + 1], *reinterpret_cast<const f32x4_t*>(p + part_head(rows) + r * D + d));
+    }
+    j.put(x_s[threadIdx.x]);
+    __syncthreads();
+    if (slice) return;
+    for (int s = 1; s < kSlices; ++s) j.add(x_s[threadIdx.x + s * (D / 4)]);
+    j.template finish<T>(a, size_t(pair) * n * G, row, ((size_t(pair) * G + row % G) * n + row / G) * D, d);
+}
+
+// score[t] += sum over the rows of exp2(x - maximum) / sum, from the x that the rows kernel has left: calls of one row group, whose x are fewer bytes than
+// K's codes or not many more.  A thread has four tokens.
+__global__ __launch_bounds__(256) void score_logits_kernel(RowArgs a)
 {
     const akb_cache& c = a.c;
-    const int group = blockIdx.x, h = blockIdx.y, b = blockIdx.z, G = c.shape.Hq / c.shape.Hkv, n = a.n;
-    const int m = a.n_q ? min(max(a.n_q[b], 0), n) : n;
-    const size_t bh = size_t(b) * c.shape.Hkv + h, item = bh * a.groups + group;
-    const float* parts = a.parts + item * a.splits * part_floats<D>();
-    for (int e = threadIdx.x; e < 16 * D / 4; e += 256) {
-        const int r = e / (D / 4), d = e % (D / 4) * 4, rr = group * 16 + r;
-        if (rr >= m * G) continue;
-        float top = -__builtin_inff();
-        for (int s = 0; s < a.splits; ++s) top = fmaxf(top, parts[size_t(s) * part_floats<D>() + 16 * D + 2 * r]);
-        const float base = top == -__builtin_inff() ? 0.f : top;
-        f32x4_t o = {0, 0, 0, 0};
-        float zz = 0.f;
-        for (int s = 0; s < a.splits; ++s) {
-            const float* p = parts + size_t(s) * part_floats<D>();
-            const float f = __builtin_amdgcn_exp2f(p[16 * D + 2 * r] - base);
-            zz = fmaf(p[16 * D + 2 * r + 1], f, zz);
-            o += *reinterpret_cast<const f32x4_t*>(p + r * D + d) * f;
+    const int h = blockIdx.y, b = blockIdx.z, G = c.shape.Hq / c.shape.Hkv;
+    const int len = seq_len(c, b), m = a.n_q ? min(max(a.n_q[b], 0), a.n) : a.n, rows = m * G;
+    const size_t bh = size_t(b) * c.shape.Hkv + h;
+    const float* stats = a.stats + bh * a.n * G * 2;
+    for (int t = (blockIdx.x * 256 + threadIdx.x) * 4; t < len; t += gridDim.x * 1024) {
+        const float* x = a.logits + bh * min(a.n * G, 16) * c.shape.Ncap + size_t(t / 16) * 16 * rows + t % 16;
+        f32x4_t* p = reinterpret_cast<f32x4_t*>(c.score + bh * c.shape.Ncap + t);
+        f32x4_t acc = *p;
+#pragma unroll 4
+        for (int r = 0; r < rows; ++r) {
+            const f32x4_t v = *reinterpret_cast<const f32x4_t*>(x + r * 16);
+            const float base = stats[2 * r], inv = stats[2 * r + 1];
+            const int limit = row_limit(r, G, m, len);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (t + i < limit) acc[i] = fmaf(__builtin_amdgcn_exp2f(fmaf(v[i], a.c2, -base)), inv, acc[i]);
         }
-        const float inv = zz > 0.f || zz != zz ? 1.f / zz : 0.f;
-        o *= inv;
-        const size_t at = ((bh * G + rr % G) * n + rr / G) * D + d;
-        if (a.out_dtype == 0) *reinterpret_cast<f32x4_t*>(static_cast<float*>(a.out) + at) = o;
-        else *reinterpret_cast<u32x2_t*>(static_cast<uint16_t*>(a.out) + at) = u32x2_t{T::pack(o[0], o[1]), T::pack(o[2], o[3])};
-        if (a.stats && d == 0) {
-            a.stats[(item * 16 + r) * 2] = base;
-            a.stats[(item * 16 + r) * 2 + 1] = inv;
-        }
+        *p = acc;   // (the last of the four may lie behind the length: as they were)
     }
 }
 
@@ -302,14 +536,14 @@ __global__ __launch_bounds__(64 * kWaves) void score_kernel(RowArgs a)
     for (int blk = blockIdx.x; blk * kTB < len; blk += gridDim.x) {
         u32x4_t k[4][D / 32];
         if (blk < len / kTB) {
-            Codes<D> code;
+            KCodes<D> code;
             code.load(c, bh * (c.shape.Ncap / kTB) + blk, lane);
     #pragma unroll
             for (int t = 0; t < 4; ++t)
     #pragma unroll
                 for (int i = 0; i < D / 64; ++i) {
-                    k[t][2 * i] = cvt8<T>(code.k[t][i][0], code.k[t][i][1], code.ks);
-                    k[t][2 * i + 1] = cvt8<T>(code.k[t][i][2], code.k[t][i][3], code.ks);
+                    k[t][2 * i] = cvt8<T>(code.w[t][i][0], code.w[t][i][1], code.s);
+                    k[t][2 * i + 1] = cvt8<T>(code.w[t][i][2], code.w[t][i][3], code.s);
                 }
         } else {
             const uint16_t* kt = c.k_tail + bh * kTB * D;
@@ -324,15 +558,15 @@ __global__ __launch_bounds__(64 * kWaves) void score_kernel(RowArgs a)
             const int row = tile * 16 + (lane & 15);
             const int limit = min(row_limit(row, G, m, len), len);
             if (row_limit(min(tile * 16 + 15, m * G - 1), G, m, len) <= blk * kTB) continue;   // no row of the tile sees the block
-            RowState<T, D> st;
-            st.init(row < m * G ? a.q + ((bh * G + row % G) * n + row / G) * D : nullptr, lane);
-            const float* p = a.stats + ((bh * a.groups + tile) * 16 + (lane & 15)) * 2;
+            u32x4_t q[D / 32];
+            load_query<D>(q, row < m * G ? a.q + ((bh * G + row % G) * n + row / G) * D : nullptr, lane);
+            const float* p = a.stats + (bh * n * G + row) * 2;
             const float base = row < m * G ? p[0] : 0.f, inv = row < m * G ? p[1] : 0.f;
     #pragma unroll
             for (int t = 0; t < 4; ++t) {
                 f32x4_t s = {0, 0, 0, 0};
     #pragma unroll
-                for (int i = 0; i < D / 32; ++i) s = T::mfma16(k[t][i], st.q[i], s);
+                for (int i = 0; i < D / 32; ++i) s = T::mfma16(k[t][i], q[i], s);
     #pragma unroll
                 for (int r = 0; r < 4; ++r)
                     if (blk * kTB + 16 * t + 4 * g + r < limit) acc[t][r] = fmaf(__builtin_amdgcn_exp2f(s[r] * a.c2 - base), inv, acc[t][r]);
@@ -360,28 +594,33 @@ __global__ __launch_bounds__(64 * kWaves) void score_kernel(RowArgs a)
     }
 }
 
-template <class T, int D> static hipError_t launch(const RowArgs& r, int max_len, hipStream_t st)
+template <class T, int D> static hipError_t launch(const RowArgs& r, const AttentionPlan& p, int max_len, hipStream_t st)
 {
     const akb_shape& s = r.c.shape;
-    const dim3 grid(r.groups * r.splits, s.Hkv, s.B);
-    if (r.out_dtype == 0) hipLaunchKernelGGL((rows_kernel<T, D, true>), grid, dim3(64 * kWaves), 0, st, r);
-    else hipLaunchKernelGGL((rows_kernel<T, D, false>), grid, dim3(64 * kWaves), 0, st, r);
+    const int tiles = p.tiles, grid = p.grid;
+    auto rows = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(akv::xcd_grid(grid)), dim3(64 * kWaves), 0, st, r); };
+    if (r.out_dtype == 0) tiles == 1 ? rows(rows_kernel<T, D, true, 1>) : rows(rows_kernel<T, D, true, 2>);
+    else tiles == 1 ? rows(rows_kernel<T, D, false, 1>) : rows(rows_kernel<T, D, false, 2>);
     if (hipError_t e = hipGetLastError()) return e;
-    if (r.splits > 1) {
-        hipLaunchKernelGGL((join_kernel<T, D>), dim3(r.groups, s.Hkv, s.B), dim3(256), 0, st, r);
+    if (r.splits != 1 && !r.tickets) {
+        const int rows_all = r.n * (s.Hq / s.Hkv);
+        hipLaunchKernelGGL((join_kernel<T, D>), dim3(rows_all, s.B * s.Hkv), dim3(256), 0, st, r, 16 * tiles);
         if (hipError_t e = hipGetLastError()) return e;
     }
-    if (r.stats) hipLaunchKernelGGL((score_kernel<T, D>), dim3((max_len + kTB - 1) / kTB, s.Hkv, s.B), dim3(64 * kWaves), 0, st, r);
+    const int blocks = (max_len + kTB - 1) / kTB;
+    if (r.logits) hipLaunchKernelGGL(score_logits_kernel, dim3((blocks + 15) / 16, s.Hkv, s.B), dim3(256), 0, st, r);
+    else if (r.stats) hipLaunchKernelGGL((score_kernel<T, D>), dim3(blocks, s.Hkv, s.B), dim3(64 * kWaves), 0, st, r);
     return hipGetLastError();
 }
 
 hipError_t launch_attention(const AttentionArgs& a, hipStream_t st)
 {
     const AttentionPlan p = plan(a.c.shape, a.n, a.max_len, a.accumulate);
-    RowArgs r{a.c, a.q, a.n_q, a.n, p.groups, p.splits, a.out_dtype, a.out, a.c2, reinterpret_cast<float*>(a.ws + p.parts),
+    RowArgs r{a.c, a.q, a.n_q, a.n, p.groups, p.splits, p.grid, a.out_dtype, a.out, a.c2, p.ticketed ? reinterpret_cast<int32_t*>(a.ws + p.tickets) : nullptr,
+              reinterpret_cast<float*>(a.ws + p.parts), a.accumulate && p.tiles == 1 ? reinterpret_cast<float*>(a.ws + p.logits) : nullptr,
               a.accumulate ? reinterpret_cast<float*>(a.ws + p.stats) : nullptr};
-    if (a.c.shape.dtype == AKB_FP16) return a.c.shape.D == 64 ? launch<Fp16, 64>(r, a.max_len, st) : launch<Fp16, 128>(r, a.max_len, st);
-    return a.c.shape.D == 64 ? launch<Bf16, 64>(r, a.max_len, st) : launch<Bf16, 128>(r, a.max_len, st);
+    if (a.c.shape.dtype == AKB_FP16) return a.c.shape.D == 64 ? launch<Fp16, 64>(r, p, a.max_len, st) : launch<Fp16, 128>(r, p, a.max_len, st);
+    return a.c.shape.D == 64 ? launch<Bf16, 64>(r, p, a.max_len, st) : launch<Bf16, 128>(r, p, a.max_len, st);
 }
 
 }  // namespace akb

@@ -33,6 +33,7 @@ struct AttentionArgs {
     char* ws;
 };
 size_t attention_workspace(const akb_shape& s, int n, bool accumulate);
+size_t attention_tickets();   // bytes at the front of a workspace that are zero between calls
 hipError_t launch_attention(const AttentionArgs& a, hipStream_t st);
 
 #if defined(__HIPCC__)
@@ -109,6 +110,17 @@ __device__ __forceinline__ uint32_t pack_codes(float a, float b, float c, float 
     return uint32_t(__builtin_amdgcn_cvt_pk_fp8_f32(c, d, __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false), true));
 }
 
+// the larger of a value and that of the lane 16 / 32 further (mod the pairs of rows / the halves), in both
+__device__ __forceinline__ float max_lane16(float v)
+{
+    const auto s = __builtin_amdgcn_permlane16_swap(float_bits(v), float_bits(v), false, false);
+    return fmaxf(bits_float(s[0]), bits_float(s[1]));
+}
+__device__ __forceinline__ float max_lane32(float v)
+{
+    const auto s = __builtin_amdgcn_permlane32_swap(float_bits(v), float_bits(v), false, false);
+    return fmaxf(bits_float(s[0]), bits_float(s[1]));
+}
 // A barrier for data in LDS alone: loads from memory that are in flight stay so (__syncthreads waits for them)
 __device__ __forceinline__ void lds_barrier()
 {
