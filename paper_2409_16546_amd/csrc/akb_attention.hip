@@ -1,24 +1,10 @@
 // Attention over the block-scaled 8-bit cache (rules and layout: include/akb.h).
 //
-// Rows: the query rows of one (sequence, KV head) are its n_q query tokens times its G query heads, row = token * G + head, so
-// that one walk over K and V serves the whole group; 16 rows form a matrix tile.
-// Both products are taken transposed, S^T = K Q^T and O^T = V^T P^T, so that a lane's column is a query row throughout: its
-// four scores of a tile are four tokens of one row, which is what the second product takes as its operand (V's bytes lie in
-// that order), and the running maximum, the sum and the rescaling of a row need no value of another row's lanes.
-#include "akb_common.h"
+#include "akb_rows.h"
 
 namespace akb {
 
-// In 16 bits the weights of fp16 caches would lose bits below 2^-14: they are taken relative to 2^-14 of the maximum (up to 2^14).
-constexpr float kWeightBits = 14.f;
-constexpr int kWaves = 4;
 constexpr int kTileRows = 16;
-
-// What one split of a row group leaves for the workgroup that joins them: per row (maximum, sum), padded to 16 bytes, then O [row][D]
-__host__ __device__ constexpr int part_head(int rows) { return (2 * rows + 3) / 4 * 4; }
-__host__ __device__ constexpr int part_floats(int rows, int D) { return part_head(rows) + rows * D; }
-
-constexpr int kMostCut = 256;   // sequences whose lengths every workgroup looks through
 
 // How the walks over the blocks (one per row group) are shared out.  `slots` workgroups run at a time, two per compute unit (three or four per unit measured
 // behind: their fixed costs, parts to write and join, outweigh what more loads in flight give; 8 x 8 pairs of 4096 tokens 15.6 / 18.3 / 19.4 us).  Where there
@@ -27,113 +13,46 @@ constexpr int kMostCut = 256;   // sequences whose lengths every workgroup looks
 // 123 us).  Elsewhere every walk is cut into the same number of parts: a short call would wait for the lengths (8.0 -> 9.9 us), and with many walks the
 // parts that are not full cost what they even out (16 x 32 pairs of 2048 to 8192 tokens 131 -> 145 us).
 struct AttentionPlan {
-    int tiles;      // row tiles of a row group: 1, 2
+    int tiles;      // row tiles of a row group: 1, 2 (rows kernel), 8 (prompt kernel)
     int groups;     // row groups of a (sequence, KV head)
     int splits;     // parts of a walk, or 0: cut by the device
     int grid;       // workgroups at most
     bool ticketed;  // the last workgroup of a row group joins its parts; otherwise a launch does
     size_t tickets, parts, logits, stats, total;   // offsets into the workspace
 };
-// Row tiles that share a walk over K and V.
-static int tiles_for(long rows) { return rows <= 16 ? 1 : 2; }
+// Parts of each of `items` walks: none where they fill the slots; at most 2 slots parts in all, which is what the workspace has room for.
+static long parts_of(long items, long blocks, long slots)
+{
+    return items >= slots ? 1 : std::max(1L, std::min({(slots + items - 1) / items, (blocks + kWaves - 1) / kWaves, 2 * slots / items}));
+}
 static AttentionPlan plan(const akb_shape& s, int n, int max_len, bool accumulate)
 {
     AttentionPlan p;
-    const long slots = 2L * akv::compute_units(), rows = long(n) * (s.Hq / s.Hkv), pairs = long(s.B) * s.Hkv;
-    p.tiles = tiles_for(rows);
-    p.groups = (int)((rows + 16 * p.tiles - 1) / (16 * p.tiles));
-    const long items = pairs * p.groups, blocks = (max_len + kTB - 1) / kTB;
-    const long splits = items >= slots ? 1 : std::max(1L, std::min((slots + items - 1) / items, (blocks + kWaves - 1) / kWaves));
+    const long slots = 2L * akv::compute_units(), rows = long(n) * (s.Hq / s.Hkv), pairs = long(s.B) * s.Hkv, blocks = (max_len + kTB - 1) / kTB;
+    auto items_of = [&](int tiles) { return pairs * ((rows + 16 * tiles - 1) / (16 * tiles)); };
+    // The prompt kernel from 65 rows on, where its parts are 12 blocks or longer (it fills a pipeline, and its parts have 128 rows to write and join).  Rows / prompt
+    // kernel, us: 32 pairs of 5000 tokens 256 rows 38.8 / 42.6, 1024 rows 111 / 103; 32 of 5000, 100 rows 25.2 / 29.0; 64 of 3000, 160 rows 41.6 / 40.2; 8 of
+    // 20000, 2048 rows 206 / 182; 8 of 100000, 64 rows 57 / 70; 24 of 13000, 40 rows 25.6 / 39.5; a prompt of 8192 tokens, 8 pairs of 32768 rows 730 / 558.
+    constexpr int kPromptTiles = kPromptRows / 16;
+    const long prompt_items = items_of(kPromptTiles);
+    p.tiles = rows <= 16 ? 1 : (rows > 64 && blocks >= 12 * parts_of(prompt_items, blocks, slots) ? kPromptTiles : 2);
+    const long items = items_of(p.tiles), splits = parts_of(items, blocks, slots);
+    p.groups = (int)(items / pairs);
     p.splits = s.B > 1 && s.B <= kMostCut && items * 4 <= slots && blocks >= 8 * kWaves * splits ? 0 : (int)splits;
     p.grid = (int)(p.splits ? items * p.splits : slots);
-    // Joined by the last workgroup where that has little to read (a launch less), by a launch of one workgroup per row where it has much: rows x parts per row
-    // group 4 7.4 / 11.0 us, 48 11.6 / 14.4, 64 40.5 / 45.1; 128 23.2 / 20.9, 350 29.7 / 25.9, 512 27.9 / 19.3 (last workgroup / launch).
-    p.ticketed = std::min(rows, 16L * p.tiles) * splits <= 64;
-    // (calls of fewer query tokens fit into what is laid out for more: fewer than `2 slots` parts of up to 32 rows, and as many tickets)
+    // Joined by the last workgroup where that has little to read (a launch less), by a launch of its own where it has much: rows x parts per row group 4 7.4 /
+    // 11.0 us, 48 11.6 / 14.4, 64 40.5 / 45.1; 128 23.2 / 20.9, 350 29.7 / 25.9, 512 27.9 / 19.3 (last workgroup / launch).
+    p.ticketed = p.tiles <= 2 && std::min(rows, 16L * p.tiles) * splits <= 64;
+    // (calls of fewer query tokens fit into what is laid out for more: at most `2 slots` parts of up to 128 rows, and as many tickets)
     p.tickets = 0;
     p.parts = align256(size_t(2 * slots) * sizeof(int32_t));
-    p.logits = p.parts + align256(size_t(2 * slots) * part_floats((int)std::min(rows, 32L), s.D) * sizeof(float));
+    p.logits = p.parts + align256(size_t(2 * slots) * part_floats((int)std::min(rows, long(kPromptRows)), s.D) * sizeof(float));
     p.stats = p.logits + (accumulate ? align256(size_t(pairs) * std::min(rows, 16L) * s.Ncap * sizeof(float)) : 0);
     p.total = p.stats + (accumulate ? align256(size_t(pairs) * rows * 2 * sizeof(float)) : 0);
     return p;
 }
 size_t attention_workspace(const akb_shape& s, int n, bool accumulate) { return plan(s, std::max(n, 1), s.Ncap, accumulate).total; }
 size_t attention_tickets() { return size_t(4) * akv::compute_units() * sizeof(int32_t); }
-
-struct RowArgs {
-    akb_cache c;
-    const uint16_t* q;
-    const int32_t* n_q;
-    int n, groups, splits, slots, out_dtype;
-    void* out;
-    float c2;
-    int32_t* tickets;   // [sequence, KV head, row group]: splits that have arrived, zero between calls; NULL: join_kernel follows
-    float *parts, *logits, *stats;   // logits: q . k of the one row group, [sequence, KV head][block][tile][row][16]; stats: (maximum, 1 / sum) per row; or NULL
-};
-
-// The tokens that rows see: row r (its query token r / G of m) the first `limit`
-__device__ __forceinline__ int row_limit(int row, int G, int m, int len) { return row < m * G ? len - m + row / G + 1 : 0; }
-
-// How the walks of a call are cut: the same in every wave that asks.  Lane l has sequences l, l + 64, ..
-struct Cut {
-    unsigned w;        // this workgroup's number among those that have work
-    int b, splits;     // its sequence, the parts of its walks
-    unsigned first;    // the sequence's first workgroup
-    // An XCD has one stretch of the work, so that the row groups and parts of a (sequence, KV head) share its L2 (workgroups are dealt to the XCDs in turn):
-    // false where none is left.
-    __device__ __forceinline__ bool stretch(unsigned n)
-    {
-        const unsigned per = (n + akv::kXcds - 1) / akv::kXcds, x = blockIdx.x % akv::kXcds, i = blockIdx.x / akv::kXcds;
-        w = x * per + i;
-        return i < per && w < n;
-    }
-    // OF: of sequence `of`; otherwise of this workgroup; false where there is no work for it
-    template <bool OF> __device__ __forceinline__ bool find(const RowArgs& a, int of)
-    {
-        const int B = a.c.shape.B, walks = a.c.shape.Hkv * a.groups, lane = threadIdx.x & 63;   // walks: per sequence
-        splits = a.splits;
-        if (splits) {
-            if (!OF && !stretch(unsigned(B) * walks * splits)) return false;
-            b = OF ? of : int(w / unsigned(walks * splits));
-            first = unsigned(b) * walks * splits;
-            return true;
-        }
-        constexpr int kTurns = kMostCut / 64;
-        int nb[kTurns];   // blocks of sequence 64 i + lane
-#pragma unroll
-        for (int i = 0; i < kTurns; ++i) {
-            const int s = 64 * i + lane;
-            nb[i] = s < B && (!a.n_q || a.n_q[s] > 0) ? (seq_len(a.c, s) + kTB - 1) / kTB : 0;
-        }
-        unsigned total = 0;   // fewer than 2^25: at most 128 walks of 65536 blocks (and at least one part per walk in the `slots`)
-#pragma unroll
-        for (int i = 0; i < kTurns; ++i)
-            if (64 * i < B) total += akv::wave_read(akv::wave_scan_add(nb[i]), 63);
-        // the sum of all ceil(blocks / q) is below total / q + walks, so it fits the slots
-        const unsigned most = a.slots - B * walks, q = max(unsigned(kWaves), (total * walks + most - 1) / most);
-        auto parts = [&](int i) { return 64 * i + lane < B ? max(int((nb[i] + q - 1) / q), 1) : 0; };
-        unsigned n = 0, before = 0;
-#pragma unroll
-        for (int i = 0; i < kTurns; ++i)
-            if (64 * i < B) n += akv::wave_read(akv::wave_scan_add(parts(i)), 63);
-        if (!OF && !stretch(n * walks)) return false;
-        b = B;
-#pragma unroll
-        for (int i = 0; i < kTurns; ++i) {
-            if (64 * i >= B || b < B) continue;
-            const int mine = parts(i), upto = akv::wave_scan_add(mine);
-            const bool here = 64 * i + lane < B && (OF ? 64 * i + lane == of : (before + unsigned(upto)) * walks > w);
-            if (const uint64_t past = __ballot(here)) {
-                const int l = __builtin_ctzll(past);
-                b = 64 * i + l;
-                splits = akv::wave_read(mine, l);
-                first = (before + unsigned(akv::wave_read(upto, l)) - splits) * walks;
-            }
-            before += akv::wave_read(upto, 63);
-        }
-        return true;
-    }
-};
 
 // A block of K or V as the matrix instructions take it: lane (token t % 16 or channel % 16, quarter): 16 codes
 template <int D> struct KCodes {
@@ -195,15 +114,15 @@ template <class T, int D> struct RowState {
                 mx = fmaxf(mx, s[t][r]);
             }
         mx = max_lane32(max_lane16(mx));
-        const float m_new = fmaxf(m, fmaf(mx, c2, -kWeightBits));
-        const float base = m_new == -__builtin_inff() ? 0.f : m_new;   // nothing seen yet: all weights are 2^-inf
-        if (__any(m_new != m)) {
-            const float a = __builtin_amdgcn_exp2f(m - base);
+        const float now = fmaf(mx, c2, -kWeightBits);
+        if (__any(now > m + kSlackBits)) {
+            const float up = fmaxf(m, now), a = __builtin_amdgcn_exp2f(m - (up == -__builtin_inff() ? 0.f : up));
             z *= a;
 #pragma unroll
             for (int i = 0; i < D / 16; ++i) o[i] *= a;
-            m = m_new;
+            m = up;
         }
+        const float base = m == -__builtin_inff() ? 0.f : m;   // nothing seen yet: all weights are 2^-inf
         float sum = 0.f;
 #pragma unroll
         for (int t = 0; t < 4; ++t)
@@ -231,45 +150,6 @@ __device__ __forceinline__ void store_logits(float* block, const f32x4_t (&s)[4]
 #pragma unroll
     for (int t = 0; t < 4; ++t) __builtin_nontemporal_store(s[t], reinterpret_cast<f32x4_t*>(block + (t * rows + row) * 16 + 4 * (lane >> 4)));
 }
-
-template <class T> __device__ __forceinline__ void store_row(void* out, int out_dtype, size_t at, f32x4_t o)
-{
-    if (out_dtype == 0) *reinterpret_cast<f32x4_t*>(static_cast<float*>(out) + at) = o;
-    else *reinterpret_cast<u32x2_t*>(static_cast<uint16_t*>(out) + at) = u32x2_t{T::pack(o[0], o[1]), T::pack(o[2], o[3])};
-}
-
-// Four channels of a row, put together from parts
-struct Joined {
-    float top = -__builtin_inff(), z = 0.f;
-    f32x4_t o = {0, 0, 0, 0};
-    __device__ __forceinline__ void add(float m1, float z1, f32x4_t o1)
-    {
-        const float up = fmaxf(top, m1), base = up == -__builtin_inff() ? 0.f : up;
-        const float f = __builtin_amdgcn_exp2f(top - base), g = __builtin_amdgcn_exp2f(m1 - base);
-        z = fmaf(z, f, z1 * g);
-        o = o * f + o1 * g;
-        top = up;
-    }
-    __device__ __forceinline__ void put(float (&p)[6]) const
-    {
-        p[0] = top;
-        p[1] = z;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) p[2 + i] = o[i];
-    }
-    __device__ __forceinline__ void add(const float (&p)[6]) { add(p[0], p[1], f32x4_t{p[2], p[3], p[4], p[5]}); }
-    // the row's channels d .. d + 3 at `at` of out, and its statistics
-    template <class T> __device__ __forceinline__ void finish(const RowArgs& a, size_t first_row, int row, size_t at, int d) const
-    {
-        const float inv = z == 0.f ? 0.f : 1.f / z;   // zero: the row sees nothing
-        store_row<T>(a.out, a.out_dtype, at + d, o * inv);
-        if (a.stats && d == 0) {
-            float* p = a.stats + (first_row + row) * 2;
-            p[0] = top == -__builtin_inff() ? 0.f : top;
-            p[1] = inv;
-        }
-    }
-};
 
 // One workgroup of four waves per (row group of RT row tiles, split): wave w takes every fourth block of the split, and the four states are put together
 // through LDS.  Where a row group has several splits, the last of its workgroups to arrive joins them (the parts go through memory with device scope, as
@@ -462,39 +342,6 @@ __global__ __launch_bounds__(64 * kWaves, 2) void rows_kernel(RowArgs a)
     }
 }
 
-// The parts joined by a launch of their own: one workgroup of 256 threads per row, a thread with four channels of every eighth (D = 128; sixteenth) split.
-template <class T, int D>
-__global__ __launch_bounds__(256) void join_kernel(RowArgs a, int group_rows)
-{
-    constexpr int kSlices = 256 / (D / 4);
-    __shared__ float x_s[256][6];
-    const akb_cache& c = a.c;
-    const int G = c.shape.Hq / c.shape.Hkv, n = a.n;
-    const unsigned pair = blockIdx.y;
-    const int b = pair / c.shape.Hkv, row = blockIdx.x;
-    const int m = a.n_q ? min(max(a.n_q[b], 0), n) : n;
-    if (row >= m * G) return;
-    Cut cut;
-    cut.find<true>(a, b);
-    const int splits = cut.splits;
-    if (splits == 1) return;   // its rows are there already
-    const int group = row / group_rows, r = row % group_rows, rows = min(group_rows, m * G - group * group_rows), part = part_floats(rows, D);
-    const unsigned walk = (pair % c.shape.Hkv) * a.groups + a.groups - 1 - group;   // as the rows kernel counts them
-    const float* parts = a.parts + (size_t(cut.first) + size_t(walk) * splits) * part_floats(min(n * G, group_rows), D);
-    const int d = threadIdx.x % (D / 4) * 4, slice = threadIdx.x / (D / 4);
-    Joined j;
-#pragma unroll 8
-    for (int s = slice; s < splits; s += kSlices) {
-        const float* p = parts + size_t(s) * part;
-        j.add(p[2 * r], p[2 * r + 1], *reinterpret_cast<const f32x4_t*>(p + part_head(rows) + r * D + d));
-    }
-    j.put(x_s[threadIdx.x]);
-    __syncthreads();
-    if (slice) return;
-    for (int s = 1; s < kSlices; ++s) j.add(x_s[threadIdx.x + s * (D / 4)]);
-    j.template finish<T>(a, size_t(pair) * n * G, row, ((size_t(pair) * G + row % G) * n + row / G) * D, d);
-}
-
 // score[t] += sum over the rows of exp2(x - maximum) / sum, from the x that the rows kernel has left: calls of one row group, whose x are fewer bytes than
 // K's codes or not many more.  A thread has four tokens.
 __global__ __launch_bounds__(256) void score_logits_kernel(RowArgs a)
@@ -521,72 +368,140 @@ __global__ __launch_bounds__(256) void score_logits_kernel(RowArgs a)
     }
 }
 
+// The parts joined by a launch of their own: a thread has four channels of a row in every `SLICES`-th split, a workgroup of 256 threads as many rows as that
+// leaves (many parts: one row at D = 128, two at 64; few: eight or sixteen).
+template <class T, int D, int SLICES>
+__global__ __launch_bounds__(256) void join_kernel(RowArgs a, int group_rows)
+{
+    constexpr int kRun = D / 4, kRows = 256 / (kRun * SLICES);
+    __shared__ float x_s[256][6];
+    const akb_cache& c = a.c;
+    const int G = c.shape.Hq / c.shape.Hkv, n = a.n, tid = threadIdx.x;
+    const unsigned pair = blockIdx.y;
+    const int b = pair / c.shape.Hkv;
+    const int m = a.n_q ? min(max(a.n_q[b], 0), n) : n;
+    if (int(blockIdx.x) * kRows >= m * G) return;
+    Cut cut;
+    cut.find<true>(a, b);
+    const int splits = cut.splits;
+    if (splits == 1) return;   // its rows are there already
+    const int row = blockIdx.x * kRows + tid / (kRun * SLICES), slice = tid / kRun % SLICES, d = tid % kRun * 4;
+    const int group = row / group_rows, r = row % group_rows, rows = min(group_rows, m * G - group * group_rows), part = part_floats(rows, D);
+    Joined j;
+    if (row < m * G) {
+        const unsigned walk = (pair % c.shape.Hkv) * a.groups + a.groups - 1 - group;   // as the kernels of the parts count them
+        const float* parts = a.parts + (size_t(cut.first) + size_t(walk) * splits) * part_floats(min(n * G, group_rows), D);
+#pragma unroll 8
+        for (int s = slice; s < splits; s += SLICES) {
+            const float* p = parts + size_t(s) * part;
+            j.add(p[2 * r], p[2 * r + 1], *reinterpret_cast<const f32x4_t*>(p + part_head(rows) + r * D + d));
+        }
+    }
+    if (SLICES > 1) {
+        j.put(x_s[tid]);
+        __syncthreads();
+        if (slice) return;
+        for (int s = 1; s < SLICES; ++s) j.add(x_s[tid + s * kRun]);
+    }
+    if (row < m * G) j.template finish<T>(a, size_t(pair) * n * G, row, ((size_t(pair) * G + row % G) * n + row / G) * D, d);
+}
+
 // score[t] += sum over the rows of exp2(x - maximum) / sum: the scores of a block of K once more, for all rows (the weights of a row are known
-// only when its last token has been seen).  One workgroup per (block, KV head, sequence), wave w takes every fourth row tile.
+// only when its last token has been seen).  One workgroup per block; the block's 16-bit numbers stay in the registers of every wave as the operand of 32 x 32 x 16
+// matrix instructions, wave w takes every fourth tile of 32 query rows, asked for a tile ahead.  Bound by the matrix instructions (16 of 32 cycles per tile)
+// and the 32 weights per lane.  The sum over a lane's rows stays in its registers; lanes and waves meet once, at the end.
 template <class T, int D>
-__global__ __launch_bounds__(64 * kWaves) void score_kernel(RowArgs a)
+__global__ __launch_bounds__(64 * kWaves, 2) void score_kernel(RowArgs a)
 {
     __shared__ float sum_s[kWaves][kTB];
     const akb_cache& c = a.c;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, low = lane & 31, half = lane >> 5;
     const int h = blockIdx.y, b = blockIdx.z, G = c.shape.Hq / c.shape.Hkv, n = a.n;
     const int len = seq_len(c, b), m = a.n_q ? min(max(a.n_q[b], 0), n) : n;
     if (m == 0) return;
     const size_t bh = size_t(b) * c.shape.Hkv + h;
     for (int blk = blockIdx.x; blk * kTB < len; blk += gridDim.x) {
-        u32x4_t k[4][D / 32];
+        // step 2 i + e of 16 channels, half of the lanes: channels 16 (2 i + half) + 8 e .. + 7
+        u32x4_t k[2][D / 16];
         if (blk < len / kTB) {
-            KCodes<D> code;
-            code.load(c, bh * (c.shape.Ncap / kTB) + blk, lane);
-    #pragma unroll
-            for (int t = 0; t < 4; ++t)
-    #pragma unroll
-                for (int i = 0; i < D / 64; ++i) {
-                    k[t][2 * i] = cvt8<T>(code.w[t][i][0], code.w[t][i][1], code.s);
-                    k[t][2 * i + 1] = cvt8<T>(code.w[t][i][2], code.w[t][i][3], code.s);
+            const size_t block = bh * (c.shape.Ncap / kTB) + blk;
+            const float s = pow2(c.exps[block * 2]);
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int i = 0; i < D / 32; ++i) {
+                    const u32x4_t w = *reinterpret_cast<const u32x4_t*>(c.k8 + block * (kTB * D) + k_place<D>(32 * t + low, 16 * (2 * i + half)));
+                    k[t][2 * i] = cvt8<T>(w[0], w[1], s);
+                    k[t][2 * i + 1] = cvt8<T>(w[2], w[3], s);
                 }
         } else {
             const uint16_t* kt = c.k_tail + bh * kTB * D;
-    #pragma unroll
-            for (int t = 0; t < 4; ++t)
-    #pragma unroll
-                for (int i = 0; i < D / 32; ++i) k[t][i] = *reinterpret_cast<const u32x4_t*>(kt + (16 * t + (lane & 15)) * D + 64 * (i >> 1) + 16 * g + 8 * (i & 1));
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int i = 0; i < D / 16; ++i) k[t][i] = *reinterpret_cast<const u32x4_t*>(kt + (32 * t + low) * D + 16 * (2 * (i >> 1) + half) + 8 * (i & 1));
         }
-        f32x4_t acc[4] = {};
-        const int tiles = (m * G + 15) / 16;
-        for (int tile = wave; tile < tiles; tile += kWaves) {
-            const int row = tile * 16 + (lane & 15);
-            const int limit = min(row_limit(row, G, m, len), len);
-            if (row_limit(min(tile * 16 + 15, m * G - 1), G, m, len) <= blk * kTB) continue;   // no row of the tile sees the block
-            u32x4_t q[D / 32];
-            load_query<D>(q, row < m * G ? a.q + ((bh * G + row % G) * n + row / G) * D : nullptr, lane);
-            const float* p = a.stats + (bh * n * G + row) * 2;
-            const float base = row < m * G ? p[0] : 0.f, inv = row < m * G ? p[1] : 0.f;
-    #pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                f32x4_t s = {0, 0, 0, 0};
-    #pragma unroll
-                for (int i = 0; i < D / 32; ++i) s = T::mfma16(k[t][i], q[i], s);
-    #pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    if (blk * kTB + 16 * t + 4 * g + r < limit) acc[t][r] = fmaf(__builtin_amdgcn_exp2f(s[r] * a.c2 - base), inv, acc[t][r]);
+        f32x16_t acc[2];
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[t][r] = 0.f;
+        const int tiles = (m * G + 31) / 32;
+        u32x4_t q[D / 16];
+        float base, inv;
+        auto fetch = [&](int tile) {
+            const int row = min(tile * 32 + low, m * G - 1);   // (a row behind the last weighs nothing: inv)
+            const uint16_t* p = a.q + ((bh * G + row % G) * n + row / G) * D;
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i) q[i] = *reinterpret_cast<const u32x4_t*>(p + 16 * (2 * (i >> 1) + half) + 8 * (i & 1));
+            const float* st = a.stats + (bh * n * G + row) * 2;
+            base = st[0];
+            inv = tile * 32 + low < m * G ? st[1] : 0.f;
+        };
+        int tile = max(0, (blk * kTB - (len - m)) * G) / 32 + wave;   // from the first with a row that sees the block
+        if (tile < tiles) fetch(tile);
+        for (; tile < tiles; tile += kWaves) {
+            f32x16_t s[2];
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[t][r] = 0.f;
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+                for (int t = 0; t < 2; ++t) s[t] = T::mfma32(k[t][i], q[i], s[t]);
+            const float bs = base, iv = inv;
+            if (tile + kWaves < tiles) fetch(tile + kWaves);
+            if ((blk + 1) * kTB > row_limit(tile * 32, G, m, len)) {
+                const int limit = min(row_limit(tile * 32 + low, G, m, len), len);
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        if (blk * kTB + 32 * t + 8 * (r >> 2) + 4 * half + (r & 3) >= limit) s[t][r] = -__builtin_inff();
             }
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) acc[t][r] = fmaf(__builtin_amdgcn_exp2f(fmaf(s[t][r], a.c2, -bs)), iv, acc[t][r]);
         }
-    #pragma unroll
-        for (int t = 0; t < 4; ++t)
-    #pragma unroll
-            for (int r = 0; r < 4; ++r) {
+        // over the 32 rows of a half of the lanes
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
                 float v = acc[t][r];
                 v = akv::add_dpp<0xB1>(v);
                 v = akv::add_dpp<0x4E>(v);
                 v = akv::add_dpp<0x124>(v);
                 v = akv::add_dpp<0x128>(v);
-                if ((lane & 15) == 0) sum_s[wave][16 * t + 4 * g + r] = v;
+                v = akv::add_lane16(v);
+                if (low == r) sum_s[wave][32 * t + 8 * (r >> 2) + 4 * half + (r & 3)] = v;
             }
         __syncthreads();
         if (threadIdx.x < kTB && blk * kTB + int(threadIdx.x) < len) {
             float v = 0.f;
-    #pragma unroll
+#pragma unroll
             for (int w = 0; w < kWaves; ++w) v += sum_s[w][threadIdx.x];
             c.score[bh * c.shape.Ncap + blk * kTB + threadIdx.x] += v;
         }
@@ -599,12 +514,16 @@ template <class T, int D> static hipError_t launch(const RowArgs& r, const Atten
     const akb_shape& s = r.c.shape;
     const int tiles = p.tiles, grid = p.grid;
     auto rows = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(akv::xcd_grid(grid)), dim3(64 * kWaves), 0, st, r); };
-    if (r.out_dtype == 0) tiles == 1 ? rows(rows_kernel<T, D, true, 1>) : rows(rows_kernel<T, D, true, 2>);
+    if (tiles > 2) {
+        if (hipError_t e = launch_prompt(r, grid, st)) return e;
+    } else if (r.out_dtype == 0) tiles == 1 ? rows(rows_kernel<T, D, true, 1>) : rows(rows_kernel<T, D, true, 2>);
     else tiles == 1 ? rows(rows_kernel<T, D, false, 1>) : rows(rows_kernel<T, D, false, 2>);
     if (hipError_t e = hipGetLastError()) return e;
     if (r.splits != 1 && !r.tickets) {
         const int rows_all = r.n * (s.Hq / s.Hkv);
-        hipLaunchKernelGGL((join_kernel<T, D>), dim3(rows_all, s.B * s.Hkv), dim3(256), 0, st, r, 16 * tiles);
+        auto join = [&](auto kernel, int rows) { hipLaunchKernelGGL(kernel, dim3((rows_all + rows - 1) / rows, s.B * s.Hkv), dim3(256), 0, st, r, 16 * tiles); };
+        if (r.splits && r.splits <= 4) join(join_kernel<T, D, 1>, 1024 / D);
+        else join(join_kernel<T, D, 8>, 128 / D);
         if (hipError_t e = hipGetLastError()) return e;
     }
     const int blocks = (max_len + kTB - 1) / kTB;

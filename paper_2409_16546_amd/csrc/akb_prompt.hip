@@ -1,0 +1,210 @@
+// Attention of many query rows over the block-scaled 8-bit cache (rules and layout: include/akb.h; rows and parts: akb_rows.h).
+//
+// With many rows the products are what takes time, and turning codes into 16-bit numbers the next: a wave that does it for its own rows alone (the rows kernel)
+// spends more on that than on its softmax.  Here the four waves of a workgroup have 32 rows each and share every block: it is turned once, into LDS, in the order
+// in which 32 x 32 x 16 matrix instructions take their operands (1 KB per operand, lane after lane), while the block before is multiplied.
+// Per block and wave: 32 matrix instructions of 32 cycles for K and V together (48 with 32-bit results), 32 reads of 1 KB from LDS, and the softmax of 64 x 32 scores,
+// 32 per lane.  Two workgroups of 64 KB share a compute unit, so that one's products run beside the other's softmax.
+#include "akb_rows.h"
+
+namespace akb {
+
+constexpr int kWaveRows = kPromptRows / kWaves;
+
+// lane l has row l % 32; of a tile of 32 tokens (channels) it has 8 i + 4 (l / 32) .. + 3, i = 0 .. 3, in order
+template <int D> struct BlockLds {
+    u32x4_t k[2][D / 16][64];   // [32 tokens][16 channels]: lane (token % 32, half): channels 8 half .. + 7
+    u32x4_t v[D / 32][4][64];   // [32 channels][16 tokens]: lane (channel % 32, half): tokens 4 half .. + 3, 8 + 4 half .. + 3
+};
+
+// A block on its way from memory to LDS: wave w has pieces of 16 codes w, w + 4, .. of K's [tile][64 channels] and V's [16 channels]
+template <class T, int D> struct Stage {
+    static constexpr int kPieces = D / 64;   // per wave, of K and of V
+    u32x4_t k[kPieces], v[kPieces];
+    float ks, vs;
+    __device__ __forceinline__ void load(const akb_cache& c, size_t block, int wave, int lane)
+    {
+        const size_t at = block * (kTB * D) + (lane & 15) * 64 + (lane >> 4) * 16;
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+            k[i] = *reinterpret_cast<const u32x4_t*>(c.k8 + at + (wave + kWaves * i) * 1024);
+            v[i] = *reinterpret_cast<const u32x4_t*>(c.v8 + at + (wave + kWaves * i) * 1024);
+        }
+        ks = pow2(c.exps[block * 2]);
+        vs = pow2(c.exps[block * 2 + 1]);
+    }
+    __device__ __forceinline__ void store(BlockLds<D>& lds, int wave, int lane) const
+    {
+        const int low = lane & 15, g = lane >> 4;
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+            const int piece = wave + kWaves * i;
+            const int token = piece / (D / 64) * 16 + low, ch16 = piece % (D / 64) * 4 + g;   // K: 16 channels of a token
+            lds.k[token >> 5][ch16][token & 31] = cvt8<T>(k[i][0], k[i][1], ks);
+            lds.k[token >> 5][ch16][32 + (token & 31)] = cvt8<T>(k[i][2], k[i][3], ks);
+            const int ch = piece * 16 + low;                                                   // V: tokens 16 t + 4 g .. + 3 of a channel, t = 0 .. 3
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+                reinterpret_cast<u32x2_t*>(&lds.v[ch >> 5][t][(ch & 31) + 32 * (g & 1)])[g >> 1] = u32x2_t{T::template cvt2<false>(v[i][t], vs), T::template cvt2<true>(v[i][t], vs)};
+        }
+    }
+    // the incomplete block of `left` tokens, in 16 bits; what lies behind is zero
+    __device__ __forceinline__ static void store_tail(const akb_cache& c, size_t bh, int left, BlockLds<D>& lds, int tid)
+    {
+        const uint16_t *kt = c.k_tail + bh * kTB * D, *vt = c.v_tail + bh * kTB * D;
+        for (int e = tid; e < kTB * (D / 8); e += 64 * kWaves) {   // 8 channels of a token
+            const int token = e % kTB, oct = e / kTB;
+            lds.k[token >> 5][oct >> 1][(token & 31) + 32 * (oct & 1)] = token < left ? *reinterpret_cast<const u32x4_t*>(kt + token * D + oct * 8) : u32x4_t{0, 0, 0, 0};
+        }
+        for (int e = tid; e < D * 16; e += 64 * kWaves) {          // tokens 16 t + 4 g .. + 3 of a channel
+            const int ch = e % D, t = (e / D) & 3, g = e / D / 4, token = 16 * t + 4 * g;
+            u32x2_t w = {0, 0};
+            if (token < left) {
+                w = *reinterpret_cast<const u32x2_t*>(vt + ch * kTB + 16 * g + 4 * t);
+#pragma unroll
+                for (int k = 0; k < 2; ++k) w[k] = token + 2 * k + 1 < left ? w[k] : (token + 2 * k < left ? w[k] & 0xFFFFu : 0u);
+            }
+            reinterpret_cast<u32x2_t*>(&lds.v[ch >> 5][t][(ch & 31) + 32 * (g & 1)])[g >> 1] = w;
+        }
+    }
+};
+
+template <class T, int D, bool EXACT>
+__global__ __launch_bounds__(64 * kWaves, 2) void prompt_kernel(RowArgs a)
+{
+    __shared__ BlockLds<D> lds[2];
+    const akb_cache& c = a.c;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
+    Cut cut;
+    if (!cut.find<false>(a, 0)) return;
+    const int splits = cut.splits, split = (cut.w - cut.first) % splits, walk = (cut.w - cut.first) / splits;
+    const int group = a.groups - 1 - walk % a.groups;   // the rows that see most go first
+    const int b = cut.b, G = c.shape.Hq / c.shape.Hkv, n = a.n;
+    const size_t bh = size_t(b) * c.shape.Hkv + walk / a.groups;
+    const int len = seq_len(c, b), m = a.n_q ? min(max(a.n_q[b], 0), n) : n;
+    const int row0 = group * kPromptRows, rows = min(kPromptRows, m * G - row0);
+    if (rows <= 0) return;
+    const int nb = (max(row_limit(row0 + rows - 1, G, m, len), 0) + kTB - 1) / kTB;
+    const int lo = (int)(long(nb) * split / splits), hi = (int)(long(nb) * (split + 1) / splits);
+    const int first_row = row0 + wave * kWaveRows, row = first_row + (lane & 31);
+    const int wave_rows = min(kWaveRows, row0 + rows - first_row);   // may be below 1: the wave only helps to turn blocks
+    const int all_see = row_limit(first_row, G, m, len), most_see = wave_rows > 0 ? row_limit(first_row + wave_rows - 1, G, m, len) : 0;
+    const int limit = row_limit(row, G, m, len);
+    auto place = [&](int row) { return ((bh * G + row % G) * n + row / G) * D; };   // of a row in q and out
+    u32x4_t q[D / 16];
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) q[i] = row < m * G ? *reinterpret_cast<const u32x4_t*>(a.q + place(row) + 16 * i + 8 * half) : u32x4_t{0, 0, 0, 0};
+    f32x16_t o[D / 32];
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[i][r] = 0.f;
+    float top = -__builtin_inff(), z = 0.f;
+
+    const size_t block0 = bh * (c.shape.Ncap / kTB);
+    const int whole = len / kTB;   // blocks in 8 bits
+    Stage<T, D> stage;
+    auto fetch = [&](int blk) { if (blk < whole) stage.load(c, block0 + blk, wave, lane); };
+    auto put = [&](int blk, BlockLds<D>& to) {
+        if (blk < whole) stage.store(to, wave, lane);
+        else Stage<T, D>::store_tail(c, bh, len - blk * kTB, to, threadIdx.x);
+    };
+    if (lo < hi) {
+        fetch(lo);
+        put(lo, lds[0]);
+    }
+    auto step = [&](int blk, const BlockLds<D>& x, BlockLds<D>& next) {
+        lds_barrier();   // this block is there, and nobody reads the one before any more
+        if (blk + 1 < hi) fetch(blk + 1);
+        if (blk * kTB < most_see) {   // some row of the wave sees it
+            f32x16_t s[2];
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[t][r] = 0.f;
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+                for (int t = 0; t < 2; ++t) s[t] = T::mfma32(x.k[t][i][lane], q[i], s[t]);
+            if ((blk + 1) * kTB > all_see) {
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        if (blk * kTB + 32 * t + 8 * (r >> 2) + 4 * half + (r & 3) >= limit) s[t][r] = -__builtin_inff();
+            }
+            float mx = -__builtin_inff();
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[t][r]);
+            mx = max_lane32(mx);
+            const float now = fmaf(mx, a.c2, -kWeightBits);
+            if (__any(now > top + kSlackBits)) {
+                const float up = fmaxf(top, now), f = __builtin_amdgcn_exp2f(top - (up == -__builtin_inff() ? 0.f : up));
+                z *= f;
+#pragma unroll
+                for (int i = 0; i < D / 32; ++i) o[i] *= f;
+                top = up;
+            }
+            const float base = top == -__builtin_inff() ? 0.f : top;   // nothing seen yet: all weights are 2^-inf
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {   // 16 tokens
+                u32x4_t ph, pl;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int r = 8 * (t & 1) + 2 * k;
+                    const float p0 = __builtin_amdgcn_exp2f(fmaf(s[t >> 1][r], a.c2, -base)), p1 = __builtin_amdgcn_exp2f(fmaf(s[t >> 1][r + 1], a.c2, -base));
+                    z += p0 + p1;
+                    ph[k] = T::pack(p0, p1);
+                    if (EXACT) pl[k] = T::pack(p0 - T::lo(ph[k]), p1 - T::hi(ph[k]));
+                }
+#pragma unroll
+                for (int i = 0; i < D / 32; ++i) {
+                    const u32x4_t v = x.v[i][t][lane];
+                    o[i] = T::mfma32(v, ph, o[i]);
+                    if (EXACT) o[i] = T::mfma32(v, pl, o[i]);
+                }
+            }
+        }
+        if (blk + 1 < hi) put(blk + 1, next);
+    };
+    for (int blk = lo; blk < hi; blk += 2) {   // (in pairs: which half of LDS is which is known to the compiler)
+        step(blk, lds[0], lds[1]);
+        if (blk + 1 < hi) step(blk + 1, lds[1], lds[0]);
+    }
+    if (wave_rows <= 0 || (lane & 31) >= wave_rows) return;
+    z = akv::add_lane32(z);
+    const int r = row - row0;
+    Joined j;
+    j.top = top;
+    j.z = z;
+    float* part = a.parts + size_t(cut.w - split) * part_floats(min(n * G, kPromptRows), D) + size_t(split) * part_floats(rows, D);
+    if (splits > 1 && half == 0) {
+        part[2 * r] = top;
+        part[2 * r + 1] = z;
+    }
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int d = 32 * i + 8 * k + 4 * half;
+            j.o = f32x4_t{o[i][4 * k], o[i][4 * k + 1], o[i][4 * k + 2], o[i][4 * k + 3]};
+            if (splits == 1) j.template finish<T>(a, bh * n * G, row, place(row), d);
+            else *reinterpret_cast<f32x4_t*>(part + part_head(rows) + r * D + d) = j.o;
+        }
+}
+
+template <class T, int D> static void launch(const RowArgs& r, int grid, hipStream_t st)
+{
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(akv::xcd_grid(grid)), dim3(64 * kWaves), 0, st, r); };
+    r.out_dtype == 0 ? go(prompt_kernel<T, D, true>) : go(prompt_kernel<T, D, false>);
+}
+hipError_t launch_prompt(const RowArgs& r, int grid, hipStream_t st)
+{
+    if (r.c.shape.dtype == AKB_FP16) r.c.shape.D == 64 ? launch<Fp16, 64>(r, grid, st) : launch<Fp16, 128>(r, grid, st);
+    else r.c.shape.D == 64 ? launch<Bf16, 64>(r, grid, st) : launch<Bf16, 128>(r, grid, st);
+    return hipGetLastError();
+}
+
+}  // namespace akb
