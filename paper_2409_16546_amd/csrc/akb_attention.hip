@@ -18,6 +18,7 @@ struct AttentionPlan {
     int splits;     // parts of a walk, or 0: cut by the device
     int grid;       // workgroups at most
     bool ticketed;  // the last workgroup of a row group joins its parts; otherwise a launch does
+    int shares;     // parts the rows are cut into for the score
     size_t tickets, parts, logits, stats, total;   // offsets into the workspace
 };
 // Parts of each of `items` walks: none where they fill the slots; at most 2 slots parts in all, which is what the workspace has room for.
@@ -47,6 +48,9 @@ static AttentionPlan plan(const akb_shape& s, int n, int max_len, bool accumulat
     p.tickets = 0;
     p.parts = align256(size_t(2 * slots) * sizeof(int32_t));
     p.logits = p.parts + align256(size_t(2 * slots) * part_floats((int)std::min(rows, long(kPromptRows)), s.D) * sizeof(float));
+    // the score of many rows: two rounds of workgroups, at most eight shares of 256 rows or more
+    const long quads = pairs * ((blocks + kWaves - 1) / kWaves);
+    p.shares = (int)std::max(1L, std::min({(2 * slots + quads - 1) / quads, 8L, rows / 256}));
     p.stats = p.logits + (accumulate ? align256(size_t(pairs) * std::min(rows, 16L) * s.Ncap * sizeof(float)) : 0);
     p.total = p.stats + (accumulate ? align256(size_t(pairs) * rows * 2 * sizeof(float)) : 0);
     return p;
@@ -106,11 +110,12 @@ template <class T, int D> struct RowState {
     template <bool EXACT> __device__ __forceinline__ void weights(f32x4_t (&s)[4], int first, bool masked, float c2, int lane, u32x4_t (&ph)[2], u32x4_t (&pl)[2])
     {
         float mx = -__builtin_inff();
+        const int seen = limit - first - 4 * (lane >> 4);   // counted from the lane's first token
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                if (masked && first + 16 * t + 4 * (lane >> 4) + r >= limit) s[t][r] = -__builtin_inff();
+                if (masked && 16 * t + r >= seen) s[t][r] = -__builtin_inff();
                 mx = fmaxf(mx, s[t][r]);
             }
         mx = max_lane32(max_lane16(mx));
@@ -175,16 +180,16 @@ __global__ __launch_bounds__(64 * kWaves, 2) void rows_kernel(RowArgs a)
     const size_t bh = pair, item = bh * a.groups + group;
     const int row0 = group * kRows, rows = min(kRows, m * G - row0);
     if (rows <= 0) return;   // no row of the group is wanted (in any split)
-    const int keys = max(row_limit(row0 + rows - 1, G, m, len), 0), nb = (keys + kTB - 1) / kTB;
-    const int all_see = row_limit(row0, G, m, len);               // tokens that every row sees
+    const int keys = max(row_limit(a, row0 + rows - 1, G, m, len), 0), nb = (keys + kTB - 1) / kTB;
+    const int all_see = row_limit(a, row0, G, m, len);               // tokens that every row sees
     const int lo = (int)(long(nb) * split / splits), hi = (int)(long(nb) * (split + 1) / splits);
     const int whole = min(hi, len / kTB);                          // blocks in 8 bits
-    auto place = [&](int row) { return ((bh * G + row % G) * n + row / G) * D; };   // of a row in q and out
+    auto place = [&](int row) { return row_place(a, bh, G, row, D); };   // of a row in q and out
     RowState<T, D> st[RT];
 #pragma unroll
     for (int k = 0; k < RT; ++k) {
         const int row = row0 + 16 * k + (lane & 15);
-        st[k].init(row < m * G ? a.q + place(row) : nullptr, row_limit(row, G, m, len), lane);
+        st[k].init(row < m * G ? a.q + place(row) : nullptr, row_limit(a, row, G, m, len), lane);
     }
     float* logits = RT == 1 && a.logits ? a.logits + bh * min(a.n * G, 16) * c.shape.Ncap : nullptr;
     const size_t block0 = bh * (c.shape.Ncap / kTB);
@@ -359,7 +364,7 @@ __global__ __launch_bounds__(256) void score_logits_kernel(RowArgs a)
         for (int r = 0; r < rows; ++r) {
             const f32x4_t v = *reinterpret_cast<const f32x4_t*>(x + r * 16);
             const float base = stats[2 * r], inv = stats[2 * r + 1];
-            const int limit = row_limit(r, G, m, len);
+            const int limit = row_limit(a, r, G, m, len);
 #pragma unroll
             for (int i = 0; i < 4; ++i)
                 if (t + i < limit) acc[i] = fmaf(__builtin_amdgcn_exp2f(fmaf(v[i], a.c2, -base)), inv, acc[i]);
@@ -403,91 +408,125 @@ __global__ __launch_bounds__(256) void join_kernel(RowArgs a, int group_rows)
         if (slice) return;
         for (int s = 1; s < SLICES; ++s) j.add(x_s[tid + s * kRun]);
     }
-    if (row < m * G) j.template finish<T>(a, size_t(pair) * n * G, row, ((size_t(pair) * G + row % G) * n + row / G) * D, d);
+    if (row < m * G) j.template finish<T>(a, size_t(pair) * n * G, row, row_place(a, pair, G, row, D), d);
 }
 
 // score[t] += sum over the rows of exp2(x - maximum) / sum: the scores of a block of K once more, for all rows (the weights of a row are known
-// only when its last token has been seen).  One workgroup per block; the block's 16-bit numbers stay in the registers of every wave as the operand of 32 x 32 x 16
-// matrix instructions, wave w takes every fourth tile of 32 query rows, asked for a tile ahead.  Bound by the matrix instructions (16 of 32 cycles per tile)
-// and the 32 weights per lane.  The sum over a lane's rows stays in its registers; lanes and waves meet once, at the end.
+// only when its last token has been seen).  A wave keeps a block's 16-bit numbers in its registers as the operand of 32 x 32 x 16 matrix instructions; the
+// query rows come 64 at a time through LDS for the four waves (four blocks) of a workgroup, asked for a turn ahead (read by every wave for itself they cost
+// more than the products: 252 us of a chunk of 777 tokens onto 20000, 2 x 32 heads).  Bound by the matrix instructions (32 of 32 cycles per turn) and
+// the 64 weights per lane.  The sum over a lane's rows stays in its registers; lanes meet once, at the end.  Few blocks: the rows are cut into `shares`, whose sums
+// score_join_kernel adds up in their order.
+constexpr int kScoreRows = 64;
 template <class T, int D>
-__global__ __launch_bounds__(64 * kWaves, 2) void score_kernel(RowArgs a)
+__global__ __launch_bounds__(64 * kWaves, 2) void score_kernel(RowArgs a, int shares, float* __restrict__ sums)
 {
-    __shared__ float sum_s[kWaves][kTB];
+    constexpr int kSteps = D / 16, kOct = D / 8, kPieces = kScoreRows * kOct / (64 * kWaves);
+    // [32 rows][16 channels]: lane (row % 32, half): channels 8 half .. + 7.  The place of a lane's 16 bytes is turned by the channel octet, so that a row's
+    // octets, which neighbouring threads write, lie in different banks.
+    __shared__ u32x4_t q_s[2][2][kSteps][64];
+    __shared__ f32x2_t stats_s[2][kScoreRows];
     const akb_cache& c = a.c;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, low = lane & 31, half = lane >> 5;
-    const int h = blockIdx.y, b = blockIdx.z, G = c.shape.Hq / c.shape.Hkv, n = a.n;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), low = lane & 31, half = lane >> 5;
+    const int share = blockIdx.x % shares, h = blockIdx.y, b = blockIdx.z, G = c.shape.Hq / c.shape.Hkv, n = a.n;
     const int len = seq_len(c, b), m = a.n_q ? min(max(a.n_q[b], 0), n) : n;
-    if (m == 0) return;
     const size_t bh = size_t(b) * c.shape.Hkv + h;
-    for (int blk = blockIdx.x; blk * kTB < len; blk += gridDim.x) {
-        // step 2 i + e of 16 channels, half of the lanes: channels 16 (2 i + half) + 8 e .. + 7
-        u32x4_t k[2][D / 16];
-        if (blk < len / kTB) {
+    auto slot = [](int s, int oct) { return (s & 48) | ((s ^ oct) & 15); };
+    for (int blk0 = blockIdx.x / shares * kWaves; blk0 * kTB < len && m > 0; blk0 += gridDim.x / shares * kWaves) {
+        const int blk = blk0 + wave;
+        const bool mine = blk * kTB < len;
+        // K: lane (token % 32, half): channels 16 i + 8 half .. + 7
+        u32x4_t k[2][kSteps];
+        if (mine && blk < len / kTB) {
             const size_t block = bh * (c.shape.Ncap / kTB) + blk;
             const float s = pow2(c.exps[block * 2]);
 #pragma unroll
             for (int t = 0; t < 2; ++t)
 #pragma unroll
-                for (int i = 0; i < D / 32; ++i) {
-                    const u32x4_t w = *reinterpret_cast<const u32x4_t*>(c.k8 + block * (kTB * D) + k_place<D>(32 * t + low, 16 * (2 * i + half)));
-                    k[t][2 * i] = cvt8<T>(w[0], w[1], s);
-                    k[t][2 * i + 1] = cvt8<T>(w[2], w[3], s);
+                for (int i = 0; i < kSteps; ++i) {
+                    const u32x2_t w = *reinterpret_cast<const u32x2_t*>(c.k8 + block * (kTB * D) + k_place<D>(32 * t + low, 16 * i + 8 * half));
+                    k[t][i] = cvt8<T>(w[0], w[1], s);
                 }
-        } else {
+        } else if (mine) {
             const uint16_t* kt = c.k_tail + bh * kTB * D;
 #pragma unroll
             for (int t = 0; t < 2; ++t)
 #pragma unroll
-                for (int i = 0; i < D / 16; ++i) k[t][i] = *reinterpret_cast<const u32x4_t*>(kt + (32 * t + low) * D + 16 * (2 * (i >> 1) + half) + 8 * (i & 1));
+                for (int i = 0; i < kSteps; ++i) k[t][i] = *reinterpret_cast<const u32x4_t*>(kt + (32 * t + low) * D + 16 * i + 8 * half);
         }
         f32x16_t acc[2];
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
             for (int r = 0; r < 16; ++r) acc[t][r] = 0.f;
-        const int tiles = (m * G + 31) / 32;
-        u32x4_t q[D / 16];
-        float base, inv;
-        auto fetch = [&](int tile) {
-            const int row = min(tile * 32 + low, m * G - 1);   // (a row behind the last weighs nothing: inv)
-            const uint16_t* p = a.q + ((bh * G + row % G) * n + row / G) * D;
+        const int turns = (m * G + kScoreRows - 1) / kScoreRows, begin = max(0, (blk0 * kTB - (len - m)) * G) / kScoreRows;   // from the first row that sees the first block
+        const int lo = begin + int(long(turns - begin) * share / shares), hi = begin + int(long(turns - begin) * (share + 1) / shares);
+        u32x4_t piece[kPieces];
+        f32x2_t stat;
+        auto fetch = [&](int turn) {
 #pragma unroll
-            for (int i = 0; i < D / 16; ++i) q[i] = *reinterpret_cast<const u32x4_t*>(p + 16 * (2 * (i >> 1) + half) + 8 * (i & 1));
-            const float* st = a.stats + (bh * n * G + row) * 2;
-            base = st[0];
-            inv = tile * 32 + low < m * G ? st[1] : 0.f;
-        };
-        int tile = max(0, (blk * kTB - (len - m)) * G) / 32 + wave;   // from the first with a row that sees the block
-        if (tile < tiles) fetch(tile);
-        for (; tile < tiles; tile += kWaves) {
-            f32x16_t s[2];
-#pragma unroll
-            for (int t = 0; t < 2; ++t)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) s[t][r] = 0.f;
-#pragma unroll
-            for (int i = 0; i < D / 16; ++i)
-#pragma unroll
-                for (int t = 0; t < 2; ++t) s[t] = T::mfma32(k[t][i], q[i], s[t]);
-            const float bs = base, iv = inv;
-            if (tile + kWaves < tiles) fetch(tile + kWaves);
-            if ((blk + 1) * kTB > row_limit(tile * 32, G, m, len)) {
-                const int limit = min(row_limit(tile * 32 + low, G, m, len), len);
-#pragma unroll
-                for (int t = 0; t < 2; ++t)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r)
-                        if (blk * kTB + 32 * t + 8 * (r >> 2) + 4 * half + (r & 3) >= limit) s[t][r] = -__builtin_inff();
+            for (int i = 0; i < kPieces; ++i) {
+                const int e = tid + 64 * kWaves * i, row = min(turn * kScoreRows + e / kOct, m * G - 1);
+                piece[i] = *reinterpret_cast<const u32x4_t*>(a.q + row_place(a, bh, G, row, D) + e % kOct * 8);
             }
+            if (tid < kScoreRows) {
+                const int row = turn * kScoreRows + tid;
+                stat = row < m * G ? *reinterpret_cast<const f32x2_t*>(a.stats + (bh * n * G + row) * 2) : f32x2_t{0.f, 0.f};   // a row behind the last weighs nothing
+            }
+        };
+        auto put = [&](int to) {
 #pragma unroll
-            for (int t = 0; t < 2; ++t)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) acc[t][r] = fmaf(__builtin_amdgcn_exp2f(fmaf(s[t][r], a.c2, -bs)), iv, acc[t][r]);
+            for (int i = 0; i < kPieces; ++i) {
+                const int e = tid + 64 * kWaves * i, row = e / kOct, oct = e % kOct;
+                q_s[to][row >> 5][oct >> 1][slot((row & 31) + 32 * (oct & 1), oct)] = piece[i];
+            }
+            if (tid < kScoreRows) stats_s[to][tid] = stat;
+        };
+        if (lo < hi) {
+            fetch(lo);
+            put(0);
         }
-        // over the 32 rows of a half of the lanes
+        for (int turn = lo; turn < hi; ++turn) {
+            const int at = (turn - lo) & 1;
+            lds_barrier();
+            if (turn + 1 < hi) fetch(turn + 1);
+            if (mine) {
+#pragma unroll 1   // (both at a time do not fit the registers)
+                for (int j = 0; j < 2; ++j) {
+                    f32x16_t s[2];
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
+                    for (int t = 0; t < 2; ++t)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) s[t][r] = 0.f;
+#pragma unroll
+                    for (int i = 0; i < kSteps; ++i) {
+                        const u32x4_t q = q_s[at][j][i][slot(lane, 2 * i + half)];
+#pragma unroll
+                        for (int t = 0; t < 2; ++t) s[t] = T::mfma32(k[t][i], q, s[t]);
+                    }
+                    const f32x2_t stat = stats_s[at][32 * j + low];
+                    const int row0 = turn * kScoreRows + 32 * j;
+                    if ((blk + 1) * kTB > row_limit(a, row0, G, m, len)) {
+                        const int seen = min(row_limit(a, row0 + low, G, m, len), len) - blk * kTB - 4 * half;   // counted from the lane's first token
+#pragma unroll
+                        for (int t = 0; t < 2; ++t)
+#pragma unroll
+                            for (int r = 0; r < 16; ++r)
+                                if (32 * t + 8 * (r >> 2) + (r & 3) >= seen) s[t][r] = -__builtin_inff();
+                    }
+#pragma unroll
+                    for (int t = 0; t < 2; ++t)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) acc[t][r] = fmaf(__builtin_amdgcn_exp2f(fmaf(s[t][r], a.c2, -stat.x)), stat.y, acc[t][r]);
+                }
+            }
+            if (turn + 1 < hi) put(1 - at);
+        }
+        // over the 32 rows of a half of the lanes; lane `low` < 16 then stores the token of its number
+        float* out = sums ? sums + (size_t(share) * c.shape.B * c.shape.Hkv + bh) * c.shape.Ncap : c.score + bh * c.shape.Ncap;
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            float sum = 0.f;
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
                 float v = acc[t][r];
@@ -496,20 +535,29 @@ __global__ __launch_bounds__(64 * kWaves, 2) void score_kernel(RowArgs a)
                 v = akv::add_dpp<0x124>(v);
                 v = akv::add_dpp<0x128>(v);
                 v = akv::add_lane16(v);
-                if (low == r) sum_s[wave][32 * t + 8 * (r >> 2) + 4 * half + (r & 3)] = v;
+                sum = low == r ? v : sum;
             }
-        __syncthreads();
-        if (threadIdx.x < kTB && blk * kTB + int(threadIdx.x) < len) {
-            float v = 0.f;
-#pragma unroll
-            for (int w = 0; w < kWaves; ++w) v += sum_s[w][threadIdx.x];
-            c.score[bh * c.shape.Ncap + blk * kTB + threadIdx.x] += v;
+            const int token = blk * kTB + 32 * t + 8 * (low >> 2) + 4 * half + (low & 3);
+            if (low < 16 && token < len) out[token] = sums ? sum : out[token] + sum;
         }
-        __syncthreads();   // sum_s is written again
+        lds_barrier();   // the rows are written again
     }
 }
 
-template <class T, int D> static hipError_t launch(const RowArgs& r, const AttentionPlan& p, int max_len, hipStream_t st)
+__global__ __launch_bounds__(256) void score_join_kernel(RowArgs a, int shares, const float* __restrict__ sums)
+{
+    const akb_cache& c = a.c;
+    const int len = seq_len(c, blockIdx.z);
+    if (a.n_q && a.n_q[blockIdx.z] <= 0) return;
+    const size_t bh = size_t(blockIdx.z) * c.shape.Hkv + blockIdx.y, all = size_t(c.shape.B) * c.shape.Hkv;
+    for (int t = blockIdx.x * 256 + threadIdx.x; t < len; t += gridDim.x * 256) {
+        float v = c.score[bh * c.shape.Ncap + t];
+        for (int s = 0; s < shares; ++s) v += sums[(s * all + bh) * c.shape.Ncap + t];
+        c.score[bh * c.shape.Ncap + t] = v;
+    }
+}
+
+template <class T, int D> static hipError_t launch(const RowArgs& r, const AttentionPlan& p, float* sums, int max_len, hipStream_t st)
 {
     const akb_shape& s = r.c.shape;
     const int tiles = p.tiles, grid = p.grid;
@@ -528,18 +576,25 @@ template <class T, int D> static hipError_t launch(const RowArgs& r, const Atten
     }
     const int blocks = (max_len + kTB - 1) / kTB;
     if (r.logits) hipLaunchKernelGGL(score_logits_kernel, dim3((blocks + 15) / 16, s.Hkv, s.B), dim3(256), 0, st, r);
-    else if (r.stats) hipLaunchKernelGGL((score_kernel<T, D>), dim3(blocks, s.Hkv, s.B), dim3(64 * kWaves), 0, st, r);
+    else if (r.stats) {
+        const int quads = (blocks + kWaves - 1) / kWaves;
+        hipLaunchKernelGGL((score_kernel<T, D>), dim3(quads * p.shares, s.Hkv, s.B), dim3(64 * kWaves), 0, st, r, p.shares, p.shares > 1 ? sums : nullptr);
+        if (hipError_t e = hipGetLastError()) return e;
+        if (p.shares > 1) hipLaunchKernelGGL(score_join_kernel, dim3((blocks + 3) / 4, s.Hkv, s.B), dim3(256), 0, st, r, p.shares, sums);
+    }
     return hipGetLastError();
 }
 
 hipError_t launch_attention(const AttentionArgs& a, hipStream_t st)
 {
     const AttentionPlan p = plan(a.c.shape, a.n, a.max_len, a.accumulate);
-    RowArgs r{a.c, a.q, a.n_q, a.n, p.groups, p.splits, p.grid, a.out_dtype, a.out, a.c2, p.ticketed ? reinterpret_cast<int32_t*>(a.ws + p.tickets) : nullptr,
+    const int G = a.c.shape.Hq / a.c.shape.Hkv;
+    RowArgs r{a.c, a.q, a.n_q, a.n, p.groups, p.splits, p.grid, a.out_dtype, a.out, a.c2, uint32_t(G > 1 ? ((uint64_t(1) << 32) + G - 1) / G : 0), p.ticketed ? reinterpret_cast<int32_t*>(a.ws + p.tickets) : nullptr,
               reinterpret_cast<float*>(a.ws + p.parts), a.accumulate && p.tiles == 1 ? reinterpret_cast<float*>(a.ws + p.logits) : nullptr,
               a.accumulate ? reinterpret_cast<float*>(a.ws + p.stats) : nullptr};
-    if (a.c.shape.dtype == AKB_FP16) return a.c.shape.D == 64 ? launch<Fp16, 64>(r, p, a.max_len, st) : launch<Fp16, 128>(r, p, a.max_len, st);
-    return a.c.shape.D == 64 ? launch<Bf16, 64>(r, p, a.max_len, st) : launch<Bf16, 128>(r, p, a.max_len, st);
+    float* sums = reinterpret_cast<float*>(a.ws + p.logits);   // (a call has logits or sums)
+    if (a.c.shape.dtype == AKB_FP16) return a.c.shape.D == 64 ? launch<Fp16, 64>(r, p, sums, a.max_len, st) : launch<Fp16, 128>(r, p, sums, a.max_len, st);
+    return a.c.shape.D == 64 ? launch<Bf16, 64>(r, p, sums, a.max_len, st) : launch<Bf16, 128>(r, p, sums, a.max_len, st);
 }
 
 }  // namespace akb

@@ -84,13 +84,13 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prompt_kernel(RowArgs a)
     const int len = seq_len(c, b), m = a.n_q ? min(max(a.n_q[b], 0), n) : n;
     const int row0 = group * kPromptRows, rows = min(kPromptRows, m * G - row0);
     if (rows <= 0) return;
-    const int nb = (max(row_limit(row0 + rows - 1, G, m, len), 0) + kTB - 1) / kTB;
+    const int nb = (max(row_limit(a, row0 + rows - 1, G, m, len), 0) + kTB - 1) / kTB;
     const int lo = (int)(long(nb) * split / splits), hi = (int)(long(nb) * (split + 1) / splits);
     const int first_row = row0 + wave * kWaveRows, row = first_row + (lane & 31);
     const int wave_rows = min(kWaveRows, row0 + rows - first_row);   // may be below 1: the wave only helps to turn blocks
-    const int all_see = row_limit(first_row, G, m, len), most_see = wave_rows > 0 ? row_limit(first_row + wave_rows - 1, G, m, len) : 0;
-    const int limit = row_limit(row, G, m, len);
-    auto place = [&](int row) { return ((bh * G + row % G) * n + row / G) * D; };   // of a row in q and out
+    const int all_see = row_limit(a, first_row, G, m, len), most_see = wave_rows > 0 ? row_limit(a, first_row + wave_rows - 1, G, m, len) : 0;
+    const int limit = row_limit(a, row, G, m, len);
+    auto place = [&](int row) { return row_place(a, bh, G, row, D); };   // of a row in q and out
     u32x4_t q[D / 16];
 #pragma unroll
     for (int i = 0; i < D / 16; ++i) q[i] = row < m * G ? *reinterpret_cast<const u32x4_t*>(a.q + place(row) + 16 * i + 8 * half) : u32x4_t{0, 0, 0, 0};
@@ -127,11 +127,12 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prompt_kernel(RowArgs a)
 #pragma unroll
                 for (int t = 0; t < 2; ++t) s[t] = T::mfma32(x.k[t][i][lane], q[i], s[t]);
             if ((blk + 1) * kTB > all_see) {
+                const int seen = limit - blk * kTB - 4 * half;   // counted from the lane's first token
 #pragma unroll
                 for (int t = 0; t < 2; ++t)
 #pragma unroll
                     for (int r = 0; r < 16; ++r)
-                        if (blk * kTB + 32 * t + 8 * (r >> 2) + 4 * half + (r & 3) >= limit) s[t][r] = -__builtin_inff();
+                        if (32 * t + 8 * (r >> 2) + (r & 3) >= seen) s[t][r] = -__builtin_inff();
             }
             float mx = -__builtin_inff();
 #pragma unroll

@@ -29,13 +29,22 @@ struct RowArgs {
     int n, groups, splits, slots, out_dtype;
     void* out;
     float c2;
+    uint32_t inv_g;     // ceil(2^32 / G), or 0 where G is 1 (row_token)
     int32_t* tickets;   // [sequence, KV head, row group]: splits that have arrived, zero between calls; NULL: join_kernel follows
     float *parts, *logits, *stats;   // logits: q . k of the one row group, [sequence, KV head][block][tile][row][16]; stats: (maximum, 1 / sum) per row; or NULL
 };
 
 #if defined(__HIPCC__)
-// The tokens that rows see: row r (its query token r / G of m) the first `limit`
-__device__ __forceinline__ int row_limit(int row, int G, int m, int len) { return row < m * G ? len - m + row / G + 1 : 0; }
+// the query token of a row, row / G: exact below 2^28 rows (there are at most 2^22 tokens of 16 rows)
+__device__ __forceinline__ int row_token(const RowArgs& a, int row) { return a.inv_g ? int(__umulhi(uint32_t(row), a.inv_g)) : row; }
+// the place of a row in q and out, [sequence][query head][n][D]; first: the pair's, of which G n rows follow
+__device__ __forceinline__ size_t row_place(const RowArgs& a, size_t pair, int G, int row, int D)
+{
+    const int token = row_token(a, row);
+    return ((pair * G + (row - token * G)) * a.n + token) * D;
+}
+// The tokens that rows see: row r (its query token of m) the first `limit`
+__device__ __forceinline__ int row_limit(const RowArgs& a, int row, int G, int m, int len) { return row < m * G ? len - m + row_token(a, row) + 1 : 0; }
 
 // How the walks of a call are cut: the same in every wave that asks.  Lane l has sequences l, l + 64, ..
 struct Cut {
