@@ -114,12 +114,17 @@ akv_status akb_workspace_init(void *workspace, size_t workspace_bytes, void *str
 /*
  * Attention of n query tokens per sequence.  q: device [B][Hq][n][D] of the shape's type.  n_q: device int32 [B] with the
  * number of leading query tokens (0..n) of each sequence, or NULL for n.  out: device [B][Hq][n][D] of params->out_dtype;
- * rows i >= n_q[b] are left as they were; a query token that sees nothing yields zeros.  workspace: device scratch, 256-B
+ * B * Hq * n < 2^29.  Rows i >= n_q[b] are left as they were; a query token that sees nothing yields zeros.  workspace: device scratch, 256-B
  * aligned, prepared by akb_workspace_init; calls that overlap need distinct ones, and it holds nothing between calls.  params may be
  * NULL (float32 out, no accumulation).  The same call gives the same bits.
  */
 akv_status akb_attention(const akb_cache *cache, const uint16_t *q, const int32_t *n_q, int32_t n, void *out, const akb_params *params,
                          void *workspace, size_t workspace_bytes, void *stream);
+
+/* Which kernels akb_attention takes for n query tokens: 1 = row groups of 16 rows, 2 = of 32, 3 = of 128 (many rows); max_len as in akb_params.  parts: NULL, or
+ * a host pointer that receives the parts each walk over the blocks is cut into (0: the device cuts by the lengths).  Host computation; 0 on a bad shape.  For
+ * callers that attribute time to kernels. */
+int32_t akb_attention_path(const akb_shape *shape, int32_t n, int32_t max_len, int32_t *parts);
 
 /*
  * Evict: src's tokens (their values as they are read, their scores) go to dst, at most `keep` of each (sequence, KV head):

@@ -110,6 +110,7 @@ akv_status akb_attention(const akb_cache* cache, const uint16_t* q, const int32_
     akb_params p = {};
     if (params) p = *params;
     if (n < 0 || n > s.Ncap) return fail(AKV_EINVAL, "n = %d out of range 0..Ncap", n);
+    if (size_t(s.B) * s.Hq * n >= (size_t(1) << 29)) return fail(AKV_EINVAL, "B * Hq * n = %zu query rows: 2^29 or more", size_t(s.B) * s.Hq * n);
     if (p.out_dtype != 0 && p.out_dtype != 1) return fail(AKV_EINVAL, "out_dtype = %d is neither 0 (f32) nor 1 (the cache's 16-bit type)", p.out_dtype);
     if (p.max_len < 0 || p.max_len > s.Ncap) return fail(AKV_EINVAL, "max_len = %d out of range 0..Ncap", p.max_len);
     if (!std::isfinite(p.scale)) return fail(AKV_EINVAL, "scale is not finite");
@@ -122,6 +123,12 @@ akv_status akb_attention(const akb_cache* cache, const uint16_t* q, const int32_
     const akb::AttentionArgs a{*cache, q, n_q, n, out, p.out_dtype, p.accumulate != 0, p.max_len > 0 ? p.max_len : s.Ncap,
                                (float)(scale * 1.4426950408889634), static_cast<char*>(workspace)};
     return hip_result(akb::launch_attention(a, static_cast<hipStream_t>(stream)), "attention launch");
+}
+
+int32_t akb_attention_path(const akb_shape* shape, int32_t n, int32_t max_len, int32_t* parts)
+{
+    if (!shape || !shape_ok(*shape) || n < 1 || n > shape->Ncap || max_len < 0 || max_len > shape->Ncap) return 0;
+    return akb::attention_path(*shape, n, max_len > 0 ? max_len : shape->Ncap, parts);
 }
 
 size_t akb_evict_workspace(const akb_shape* shape, int32_t keep)

@@ -56,6 +56,12 @@ static AttentionPlan plan(const akb_shape& s, int n, int max_len, bool accumulat
     return p;
 }
 size_t attention_workspace(const akb_shape& s, int n, bool accumulate) { return plan(s, std::max(n, 1), s.Ncap, accumulate).total; }
+int attention_path(const akb_shape& s, int n, int max_len, int32_t* parts)
+{
+    const AttentionPlan p = plan(s, n, max_len, false);
+    if (parts) *parts = p.splits;
+    return p.tiles <= 2 ? p.tiles : 3;
+}
 size_t attention_tickets() { return size_t(4) * akv::compute_units() * sizeof(int32_t); }
 
 // A block of K or V as the matrix instructions take it: lane (token t % 16 or channel % 16, quarter): 16 codes

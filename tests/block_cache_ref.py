@@ -83,21 +83,20 @@ class Ref:
                 K, V = self.tokens[b][h]
                 for g in range(G):
                     hq = h * G + g
-                    for i in range(m):
-                        t = max(0, L - m + i + 1)
-                        if t == 0:
-                            out[b, hq, i] = mag[b, hq, i] = eps[b, hq, i] = 0
-                            continue
-                        x = K[:t] @ q[b, hq, i] * scale
-                        p = np.exp(x - x.max())
-                        p /= p.sum()
-                        out[b, hq, i], mag[b, hq, i] = p @ V[:t], p @ np.abs(V[:t])
-                        # a score: D products summed in 32 bits (D 2^-24 of their magnitudes), scaled, the maximum subtracted (2^-23 each); the weight:
-                        # that, and its exponential (2^-22); twice (weight, sum), and the two sums of t addends, 16 per step
-                        ex = scale * self.D * 2.0 ** -24 * (np.abs(K[:t]) @ np.abs(q[b, hq, i])).max() + 2.0 ** -22 * np.abs(x).max() + 2.0 ** -22
-                        eps[b, hq, i] = 2 * ex + (t / 16 + 64) * 2.0 ** -23
-                        if accumulate:
-                            self.score[b][h][:t] += p
+                    seen = np.arange(L)[None, :] <= L - m + np.arange(m)[:, None]
+                    x = q[b, hq, :m] @ K.T * scale
+                    top = np.where(seen, x, -np.inf).max(axis=1, initial=-np.inf)
+                    top = np.where(np.isfinite(top), top, 0.0)
+                    p = np.where(seen, np.exp(np.where(seen, x - top[:, None], 0.0)), 0.0)
+                    p /= np.maximum(p.sum(axis=1, keepdims=True), 1e-300)
+                    out[b, hq, :m], mag[b, hq, :m] = p @ V, p @ np.abs(V)
+                    # a score: D products summed in 32 bits (D 2^-24 of their magnitudes), scaled, the maximum subtracted (2^-23 each); the weight:
+                    # that, and its exponential (2^-22); twice (weight, sum), and the two sums of t addends, 16 per step
+                    size = np.where(seen, np.abs(q[b, hq, :m]) @ np.abs(K).T, 0.0).max(axis=1, initial=0.0)
+                    ex = scale * self.D * 2.0 ** -24 * size + 2.0 ** -22 * np.where(seen, np.abs(x), 0.0).max(axis=1, initial=0.0) + 2.0 ** -22
+                    eps[b, hq, :m] = (2 * ex + (seen.sum(axis=1) / 16 + 64) * 2.0 ** -23)[:, None]
+                    if accumulate:
+                        self.score[b][h] += p.sum(axis=0)
         return out, eps, mag
 
     def evict(self, keep, recent):

@@ -107,6 +107,8 @@ def test_refusals_come_before_any_launch(A):
     refused(attention(ws=None), "needed", A.AKV_EWORKSPACE)
     refused(attention(size=64), "needed", A.AKV_EWORKSPACE)
     assert attention(n=0, q=None, out=None, ws=None) == A.AKV_OK
+    many = A.akb_cache(A.akb_shape(64, 64, 4, 64, 1 << 18, 0), **ADDR)
+    refused(attention(c=many, n=1 << 17, size=1 << 50), "2^29")
 
     to = {n: a + 0x100000000 for n, a in ADDR.items()}
 
@@ -126,6 +128,19 @@ def test_refusals_come_before_any_launch(A):
     refused(evict(dst=A.akb_cache(shape, **{**to, "v8": ADDR["score"]})), "share memory")
     refused(L.akb_unpack(r(good), Q + 4, None, None), "aligned")
     assert L.akb_unpack(r(good), None, None, None) == A.AKV_OK
+
+
+def test_attention_path_is_a_host_computation_and_the_gpu_cases_reach_what_they_name(A):
+    from test_gpu_block_cache import LARGE
+    for case in LARGE:   # 256 compute units are assumed where no device can be asked
+        path, _, _, D, B, Hq, Hkv, N, _, n, _ = case
+        assert A.akb_attention_path(B, Hq, Hkv, D, (N + 63) // 64 * 64, n) == path, case
+    assert {c[0][0] for c in LARGE} == {1, 2, 3}
+    assert A.akb_attention_path(1, 6, 4, 64, 64)[0] == 0 and A.akb_attention_path(1, 4, 4, 64, 64, 65)[0] == 0 and A.akb_attention_path(1, 4, 4, 64, 64, 1, 65)[0] == 0
+    assert A.akb_attention_path(1, 32, 32, 128, 1024, 1, 64) == (1, 1)          # a bound of the lengths: one part
+    # the lines: 16 rows, 64 rows, 12 blocks a part
+    assert [A.akb_attention_path(8, 32, 8, 128, 8192, n)[0] for n in (4, 5, 16, 17)] == [1, 2, 2, 3]
+    assert A.akb_attention_path(8, 32, 8, 128, 2048, 17)[0] == 2
 
 
 def test_binding_checks_types_and_shapes(A):

@@ -157,6 +157,72 @@ def test_attention(A, case, accumulate):
     R.assert_same_tokens(A, c, ref, "the cache is as it was")
 
 
+# kernel and parts, dtype, out, D, B, Hq, Hkv, tokens, ragged, n, ragged n: calls large enough for every way a call is cut, against 64 bits on the GPU
+LARGE = [
+    ((1, 4), F16, F32, 128, 1, 4, 4, 1000, False, 1, False),         # parts joined by the last workgroup
+    ((1, 64), B16, B16, 128, 1, 64, 8, 20000, False, 1, False),      # ... by a launch, many parts
+    ((1, 8), B16, F32, 64, 1, 32, 8, 2000, False, 2, False),
+    ((1, 1), F16, F16, 128, 16, 32, 32, 300, True, 1, False),        # whole walks
+    ((1, 0), F16, F32, 128, 4, 32, 32, 9000, True, 1, False),        # parts by the lengths
+    ((1, 0), B16, B16, 64, 3, 64, 4, 90000, True, 1, False),
+    ((2, 11), F16, F32, 128, 3, 64, 8, 5000, True, 5, True),         # two row groups
+    ((2, 0), B16, B16, 64, 5, 16, 8, 30000, True, 9, True),
+    ((2, 1), F16, F16, 128, 32, 16, 16, 200, True, 40, True),
+    ((3, 1), B16, B16, 128, 2, 32, 8, 1100, False, 1100, False),     # prompts over themselves
+    ((3, 1), F16, F32, 64, 8, 10, 2, 801, True, 800, True),          # groups of five: row groups that end inside a query token
+    ((3, 2), F16, F32, 128, 4, 8, 8, 4099, True, 1000, True),        # chunks in parts
+    ((3, 0), B16, F32, 128, 2, 16, 4, 66000, True, 64, False),
+    ((2, 4), F16, F16, 64, 1, 16, 2, 6000, False, 333, False),
+    ((3, 13), F16, F16, 64, 1, 16, 2, 12000, False, 333, False),
+]
+
+
+@pytest.mark.parametrize("case", LARGE, ids=lambda c: f"kernel{c[0][0]}-parts{c[0][1]}-D{c[3]}-B{c[4]}-H{c[5]}_{c[6]}-N{c[7]}-n{c[9]}")
+def test_large_calls(A, case):
+    path, dtype, out_dtype, D, B, Hq, Hkv, N, ragged, n, ragged_n = case
+    G, Ncap = Hq // Hkv, (N + 63) // 64 * 64
+    print(case, flush=True)
+    assert A.akb_attention_path(B, Hq, Hkv, D, Ncap, n) == path
+    g = torch.Generator(device=DEV).manual_seed(N + n)
+    c = A.BlockCache.allocate(B, Hq, Hkv, D, Ncap, dtype, score=True, n=n)
+    c.k_tail.fill_(float("nan"))
+    c.v_tail.fill_(float("nan"))
+    lens = [N if not ragged else max(1, N - b * (N // B) - 7 * b) for b in range(B)]
+    n_q = [n if not ragged_n else max(0, n - b * (n // B)) for b in range(B)]
+    scale = torch.pow(10.0, torch.rand(1, Hkv, 1, D, generator=g, device=DEV) - 0.5)
+    k, v = ((torch.randn(B, Hkv, N, D, generator=g, device=DEV) * scale).to(dtype) for _ in range(2))
+    A.akb_append(c, k, v, i32(lens))
+    q = torch.randn(B, Hq, n, D, generator=g, device=DEV).to(dtype)
+    start = torch.rand(c.score.shape, generator=g, device=DEV)
+    c.score.copy_(start)
+    out = torch.full(q.shape, 3.0, dtype=out_dtype, device=DEV)
+    A.akb_attention(c, q, out, n_q=i32(n_q) if ragged_n else None, accumulate=True)
+    K, V = A.akb_unpack(c)
+    half = float(torch.finfo(dtype).eps) / 2
+    for b in range(B):
+        L, m = lens[b], n_q[b]
+        assert (out[b, :, m:].float() == 3.0).all()
+        for h in range(Hkv):
+            Kd, Vd = K[b, h, :L].double(), V[b, h, :L].double()
+            qd = q[b, h * G:(h + 1) * G, :m].double().reshape(G * m, D)
+            past = torch.arange(L, device=DEV)[None] > (L - m + torch.arange(m, device=DEV)).repeat(G)[:, None]
+            x = (qd @ Kd.T / D ** 0.5).masked_fill_(past, -float("inf"))
+            size = (qd.abs() @ Kd.abs().T).masked_fill_(past, 0.0).amax(dim=1, keepdim=True) if m else x.new_zeros(0, 1)
+            p = torch.softmax(x, dim=1).nan_to_num_(0.0)
+            want, mag = p @ Vd, p @ Vd.abs()
+            # as in the reference: products in 32 bits, the scaling and the subtraction, exponentials, sums
+            top = x.masked_fill(past, 0.0).abs().amax(dim=1, keepdim=True) if m else size
+            eps = 2 * (D ** 0.5 * 2.0 ** -24 * size + 2.0 ** -22 * top + 2.0 ** -22) + (L / 16 + 64) * 2.0 ** -23
+            bound = eps * mag + (half ** 2 * mag if out_dtype == F32 else half * mag + half * want.abs()) + (2.0 ** -25 if out_dtype == F16 else 0.0) + 1e-30
+            got = out[b, h * G:(h + 1) * G, :m].double().reshape(G * m, D)
+            assert (((got - want).abs() <= bound).all()), (b, h, float(((got - want).abs() / bound).max()))
+            add = p.sum(dim=0)
+            rel = float(eps.max()) if m else 0.0
+            now, was = c.score.view(B, Hkv, -1)[b, h].double(), start.view(B, Hkv, -1)[b, h].double()
+            assert ((now[:L] - was[:L] - add).abs() <= rel * add + (G * m / 16 + 32) * 2.0 ** -23 * (1 + add)).all(), (b, h)
+            assert (now[L:] == was[L:]).all()
+
+
 def test_scale_and_length_bound(A):
     c, ref = pair(A, 2, 4, 2, 128, 1024, F16)
     put(A, c, ref, 900, 1, [900, 130])
