@@ -512,6 +512,8 @@ class BlockCache:
     score: torch.Tensor | None = field(repr=False, default=None)
     workspace: torch.Tensor = field(repr=False, default=None)
     _struct: akb_cache = field(repr=False, default=None)
+    _ref: object = field(repr=False, default=None)
+    _params: dict = field(repr=False, default_factory=dict)
 
     def __post_init__(self):
         sz = akb_layout_sizes(self.B, self.Hq, self.Hkv, self.D, self.Ncap, self.dtype)
@@ -540,6 +542,21 @@ class BlockCache:
                                      _ptr(self.exps), _ptr(self.k_tail), _ptr(self.v_tail), _ptr(self.score), _ptr(self.lens), _ptr(self.flags))
         return self._struct
 
+    def ref(self):
+        """The struct by reference, as the calls take it (made once)."""
+        if self._ref is None:
+            self._ref = C.byref(self.struct())
+        return self._ref
+
+    def params(self, *values):
+        """akb_params of these values by reference; a program's few are kept."""
+        p = self._params.get(values)
+        if p is None:
+            if len(self._params) >= 64:
+                self._params.clear()
+            p = self._params[values] = C.byref(akb_params(*values))
+        return p
+
     def reserve(self, n: int = 1, keep: int = 0) -> "BlockCache":
         """Make the workspace large enough for attention of up to n query tokens and, where keep > 0, for evictions down to `keep` tokens."""
         shp = self.struct().shape
@@ -557,7 +574,8 @@ class BlockCache:
 def _here(*tensors) -> None:
     """The calls go to the current stream of the current device: every tensor has to lie there."""
     dev = torch.cuda.current_device()
-    assert all(t is None or t.device.index == dev for t in tensors), f"tensors of the current device (cuda:{dev}) only"
+    for t in tensors:
+        assert t is None or t.get_device() == dev, f"tensors of the current device (cuda:{dev}) only"
 
 
 def akb_cache_reset(cache: BlockCache) -> None:
@@ -573,11 +591,12 @@ def akb_workspace_init(workspace: torch.Tensor) -> None:
 
 def akb_append(cache: BlockCache, k_new: torch.Tensor, v_new: torch.Tensor, n_new: torch.Tensor | None = None) -> None:
     """k_new, v_new: [B, Hkv, n, D] of the cache's type on the device; n_new: int32 [B] on the device or None."""
-    n = k_new.shape[2]
-    assert k_new.dtype == v_new.dtype == cache.dtype and tuple(k_new.shape) == (cache.B, cache.Hkv, n, cache.D) == tuple(v_new.shape)
-    assert n_new is None or (n_new.dtype == torch.int32 and tuple(n_new.shape) == (cache.B,))
+    shape = k_new.shape
+    n = shape[2]
+    assert k_new.dtype == v_new.dtype == cache.dtype and shape == (cache.B, cache.Hkv, n, cache.D) and shape == v_new.shape
+    assert n_new is None or (n_new.dtype == torch.int32 and n_new.shape == (cache.B,))
     _here(cache.k8, k_new, v_new, n_new)
-    _check(lib().akb_append(C.byref(cache.struct()), _ptr(k_new), _ptr(v_new), _ptr(n_new), n, _stream()))
+    _check(lib().akb_append(cache.ref(), _ptr(k_new), _ptr(v_new), _ptr(n_new), n, _stream()))
 
 
 def akb_attention(cache: BlockCache, q: torch.Tensor, out: torch.Tensor | None = None, *, n_q: torch.Tensor | None = None, scale: float = 0.0,
@@ -585,16 +604,17 @@ def akb_attention(cache: BlockCache, q: torch.Tensor, out: torch.Tensor | None =
     """q: [B, Hq, n, D] (or [B, Hq, D]: one query token) of the cache's type; out: float32 or the cache's type, q's shape (float32 if None).
     n_q: int32 [B] query tokens of each sequence (rows behind them are left as they were), or None for n.  accumulate: add the weights to the
     cache's score.  The cache's workspace has to be large enough for n (``BlockCache.reserve``)."""
-    n = 1 if q.dim() == 3 else q.shape[2]
-    assert q.dtype == cache.dtype and tuple(q.shape) in ((cache.B, cache.Hq, n, cache.D), (cache.B, cache.Hq, cache.D))
-    assert n_q is None or (n_q.dtype == torch.int32 and tuple(n_q.shape) == (cache.B,))
+    shape = q.shape
+    n = 1 if len(shape) == 3 else shape[2]
+    assert q.dtype == cache.dtype and shape == ((cache.B, cache.Hq, cache.D) if len(shape) == 3 else (cache.B, cache.Hq, n, cache.D))
+    assert n_q is None or (n_q.dtype == torch.int32 and n_q.shape == (cache.B,))
     if out is None:
-        out = (torch.empty if n_q is None else torch.zeros)(q.shape, dtype=torch.float32, device=q.device)
-    assert out.dtype in (torch.float32, cache.dtype) and out.shape == q.shape
+        out = (torch.empty if n_q is None else torch.zeros)(shape, dtype=torch.float32, device=q.device)
+    assert out.dtype in (torch.float32, cache.dtype) and out.shape == shape
     ws = cache.workspace if workspace is None else workspace
     _here(cache.k8, q, out, n_q, ws)
-    p = akb_params(scale, 0 if out.dtype == torch.float32 else 1, int(accumulate), max_len)
-    _check(lib().akb_attention(C.byref(cache.struct()), _ptr(q), _ptr(n_q), n, _ptr(out), C.byref(p), _ptr(ws), ws.numel() * ws.element_size(), _stream()))
+    p = cache.params(scale, 0 if out.dtype == torch.float32 else 1, int(accumulate), max_len)
+    _check(lib().akb_attention(cache.ref(), _ptr(q), _ptr(n_q), n, _ptr(out), p, _ptr(ws), ws.numel() * ws.element_size(), _stream()))
     return out
 
 
@@ -611,7 +631,7 @@ def akb_evict(src: BlockCache, dst: BlockCache, keep: int, recent: int = 0, *, k
     assert kept is None or (kept.dtype == torch.int32 and tuple(kept.shape) == (src.B, src.Hkv, keep))
     ws = src.workspace if workspace is None else workspace
     _here(src.k8, dst.k8, kept, ws)
-    _check(lib().akb_evict(C.byref(src.struct()), C.byref(dst.struct()), keep, recent, _ptr(kept), _ptr(ws), ws.numel() * ws.element_size(), _stream()))
+    _check(lib().akb_evict(src.ref(), dst.ref(), keep, recent, _ptr(kept), _ptr(ws), ws.numel() * ws.element_size(), _stream()))
 
 
 def akb_unpack(cache: BlockCache) -> tuple[torch.Tensor, torch.Tensor]:

@@ -3,7 +3,7 @@
 
 namespace akb {
 
-// One workgroup of 2 D threads per (block that the call touches, side, KV head, sequence); the lanes of a wave read whole rows.
+// One workgroup of 2 D threads per (block that the call touches, KV head, sequence), for both sides; the lanes of a wave read whole rows.
 //   A complete block takes the tokens that the tail held and new ones.
 //   The incomplete last block goes to the tail, by the workgroups of the first block alone: they are the ones that read the tail.
 // Who moves the length: with few workgroups the last of the sequence by ticket (every one has read the old length by then), as in the
@@ -14,8 +14,7 @@ __global__ __launch_bounds__(2 * D) void append_kernel(akb_cache c, const uint16
 {
     __shared__ PackLds<D> lds;
     const int tid = threadIdx.x, h = blockIdx.y, b = blockIdx.z;
-    const bool is_v = blockIdx.x & 1;
-    const int j = blockIdx.x >> 1;
+    const int j = blockIdx.x;
     const int Hkv = c.shape.Hkv, Ncap = c.shape.Ncap;
     const int len = akb::seq_len(c, b);
     const int cnt = n_new ? min(max(n_new[b], 0), n) : n;
@@ -31,36 +30,41 @@ __global__ __launch_bounds__(2 * D) void append_kernel(akb_cache c, const uint16
     }
     const size_t bh = size_t(b) * Hkv + h;
     const int first = len / kTB, had = len % kTB, total = had + cnt;   // counted from the start of block `first`
-    const uint16_t* fresh = (is_v ? v_new : k_new) + bh * n * D;
     const BlockLane<D> at(tid);
-    auto load_fresh = [&](int w) -> u32x4_t {             // token w counted from the start of block `first`
-        return w >= had && w < total ? *reinterpret_cast<const u32x4_t*>(fresh + size_t(w - had) * D + at.oct * 8) : u32x4_t{0, 0, 0, 0};
-    };
     const int t0 = at.t0;
-    if ((j + 1) * kTB <= total) {
-        u32x4_t x[4];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) x[r] = load_fresh(j * kTB + t0 + r);
-        if (j == 0 && had > 0) {
-            const bool old[4] = {t0 < had, t0 + 1 < had, t0 + 2 < had, t0 + 3 < had};
-            const int token[4] = {t0, t0 + 1, t0 + 2, t0 + 3};
-            load_tail<D, true>(c, bh, is_v, x, old, token);
+    for (int side = 0; side < 2; ++side) {
+        const bool is_v = side == 1;
+        const uint16_t* fresh = (is_v ? v_new : k_new) + bh * n * D;
+        auto load_fresh = [&](int w) -> u32x4_t {             // token w counted from the start of block `first`
+            return w >= had && w < total ? *reinterpret_cast<const u32x4_t*>(fresh + size_t(w - had) * D + at.oct * 8) : u32x4_t{0, 0, 0, 0};
+        };
+        if ((j + 1) * kTB <= total) {
+            u32x4_t x[4];
+    #pragma unroll
+            for (int r = 0; r < 4; ++r) x[r] = load_fresh(j * kTB + t0 + r);
+            if (j == 0 && had > 0) {
+                const bool old[4] = {t0 < had, t0 + 1 < had, t0 + 2 < had, t0 + 3 < had};
+                const int token[4] = {t0, t0 + 1, t0 + 2, t0 + 3};
+                load_tail<D, true>(c, bh, is_v, x, old, token);
+            }
+            if (is_v) __syncthreads();   // K's block has been packed
+            pack_block<T, D>(c, bh * (Ncap / kTB) + first + j, is_v, x, lds);
         }
-        pack_block<T, D>(c, bh * (Ncap / kTB) + first + j, is_v, x, lds);
-    }
-    if (j == 0 && total % kTB) {   // the incomplete block: its new tokens go to the tail (what of the old ones is needed has been read)
-        __syncthreads();
-        const int last = total / kTB * kTB;
-        u32x4_t x[4];
-        bool store[4];
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            x[r] = load_fresh(last + t0 + r);
-            store[r] = last + t0 + r >= had && last + t0 + r < total;
+        if (j == 0 && total % kTB) {   // the incomplete block: its new tokens go to the tail (what of the old ones is needed has been read)
+            __syncthreads();
+            const int last = total / kTB * kTB;
+            u32x4_t x[4];
+            bool store[4];
+    #pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                x[r] = load_fresh(last + t0 + r);
+                store[r] = last + t0 + r >= had && last + t0 + r < total;
+            }
+            store_tail<D>(c, bh, is_v, x, store);
         }
-        store_tail<D>(c, bh, is_v, x, store);
     }
-    if (c.score && !is_v && tid < kTB) {   // the new tokens' scores
+    if (c.score && tid < kTB) {   // the new tokens' scores
         const int w = j * kTB + tid;
         if (w >= had && w < total) c.score[bh * Ncap + first * kTB + w] = 0.f;
     }
@@ -84,8 +88,10 @@ hipError_t launch_append(const akb_cache& c, const uint16_t* k_new, const uint16
 {
     if (n == 0) return hipSuccess;
     const int blocks = (kTB - 1 + n + kTB - 1) / kTB;
-    const dim3 grid(2 * blocks, c.shape.Hkv, c.shape.B);
-    const bool ticketed = long(grid.x) * grid.y * grid.z <= 320;
+    const dim3 grid(blocks, c.shape.Hkv, c.shape.B);
+    // A ticket per workgroup or a launch behind: device time of one token 128 workgroups 4.1 us, 512 6.0 (64 sequences) and 7.8 (16) against 4.0 + 1.4 and the gap
+    // between the two launches; 1024 8.8 and 14.6.  (Of one side per workgroup they would be twice as many, and gain nothing: 8 x 8 pairs 8192 tokens 77 us.)
+    const bool ticketed = long(grid.x) * grid.y * grid.z <= 640;
     auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(2 * c.shape.D), 0, st, c, k_new, v_new, n_new, n, ticketed ? 1 : 0); };
     if (c.shape.dtype == AKB_FP16) c.shape.D == 64 ? launch(append_kernel<Fp16, 64>) : launch(append_kernel<Fp16, 128>);
     else c.shape.D == 64 ? launch(append_kernel<Bf16, 64>) : launch(append_kernel<Bf16, 128>);
