@@ -131,8 +131,8 @@ int32_t akb_attention_path(const akb_shape *shape, int32_t n, int32_t max_len, i
  * the min(recent, kept) last ones and, of the others, those of the largest score.  A NaN counts as the largest.  dst has src's
  * B, Hkv, D and dtype, Ncap >= keep, and shares no memory with src; what it held is replaced, lens[b] becomes
  * min(lens[b], keep).  src needs a score; dst->score may be NULL.  kept: NULL, or device int32 [B][Hkv][keep] that
- * receives the kept tokens' places in src, ascending, -1 behind the last (the workspace is needed only where it is NULL).
- * src is not written.
+ * receives the kept tokens' places in src, ascending, -1 behind the last.  src is not written.
+ * workspace: as for akb_attention, of akb_evict_workspace(src's shape, keep) bytes or more.
  */
 akv_status akb_evict(const akb_cache *src, const akb_cache *dst, int32_t keep, int32_t recent, int32_t *kept, void *workspace, size_t workspace_bytes,
                      void *stream);

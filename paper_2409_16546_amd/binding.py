@@ -627,7 +627,7 @@ def akb_attention_path(B: int, Hq: int, Hkv: int, D: int, Ncap: int, n: int = 1,
 def akb_evict(src: BlockCache, dst: BlockCache, keep: int, recent: int = 0, *, kept: torch.Tensor | None = None,
               workspace: torch.Tensor | None = None) -> None:
     """Bring every (sequence, KV head) of src down to its `keep` best tokens, in dst.  kept: int32 [B, Hkv, keep] receiving their places in src, or
-    None (then a workspace: src's has to be large enough for `keep`, ``BlockCache.reserve``)."""
+    None.  src's workspace has to be large enough for `keep` (``BlockCache.reserve``)."""
     assert kept is None or (kept.dtype == torch.int32 and tuple(kept.shape) == (src.B, src.Hkv, keep))
     ws = src.workspace if workspace is None else workspace
     _here(src.k8, dst.k8, kept, ws)

@@ -137,7 +137,7 @@ size_t akb_evict_workspace(const akb_shape* shape, int32_t keep)
         fail(AKV_EINVAL, "bad shape, or keep below 1");
         return 0;
     }
-    return akv::align256(akb::attention_tickets()) + akv::align256(size_t(shape->B) * shape->Hkv * size_t(keep) * sizeof(int32_t));
+    return akv::align256(akb::attention_tickets()) + akb::evict_workspace(*shape, keep);
 }
 
 akv_status akb_evict(const akb_cache* src, const akb_cache* dst, int32_t keep, int32_t recent, int32_t* kept, void* workspace, size_t workspace_bytes, void* stream)
@@ -161,11 +161,9 @@ akv_status akb_evict(const akb_cache* src, const akb_cache* dst, int32_t keep, i
             if (y.n && xp < yp + y.n && yp < xp + x.n) return fail(AKV_EINVAL, "src and dst share memory");
         }
     if (!aligned(kept, 4)) return fail(AKV_EINVAL, "kept must be 4-byte aligned");
-    if (!kept) {
-        if (akv_status st = check_workspace(workspace, workspace_bytes, akb_evict_workspace(&s, keep))) return st;
-        kept = reinterpret_cast<int32_t*>(static_cast<char*>(workspace) + akv::align256(akb::attention_tickets()));
-    }
-    return hip_result(akb::launch_evict(*src, *dst, keep, recent, kept, static_cast<hipStream_t>(stream)), "evict launch");
+    if (akv_status st = check_workspace(workspace, workspace_bytes, akb_evict_workspace(&s, keep))) return st;
+    char* ws = static_cast<char*>(workspace) + akv::align256(akb::attention_tickets());   // (what lies in front is attention's between calls)
+    return hip_result(akb::launch_evict(*src, *dst, keep, recent, kept, ws, static_cast<hipStream_t>(stream)), "evict launch");
 }
 
 akv_status akb_unpack(const akb_cache* cache, uint16_t* k_out, uint16_t* v_out, void* stream)

@@ -18,7 +18,8 @@ inline size_t blocks(const akb_shape& s) { return size_t(s.Ncap) / kTB; }
 // host launchers, each defined next to its kernels
 hipError_t launch_append(const akb_cache& c, const uint16_t* k_new, const uint16_t* v_new, const int32_t* n_new, int n, hipStream_t st);
 hipError_t launch_unpack(const akb_cache& c, uint16_t* k_out, uint16_t* v_out, hipStream_t st);
-hipError_t launch_evict(const akb_cache& src, const akb_cache& dst, int keep, int recent, int32_t* kept, hipStream_t st);
+size_t evict_workspace(const akb_shape& s, int keep);
+hipError_t launch_evict(const akb_cache& src, const akb_cache& dst, int keep, int recent, int32_t* kept, char* ws, hipStream_t st);   // kept: or NULL
 
 struct AttentionArgs {
     akb_cache c;

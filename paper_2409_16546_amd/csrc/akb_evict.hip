@@ -138,6 +138,128 @@ __global__ __launch_bounds__(kSelThreads) void select_kernel(akb_cache c, akb_ca
     if (h == 0 && tid == 0) d.lens[b] = count;
 }
 
+// The same for few heads with long rows, where one workgroup per head would leave most of the device idle: a workgroup per 8192 scores, and a launch per step, since
+// every step needs the counts of all of a head's workgroups.  Steps 0 to 2 count 11, 11 and 10 bits (integers: their order does not matter), 3 counts the tokens
+// above the threshold and at it per workgroup, 4 writes the places.
+constexpr int kChunk = kSelThreads * kPer;
+struct SelectWs {
+    int32_t* hist;    // [3][pairs][kBins]
+    int32_t* state;   // [3][pairs][2]: bits of the threshold so far, tokens still needed
+    int32_t* counts;  // [pairs][chunks][2]
+};
+template <int STEP>
+__global__ __launch_bounds__(kSelThreads) void select_step_kernel(akb_cache c, akb_cache d, int keep, int recent, int32_t* __restrict__ kept, SelectWs ws)
+{
+    __shared__ int hist_s[STEP < 3 ? kCopies * kBins : 1];
+    __shared__ int wave_s[kSelThreads / 64];
+    __shared__ int found_s[2];
+    const int chunk = blockIdx.x, h = blockIdx.y, b = blockIdx.z, tid = threadIdx.x;
+    const size_t pairs = size_t(c.shape.B) * c.shape.Hkv, bh = size_t(b) * c.shape.Hkv + h;
+    const int len = seq_len(c, b), count = min(len, keep), sure = min(recent, count), pool = len - sure;
+    const int want = count - sure;
+    const bool choose = want > 0 && want < pool;
+    int32_t* out = kept + bh * keep;
+    if (STEP == 4 && chunk == 0) {
+        for (int i = tid; i < sure; i += kSelThreads) out[want + i] = len - sure + i;
+        for (int i = count + tid; i < keep; i += kSelThreads) out[i] = -1;
+        if (h == 0 && tid == 0) d.lens[b] = count;
+    }
+    if (chunk * kChunk >= pool || want <= 0) return;
+    const int t0 = chunk * kChunk + tid * kPer;
+    if (!choose) {   // all stay
+        if (STEP == 4)
+            for (int i = 0; i < kPer; ++i)
+                if (t0 + i < pool) out[t0 + i] = t0 + i;
+        return;
+    }
+    uint32_t key[kPer];
+    {
+        const float* score = c.score + bh * c.shape.Ncap;
+        f32x4_t v[kPer / 4];
+#pragma unroll
+        for (int i = 0; i < kPer / 4; ++i) v[i] = t0 + 4 * i < pool ? *reinterpret_cast<const f32x4_t*>(score + t0 + 4 * i) : f32x4_t{0, 0, 0, 0};   // rows are whole blocks long
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) key[i] = order_key(v[i >> 2][i & 3]);
+    }
+    uint32_t prefix = 0;
+    int need = want;
+    if (STEP > 0) {   // what the step before has counted: the value of its bits that the threshold has
+        const int at = min(STEP, 3) - 1, bits = at == 2 ? 10 : 11;
+        const int32_t* state = ws.state + (size_t(at) * pairs + bh) * 2;
+        if (STEP == 4) {
+            prefix = state[0];
+            need = state[1];
+        } else {
+            if (at > 0) {
+                prefix = state[-2 * int(pairs)];
+                need = state[1 - 2 * int(pairs)];
+            }
+            const int32_t* hist = ws.hist + (size_t(at) * pairs + bh) * kBins;
+            const int top = kBins - 1 - 2 * tid, h0 = hist[top], h1 = hist[top - 1];
+            int all;
+            const int upto = block_scan(h0 + h1, wave_s, &all), before = upto - h0 - h1;
+            if (before < need && need <= upto) {
+                const bool first = need <= before + h0;
+                found_s[0] = first ? top : top - 1;
+                found_s[1] = first ? before : before + h0;
+            }
+            __syncthreads();
+            prefix = (prefix << bits) | uint32_t(found_s[0]);
+            need -= found_s[1];
+            if (chunk == 0 && tid == 0) {
+                int32_t* mine = ws.state + (size_t(at) * pairs + bh) * 2;
+                mine[0] = int32_t(prefix);
+                mine[1] = need;
+            }
+        }
+    }
+    if constexpr (STEP < 3) {
+        const int shift = STEP == 0 ? 21 : (STEP == 1 ? 10 : 0), bits = STEP == 2 ? 10 : 11;
+        for (int i = tid; i < kCopies * kBins; i += kSelThreads) hist_s[i] = 0;
+        __syncthreads();
+        int* mine = hist_s + (tid % kCopies) * kBins;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i)
+            if (t0 + i < pool && (STEP == 0 || (key[i] >> (shift + bits)) == prefix)) atomicAdd(&mine[(key[i] >> shift) & ((1u << bits) - 1)], 1);
+        __syncthreads();
+        int32_t* hist = ws.hist + (size_t(STEP) * pairs + bh) * kBins;
+        for (int i = tid; i < kBins; i += kSelThreads) {
+            int sum = 0;
+#pragma unroll
+            for (int k = 0; k < kCopies; ++k) sum += hist_s[k * kBins + i];
+            if (sum) atomicAdd(hist + i, sum);
+        }
+    } else {
+        int mine = 0;   // above the threshold in the low half, at it in the high half
+#pragma unroll
+        for (int i = 0; i < kPer; ++i)
+            if (t0 + i < pool) mine += key[i] > prefix ? 1 : (key[i] == prefix ? 1 << 16 : 0);
+        int all;
+        const int upto = block_scan(mine, wave_s, &all) - mine;
+        int32_t* counts = ws.counts + bh * gridDim.x * 2;
+        if constexpr (STEP == 3) {
+            if (tid == 0) {
+                counts[2 * chunk] = all & 0xFFFF;
+                counts[2 * chunk + 1] = all >> 16;
+            }
+        } else {
+            int above = 0, ties = 0;   // of the chunks before
+            for (int i = 0; i < chunk; ++i) {
+                above += counts[2 * i];
+                ties += counts[2 * i + 1];
+            }
+            int a = above + (upto & 0xFFFF), e = ties + (upto >> 16);
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) {
+                if (t0 + i >= pool) continue;
+                if (key[i] > prefix || (key[i] == prefix && e < need)) out[a + min(e, need)] = t0 + i;
+                a += key[i] > prefix ? 1 : 0;
+                e += key[i] == prefix ? 1 : 0;
+            }
+        }
+    }
+}
+
 // A block of the destination: one workgroup of 2 D threads per (block, side, KV head, sequence), as in the append.  K: a token's codes are runs of 64
 // bytes, read where they lie.  V: a token is one byte in each channel's 64 (read where they lie, a wave's byte loads touched 64 lines each, 4 of
 // 5 parts of the time), so the source blocks that hold a kept token are read whole, one after the other, into LDS (rows padded to 17 dwords,
@@ -233,10 +355,41 @@ __global__ __launch_bounds__(2 * D) void gather_kernel(akb_cache c, akb_cache d,
     else store_tail<D>(d, bh, is_v, x, stays);
 }
 
-hipError_t launch_evict(const akb_cache& src, const akb_cache& dst, int keep, int recent, int32_t* kept, hipStream_t st)
+// Workgroups per head where the heads are few and their rows long.  One workgroup per head / a launch per step, us: 8 heads 131001 -> 16384
+// tokens 124.6 / 75.8 with the gather, 32 of 65536 -> 4096 125 / 110, 8 of 32768 38.1 / 37.3; 32 of 16384 41.8 / 48.8, 128 of 40000 171 / 182, 256 of 32768 270 / 299.
+static int chunks_of(const akb_shape& s)
+{
+    const int chunks = (s.Ncap + kChunk - 1) / kChunk;
+    return long(s.B) * s.Hkv <= 64 && chunks > 4 ? chunks : 1;
+}
+static size_t kept_bytes(const akb_shape& s, int keep) { return align256(size_t(s.B) * s.Hkv * size_t(keep) * sizeof(int32_t)); }
+size_t evict_workspace(const akb_shape& s, int keep)
+{
+    const int chunks = chunks_of(s);
+    return kept_bytes(s, keep) + (chunks > 1 ? align256(size_t(s.B) * s.Hkv * (3 * (kBins + 2) + 2 * size_t(chunks)) * sizeof(int32_t)) : 0);
+}
+
+hipError_t launch_evict(const akb_cache& src, const akb_cache& dst, int keep, int recent, int32_t* kept, char* ws, hipStream_t st)
 {
     const akb_shape& s = src.shape;
-    hipLaunchKernelGGL(select_kernel, dim3(s.Hkv, s.B), dim3(kSelThreads), 0, st, src, dst, keep, recent, kept);
+    const int chunks = chunks_of(s);
+    if (!kept) kept = reinterpret_cast<int32_t*>(ws);
+    if (chunks == 1) {
+        hipLaunchKernelGGL(select_kernel, dim3(s.Hkv, s.B), dim3(kSelThreads), 0, st, src, dst, keep, recent, kept);
+    } else {
+        const size_t pairs = size_t(s.B) * s.Hkv;
+        SelectWs w;
+        w.hist = reinterpret_cast<int32_t*>(ws + kept_bytes(s, keep));
+        w.state = w.hist + 3 * pairs * kBins;
+        w.counts = w.state + 3 * pairs * 2;
+        if (hipError_t e = akv::launch_zero(w.hist, 3 * pairs * kBins * sizeof(int32_t), st)) return e;
+        auto step = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(chunks, s.Hkv, s.B), dim3(kSelThreads), 0, st, src, dst, keep, recent, kept, w); };
+        step(select_step_kernel<0>);
+        step(select_step_kernel<1>);
+        step(select_step_kernel<2>);
+        step(select_step_kernel<3>);
+        step(select_step_kernel<4>);
+    }
     if (hipError_t e = hipGetLastError()) return e;
     const int blocks = (std::min(keep, s.Ncap) + kTB - 1) / kTB;
     auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(2 * blocks, s.Hkv, s.B), dim3(2 * s.D), 0, st, src, dst, keep, kept); };

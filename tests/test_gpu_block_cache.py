@@ -287,14 +287,16 @@ def test_offsets_beyond_32_bits(A):
 
 @pytest.mark.parametrize("dtype,D", [(F16, 128), (B16, 64)])
 @pytest.mark.parametrize("lens,keep,recent", [([300, 128, 0, 1, 200], 128, 30), ([300, 64, 65, 700, 129], 65, 0), ([90, 200, 500], 200, 200),
-                                              ([1500, 64, 1023], 1, 0), ([1100, 3], 1000, 64)])
+                                              ([1500, 64, 1023], 1, 0), ([1100, 3], 1000, 64),
+                                              ([40000, 33, 0, 20001, 5000], 5000, 100), ([33000, 8193], 8000, 0)])
 def test_evict(A, dtype, D, lens, keep, recent):
-    B = len(lens)
-    c, ref = pair(A, B, 2, 2, D, 1536, dtype, score=True)
+    """(More than 32768 tokens of capacity and few heads: a launch per step of the selection.)"""
+    B, Ncap = len(lens), max(1536, (max(lens) + 63) // 64 * 64)
+    c, ref = pair(A, B, 2, 2, D, Ncap, dtype, score=True)
     put(A, c, ref, max(lens), 3, lens)
-    score = torch.rand(B, 2, 1536, generator=torch.Generator().manual_seed(8))
+    score = torch.rand(B, 2, Ncap, generator=torch.Generator().manual_seed(8))
     score = torch.where(score < 0.3, torch.round(score * 8) / 8, score)     # many equal ones, zeros among them
-    score[:, 0] *= torch.exp2(torch.randint(-60, 3, (B, 1536), generator=torch.Generator().manual_seed(9)).float())
+    score[:, 0] *= torch.exp2(torch.randint(-60, 3, (B, Ncap), generator=torch.Generator().manual_seed(9)).float())
     if lens[0] > 20:
         score[0, 1, 3], score[0, 1, 11], score[0, 1, 17] = float("nan"), float("inf"), -0.0
     c.score.copy_(score.flatten())
@@ -307,7 +309,7 @@ def test_evict(A, dtype, D, lens, keep, recent):
         want.Ncap = d.Ncap
         kept = torch.full((B, 2, keep), 99, dtype=torch.int32, device=DEV)
         if with_score:
-            A.akb_evict(c, d, keep, recent, kept=kept)
+            A.akb_evict(c.reserve(1, keep), d, keep, recent, kept=kept)
             assert np.array_equal(kept.cpu().numpy(), places)
             got = d.score.view(B, 2, -1).cpu().numpy()
             for b in range(B):
