@@ -18,6 +18,7 @@ struct AttentionPlan {
     int splits;     // parts of a walk, or 0: cut by the device
     int grid;       // workgroups at most
     bool ticketed;  // the last workgroup of a row group joins its parts; otherwise a launch does
+    bool streamed;  // codes are read with the non-temporal hint
     int shares;     // parts the rows are cut into for the score
     size_t tickets, parts, logits, stats, total;   // offsets into the workspace
 };
@@ -48,6 +49,9 @@ static AttentionPlan plan(const akb_shape& s, int n, int max_len, bool accumulat
     p.tickets = 0;
     p.parts = align256(size_t(2 * slots) * sizeof(int32_t));
     p.logits = p.parts + align256(size_t(2 * slots) * part_floats((int)std::min(rows, long(kPromptRows)), s.D) * sizeof(float));
+    // Codes that are read once and are more than half of the last-level cache pass it by.  Plain / with the hint, us: 1.07 GB of 512 pairs 196 / 178, 268 MB of 256 54.0 / 47.2, 0.67 GB of
+    // 32 long ones 121 / 106; below, what a call finds there of the call before counts: 134 MB 26.0 / 26.4, 67 MB 15.6 / 15.9, two row groups of 50 MB 25.4 / 27.3.
+    p.streamed = p.tiles == 1 && size_t(pairs) * max_len * s.D * 2 > (size_t(128) << 20);
     // the score of many rows: two rounds of workgroups, at most eight shares of 256 rows or more
     const long quads = pairs * ((blocks + kWaves - 1) / kWaves);
     p.shares = (int)std::max(1L, std::min({(2 * slots + quads - 1) / quads, 8L, rows / 256}));
@@ -65,7 +69,13 @@ int attention_path(const akb_shape& s, int n, int max_len, int32_t* parts)
 size_t attention_tickets() { return size_t(4) * akv::compute_units() * sizeof(int32_t); }
 
 // A block of K or V as the matrix instructions take it: lane (token t % 16 or channel % 16, quarter): 16 codes
-template <int D> struct KCodes {
+// NT: with the non-temporal hint
+template <bool NT> __device__ __forceinline__ u32x4_t load_codes(const uint8_t* p)
+{
+    const u32x4_t* w = reinterpret_cast<const u32x4_t*>(p);
+    return NT ? __builtin_nontemporal_load(w) : *w;
+}
+template <int D, bool NT> struct KCodes {
     u32x4_t w[4][D / 64];
     float s;
     __device__ __forceinline__ void load(const akb_cache& c, size_t block, int lane)
@@ -74,18 +84,18 @@ template <int D> struct KCodes {
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
-            for (int i = 0; i < D / 64; ++i) w[t][i] = *reinterpret_cast<const u32x4_t*>(p + t * (16 * D) + i * 1024);
+            for (int i = 0; i < D / 64; ++i) w[t][i] = load_codes<NT>(p + t * (16 * D) + i * 1024);
         s = pow2(c.exps[block * 2]);
     }
 };
-template <int D> struct VCodes {
+template <int D, bool NT> struct VCodes {
     u32x4_t w[D / 16];
     float s;
     __device__ __forceinline__ void load(const akb_cache& c, size_t block, int lane)
     {
         const uint8_t* p = c.v8 + block * (kTB * D) + (lane & 15) * 64 + (lane >> 4) * 16;
 #pragma unroll
-        for (int i = 0; i < D / 16; ++i) w[i] = *reinterpret_cast<const u32x4_t*>(p + i * 1024);
+        for (int i = 0; i < D / 16; ++i) w[i] = load_codes<NT>(p + i * 1024);
         s = pow2(c.exps[block * 2 + 1]);
     }
 };
@@ -166,7 +176,7 @@ __device__ __forceinline__ void store_logits(float* block, const f32x4_t (&s)[4]
 // through LDS.  Where a row group has several splits, the last of its workgroups to arrive joins them (the parts go through memory with device scope, as
 // the partial results of the 16-bit cache's V kernel do).  EXACT: 32-bit results; the weights go into the second product as two 16-bit numbers each (their
 // sum carries 16 bits or more where one carries 8 or 11, which is what a 16-bit result keeps).
-template <class T, int D, bool EXACT, int RT>
+template <class T, int D, bool EXACT, int RT, bool NT>
 __global__ __launch_bounds__(64 * kWaves, 2) void rows_kernel(RowArgs a)
 {
     __shared__ float o_s[kWaves][kTileRows][D + 4];
@@ -200,10 +210,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void rows_kernel(RowArgs a)
     float* logits = RT == 1 && a.logits ? a.logits + bh * min(a.n * G, 16) * c.shape.Ncap : nullptr;
     const size_t block0 = bh * (c.shape.Ncap / kTB);
     int blk = lo + wave;
-    KCodes<D> kc;
+    KCodes<D, NT> kc;
     if (blk < whole) kc.load(c, block0 + blk, lane);
     for (; blk < whole; blk += kWaves) {
-        VCodes<D> vc;
+        VCodes<D, NT> vc;
         vc.load(c, block0 + blk, lane);
         f32x4_t s[RT][4];
 #pragma unroll
@@ -570,8 +580,13 @@ template <class T, int D> static hipError_t launch(const RowArgs& r, const Atten
     auto rows = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(akv::xcd_grid(grid)), dim3(64 * kWaves), 0, st, r); };
     if (tiles > 2) {
         if (hipError_t e = launch_prompt(r, grid, st)) return e;
-    } else if (r.out_dtype == 0) tiles == 1 ? rows(rows_kernel<T, D, true, 1>) : rows(rows_kernel<T, D, true, 2>);
-    else tiles == 1 ? rows(rows_kernel<T, D, false, 1>) : rows(rows_kernel<T, D, false, 2>);
+    } else if (tiles == 2) {
+        r.out_dtype == 0 ? rows(rows_kernel<T, D, true, 2, false>) : rows(rows_kernel<T, D, false, 2, false>);
+    } else if (p.streamed) {
+        r.out_dtype == 0 ? rows(rows_kernel<T, D, true, 1, true>) : rows(rows_kernel<T, D, false, 1, true>);
+    } else {
+        r.out_dtype == 0 ? rows(rows_kernel<T, D, true, 1, false>) : rows(rows_kernel<T, D, false, 1, false>);
+    }
     if (hipError_t e = hipGetLastError()) return e;
     if (r.splits != 1 && !r.tickets) {
         const int rows_all = r.n * (s.Hq / s.Hkv);
