@@ -114,8 +114,9 @@ akv_status akb_workspace_init(void *workspace, size_t workspace_bytes, void *str
 /*
  * Attention of n query tokens per sequence.  q: device [B][Hq][n][D] of the shape's type.  n_q: device int32 [B] with the
  * number of leading query tokens (0..n) of each sequence, or NULL for n.  out: device [B][Hq][n][D] of params->out_dtype;
- * B * Hq * n < 2^29.  Rows i >= n_q[b] are left as they were; a query token that sees nothing yields zeros.  workspace: device scratch, 256-B
- * aligned, prepared by akb_workspace_init; calls that overlap need distinct ones, and it holds nothing between calls.  params may be
+ * B * Hkv * ceil(n Hq/Hkv / 16) < 2^24.  Rows i >= n_q[b] are left as they were; a query token that sees nothing yields zeros.  workspace: device scratch, 256-B
+ * aligned, prepared by akb_workspace_init; calls that overlap need distinct ones, and it holds nothing between calls.
+ * Calls that accumulate into one cache's score must be ordered on one stream.  params may be
  * NULL (float32 out, no accumulation).  The same call gives the same bits.
  */
 akv_status akb_attention(const akb_cache *cache, const uint16_t *q, const int32_t *n_q, int32_t n, void *out, const akb_params *params,

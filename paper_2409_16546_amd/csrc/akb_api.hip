@@ -110,7 +110,8 @@ akv_status akb_attention(const akb_cache* cache, const uint16_t* q, const int32_
     akb_params p = {};
     if (params) p = *params;
     if (n < 0 || n > s.Ncap) return fail(AKV_EINVAL, "n = %d out of range 0..Ncap", n);
-    if (size_t(s.B) * s.Hq * n >= (size_t(1) << 29)) return fail(AKV_EINVAL, "B * Hq * n = %zu query rows: 2^29 or more", size_t(s.B) * s.Hq * n);
+    const size_t tiles = size_t(s.B) * s.Hkv * ((size_t(n) * (s.Hq / s.Hkv) + 15) / 16);
+    if (tiles >= (size_t(1) << 24)) return fail(AKV_EINVAL, "%zu tiles of 16 query rows: 2^24 or more", tiles);
     if (p.out_dtype != 0 && p.out_dtype != 1) return fail(AKV_EINVAL, "out_dtype = %d is neither 0 (f32) nor 1 (the cache's 16-bit type)", p.out_dtype);
     if (p.max_len < 0 || p.max_len > s.Ncap) return fail(AKV_EINVAL, "max_len = %d out of range 0..Ncap", p.max_len);
     if (!std::isfinite(p.scale)) return fail(AKV_EINVAL, "scale is not finite");

@@ -487,7 +487,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void score_kernel(RowArgs a, int sh
             }
             if (tid < kScoreRows) {
                 const int row = turn * kScoreRows + tid;
-                stat = row < m * G ? *reinterpret_cast<const f32x2_t*>(a.stats + (bh * n * G + row) * 2) : f32x2_t{0.f, 0.f};   // a row behind the last weighs nothing
+                stat = row < m * G ? *reinterpret_cast<const f32x2_t*>(a.stats + (bh * n * G + row) * 2) : f32x2_t{__builtin_inff(), 0.f};   // a row behind the last weighs 2^-inf
             }
         };
         auto put = [&](int to) {

@@ -312,8 +312,8 @@ __global__ __launch_bounds__(2 * D) void gather_kernel(akb_cache c, akb_cache d,
         u32x4_t piece[2];
         auto fetch = [&](int first) {
             const uint8_t* p = c.v8 + (block0 + __builtin_amdgcn_readlane(src, first)) * (kTB * D) + tid * 16;
-            piece[0] = *reinterpret_cast<const u32x4_t*>(p);
-            piece[1] = *reinterpret_cast<const u32x4_t*>(p + 2 * D * 16);
+            piece[0] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(p));
+            piece[1] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(p + 2 * D * 16));
         };
         if (starts) fetch(0);
         while (starts) {

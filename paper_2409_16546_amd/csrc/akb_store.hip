@@ -8,7 +8,7 @@ namespace akb {
 //   The incomplete last block goes to the tail, by the workgroups of the first block alone: they are the ones that read the tail.
 // Who moves the length: with few workgroups the last of the sequence by ticket (every one has read the old length by then), as in the
 // append of the 16-bit cache; otherwise a launch behind this one.
-template <class T, int D>
+template <class T, int D, bool NT>
 __global__ __launch_bounds__(2 * D) void append_kernel(akb_cache c, const uint16_t* __restrict__ k_new, const uint16_t* __restrict__ v_new,
                                                        const int32_t* __restrict__ n_new, int n, int ticketed)
 {
@@ -37,11 +37,13 @@ __global__ __launch_bounds__(2 * D) void append_kernel(akb_cache c, const uint16
         const bool is_v = side == 1;
         const uint16_t* fresh = (is_v ? v_new : k_new) + bh * n * D;
         auto load_fresh = [&](int w) -> u32x4_t {             // token w counted from the start of block `first`
-            return w >= had && w < total ? *reinterpret_cast<const u32x4_t*>(fresh + size_t(w - had) * D + at.oct * 8) : u32x4_t{0, 0, 0, 0};
+            if (w < had || w >= total) return u32x4_t{0, 0, 0, 0};
+            const u32x4_t* p = reinterpret_cast<const u32x4_t*>(fresh + size_t(w - had) * D + at.oct * 8);
+            return NT ? __builtin_nontemporal_load(p) : *p;
         };
         if ((j + 1) * kTB <= total) {
             u32x4_t x[4];
-    #pragma unroll
+#pragma unroll
             for (int r = 0; r < 4; ++r) x[r] = load_fresh(j * kTB + t0 + r);
             if (j == 0 && had > 0) {
                 const bool old[4] = {t0 < had, t0 + 1 < had, t0 + 2 < had, t0 + 3 < had};
@@ -56,7 +58,7 @@ __global__ __launch_bounds__(2 * D) void append_kernel(akb_cache c, const uint16
             const int last = total / kTB * kTB;
             u32x4_t x[4];
             bool store[4];
-    #pragma unroll
+#pragma unroll
             for (int r = 0; r < 4; ++r) {
                 x[r] = load_fresh(last + t0 + r);
                 store[r] = last + t0 + r >= had && last + t0 + r < total;
@@ -93,8 +95,12 @@ hipError_t launch_append(const akb_cache& c, const uint16_t* k_new, const uint16
     // between the two launches; 1024 8.8 and 14.6.  (Of one side per workgroup they would be twice as many, and gain nothing: 8 x 8 pairs 8192 tokens 77 us.)
     const bool ticketed = long(grid.x) * grid.y * grid.z <= 640;
     auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(2 * c.shape.D), 0, st, c, k_new, v_new, n_new, n, ticketed ? 1 : 0); };
-    if (c.shape.dtype == AKB_FP16) c.shape.D == 64 ? launch(append_kernel<Fp16, 64>) : launch(append_kernel<Fp16, 128>);
-    else c.shape.D == 64 ? launch(append_kernel<Bf16, 64>) : launch(append_kernel<Bf16, 128>);
+    // New tokens that are more than half of the last-level cache are read with the non-temporal hint; fewer may still lie there as they were made.  Plain / with the
+    // hint: 8 x 8 pairs 8192 tokens (268 MB) 75.3 / 68.8 us, 6 x 32 pairs up to 777 tokens (76 MB at most, read again and again) 28.9 / 33.8.
+    const bool streamed = size_t(c.shape.B) * c.shape.Hkv * n * c.shape.D * 4 > (size_t(128) << 20);
+    auto pick = [&](auto plain, auto hinted) { streamed ? launch(hinted) : launch(plain); };
+    if (c.shape.dtype == AKB_FP16) c.shape.D == 64 ? pick(append_kernel<Fp16, 64, false>, append_kernel<Fp16, 64, true>) : pick(append_kernel<Fp16, 128, false>, append_kernel<Fp16, 128, true>);
+    else c.shape.D == 64 ? pick(append_kernel<Bf16, 64, false>, append_kernel<Bf16, 64, true>) : pick(append_kernel<Bf16, 128, false>, append_kernel<Bf16, 128, true>);
     if (hipError_t e = hipGetLastError()) return e;
     if (!ticketed) hipLaunchKernelGGL(append_lens_kernel, dim3(1), dim3(256), 0, st, c, n_new, n);
     return hipGetLastError();

@@ -107,8 +107,8 @@ def test_refusals_come_before_any_launch(A):
     refused(attention(ws=None), "needed", A.AKV_EWORKSPACE)
     refused(attention(size=64), "needed", A.AKV_EWORKSPACE)
     assert attention(n=0, q=None, out=None, ws=None) == A.AKV_OK
-    many = A.akb_cache(A.akb_shape(64, 64, 4, 64, 1 << 18, 0), **ADDR)
-    refused(attention(c=many, n=1 << 17, size=1 << 50), "2^29")
+    many = A.akb_cache(A.akb_shape(128, 64, 4, 64, 1 << 18, 0), **ADDR)
+    refused(attention(c=many, n=1 << 17, size=1 << 50), "2^24")
 
     to = {n: a + 0x100000000 for n, a in ADDR.items()}
 

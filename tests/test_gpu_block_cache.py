@@ -162,6 +162,7 @@ LARGE = [
     ((1, 4), F16, F32, 128, 1, 4, 4, 1000, False, 1, False),         # parts joined by the last workgroup
     ((1, 64), B16, B16, 128, 1, 64, 8, 20000, False, 1, False),      # ... by a launch, many parts
     ((1, 8), B16, F32, 64, 1, 32, 8, 2000, False, 2, False),
+    ((1, 2), F16, F32, 64, 300, 4, 1, 600, True, 1, True),           # more sequences than the device would look through
     ((1, 1), F16, F16, 128, 16, 32, 32, 300, True, 1, False),        # whole walks
     ((1, 0), F16, F32, 128, 4, 32, 32, 9000, True, 1, False),        # parts by the lengths
     ((1, 0), B16, B16, 64, 3, 64, 4, 90000, True, 1, False),
@@ -256,6 +257,20 @@ def test_scores_far_apart_and_outlier_values(A):
         q = R.tokens(1, 2, 3, 128, dtype, 7, "plain") * 40
         c.reserve(3)
         R.assert_attention(A.akb_attention(c, q.to(DEV)), *ref.attention(q), dtype, str(dtype))
+
+
+@pytest.mark.parametrize("n", [1, 30, 100])
+def test_scores_of_logits_far_apart(A, n):
+    """Logits of hundreds: rows that fill a tile behind the last one weigh nothing, whatever their products are."""
+    c, ref = pair(A, 1, 1, 1, 128, 1600, B16, score=True, n=100)
+    k, v = R.tokens(1, 1, 1500, 128, B16, 5, "plain") * 8, R.tokens(1, 1, 1500, 128, B16, 6, "plain")
+    ref.append(k, v)
+    A.akb_append(c, k.to(DEV), v.to(DEV))
+    q = R.tokens(1, 1, n, 128, B16, 7, "plain") * 16
+    want, eps, mag = ref.attention(q, accumulate=True)
+    R.assert_attention(A.akb_attention(c, q.to(DEV), accumulate=True), want, eps, mag, B16, f"n {n}")
+    got, add = c.score.double().cpu().numpy()[:1500], ref.score[0][0]
+    assert (np.abs(got - add) <= eps.max() * add + n * 2.0 ** -23).all() and abs(got.sum() - n) <= eps.max() * n + 1500 * n * 2.0 ** -23
 
 
 def test_offsets_beyond_32_bits(A):
