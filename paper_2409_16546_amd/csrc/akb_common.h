@@ -49,6 +49,7 @@ typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+typedef short s16x2_t __attribute__((ext_vector_type(2)));
 typedef float f32x2_t __attribute__((ext_vector_type(2)));
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 
@@ -68,6 +69,8 @@ struct Fp16 {
     __device__ static __forceinline__ uint32_t from_float(float f) { return __builtin_bit_cast(uint16_t, (_Float16)f); }
     template <bool HI> __device__ static __forceinline__ uint32_t cvt2(uint32_t w, float s) { return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, s, HI)); }
     __device__ static __forceinline__ uint32_t pack(float a, float b) { return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t{a, b}), f16x2_t)); }
+    // two numbers over a power of two, to the nearest e4m3 numbers, in the low or the high half of a word
+    template <bool HI> __device__ static __forceinline__ uint32_t code2(uint32_t old, uint32_t w, float s) { return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_fp8_f16(__builtin_bit_cast(s16x2_t, old), __builtin_bit_cast(f16x2_t, w), s, HI)); }
     __device__ static __forceinline__ float lo(uint32_t w) { return (float)__builtin_bit_cast(f16x2_t, w).x; }
     __device__ static __forceinline__ float hi(uint32_t w) { return (float)__builtin_bit_cast(f16x2_t, w).y; }
     __device__ static __forceinline__ f32x4_t mfma16(u32x4_t a, u32x4_t b, f32x4_t c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(x8, a), __builtin_bit_cast(x8, b), c, 0, 0, 0); }
@@ -81,6 +84,7 @@ struct Bf16 {
     __device__ static __forceinline__ uint32_t from_float(float f) { return __builtin_bit_cast(uint16_t, (__bf16)f); }
     template <bool HI> __device__ static __forceinline__ uint32_t cvt2(uint32_t w, float s) { return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, s, HI)); }
     __device__ static __forceinline__ uint32_t pack(float a, float b) { return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t{a, b}), bf16x2_t)); }
+    template <bool HI> __device__ static __forceinline__ uint32_t code2(uint32_t old, uint32_t w, float s) { return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(__builtin_bit_cast(s16x2_t, old), __builtin_bit_cast(bf16x2_t, w), s, HI)); }
     __device__ static __forceinline__ float lo(uint32_t w) { return bits_float(w << 16); }
     __device__ static __forceinline__ float hi(uint32_t w) { return bits_float(w & 0xFFFF0000u); }
     __device__ static __forceinline__ f32x4_t mfma16(u32x4_t a, u32x4_t b, f32x4_t c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(x8, a), __builtin_bit_cast(x8, b), c, 0, 0, 0); }

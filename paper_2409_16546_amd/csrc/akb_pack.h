@@ -24,34 +24,71 @@ __device__ __forceinline__ void pack_block(const akb_cache& c, size_t block, boo
     constexpr int kStride = PackLds<D>::kStride;
     const int tid = threadIdx.x;
     const BlockLane<D> at(tid);
-    uint32_t mx = 0;
+    auto over_workgroup = [&](uint32_t mx) {
+        mx = akv::wave_max_int(int(mx));
+        if ((tid & 63) == 0) lds.max[tid >> 6] = mx;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < 2 * D / 64; ++w) mx = max(mx, lds.max[w]);
+        return mx;
+    };
+    uint32_t two = 0;   // magnitudes of the even and the odd channels
 #pragma unroll
     for (int r = 0; r < 4; ++r)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) mx = max(mx, max(finite_mag<T>(x[r][i] & 0xFFFFu), finite_mag<T>(x[r][i] >> 16)));
-    mx = akv::wave_max_int(int(mx));
-    if ((tid & 63) == 0) lds.max[tid >> 6] = mx;
-    __syncthreads();
+        for (int i = 0; i < 4; ++i) two = akv::max_halves(two, x[r][i] & 0x7FFF7FFFu);
+    uint32_t mx = over_workgroup(max(two & 0xFFFFu, two >> 16));
+    const bool finite = mx < T::kInf;
+    if (!finite) {   // infinities and NaN do not count
+        mx = 0;
 #pragma unroll
-    for (int w = 0; w < 2 * D / 64; ++w) mx = max(mx, lds.max[w]);
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) mx = max(mx, max(finite_mag<T>(x[r][i] & 0xFFFFu), finite_mag<T>(x[r][i] >> 16)));
+        __syncthreads();   // lds.max is written again
+        mx = over_workgroup(mx);
+    }
     const int e = scale_exponent(T::to_float(mx));
-    const float inv = pow2(-e), most = most_code<T>(e);
-    float y[4][8];
+    const float scale = pow2(e);
+    uint32_t code[8];   // K: two words of each token; V: a word of each channel
+    if (finite && e < T::kTopExp) {   // |x| <= 448 2^e: two numbers are one instruction
 #pragma unroll
-    for (int r = 0; r < 4; ++r)
+        for (int r = 0; r < 4; ++r)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            y[r][2 * i] = to_code<T>(T::lo(x[r][i]), inv, most);
-            y[r][2 * i + 1] = to_code<T>(T::hi(x[r][i]), inv, most);
-        }
+            for (int i = 0; i < 2; ++i) {
+                if (!is_v) {
+                    code[2 * r + i] = T::template code2<true>(T::template code2<false>(0, x[r][2 * i], scale), x[r][2 * i + 1], scale);
+                } else {
+                    const int ch = 2 * r + i;
+                    const uint32_t sel = ch & 1 ? 0x07060302u : 0x05040100u;   // this channel of two tokens
+                    code[ch] = T::template code2<true>(T::template code2<false>(0, __builtin_amdgcn_perm(x[1][ch >> 1], x[0][ch >> 1], sel), scale),
+                                                       __builtin_amdgcn_perm(x[3][ch >> 1], x[2][ch >> 1], sel), scale);
+                }
+            }
+    } else {
+        const float inv = pow2(-e), most = most_code<T>(e);
+        float y[4][8];
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                y[r][2 * i] = to_code<T>(T::lo(x[r][i]), inv, most);
+                y[r][2 * i + 1] = to_code<T>(T::hi(x[r][i]), inv, most);
+            }
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                code[2 * r + i] = is_v ? pack_codes(y[0][2 * r + i], y[1][2 * r + i], y[2][2 * r + i], y[3][2 * r + i])
+                                       : pack_codes(y[r][4 * i], y[r][4 * i + 1], y[r][4 * i + 2], y[r][4 * i + 3]);
+    }
     if (!is_v) {
 #pragma unroll
         for (int r = 0; r < 4; ++r)
-            __builtin_nontemporal_store((u32x2_t{pack_codes(y[r][0], y[r][1], y[r][2], y[r][3]), pack_codes(y[r][4], y[r][5], y[r][6], y[r][7])}),
-                                        reinterpret_cast<u32x2_t*>(c.k8 + block * (kTB * D) + k_place<D>(at.t0 + r, at.oct * 8)));
+            __builtin_nontemporal_store((u32x2_t{code[2 * r], code[2 * r + 1]}), reinterpret_cast<u32x2_t*>(c.k8 + block * (kTB * D) + k_place<D>(at.t0 + r, at.oct * 8)));
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) lds.codes[(at.oct * 8 + i) * kStride + at.grp] = pack_codes(y[0][i], y[1][i], y[2][i], y[3][i]);
+        for (int i = 0; i < 8; ++i) lds.codes[(at.oct * 8 + i) * kStride + at.grp] = code[i];
         __syncthreads();
         for (int p = tid; p < D * 4; p += 2 * D) {   // 16-byte pieces
             const uint32_t* s = lds.codes + (p >> 2) * kStride + (p & 3) * 4;
