@@ -51,8 +51,21 @@ struct Cut {
     unsigned w;        // this workgroup's number among those that have work
     int b, splits;     // its sequence, the parts of its walks
     unsigned first;    // the sequence's first workgroup
-    // An XCD has one stretch of the work, so that the row groups and parts of a (sequence, KV head) share its L2 (workgroups are dealt to the XCDs in turn):
-    // false where none is left.
+    // Workgroups are dealt to the XCDs in turn.  All row groups and parts of a (sequence, KV head) go to one XCD, whose L2 they share, every eighth pair to the same;
+    // where the pairs are no multiple of the XCDs the work is dealt as it comes.  With one stretch of the pairs per XCD, long sequences, or a prompt's late rows,
+    // fall to few XCDs.  Stretch / dealt, us: 16 x 8 pairs 300 query tokens, ragged 126.7 / 97.5; a prompt of 8192 tokens on 2 pairs with scores 746 / 588; 4 x 8 ragged
+    // prompts of 4096 244 / 197; 8 x 32 ragged pairs of 4300 tokens 40.4 / 35.0; 16 x 32 of 8192 161.0 / 158.1, ragged 118 / 114; but 2 x 32 chunks of 777 onto
+    // 20000 290 / 320, and 12 pairs' prompts 244 / 264.
+    __device__ __forceinline__ bool deal(unsigned pairs, unsigned per_pair)
+    {
+        w = blockIdx.x;
+        if (pairs % akv::kXcds == 0) {
+            const unsigned x = blockIdx.x % akv::kXcds, i = blockIdx.x / akv::kXcds;
+            w = (x + akv::kXcds * (i / per_pair)) * per_pair + i % per_pair;
+        }
+        return blockIdx.x < pairs * per_pair;
+    }
+    // ... of parts of equal length an XCD has one stretch: false where none is left
     __device__ __forceinline__ bool stretch(unsigned n)
     {
         const unsigned per = (n + akv::kXcds - 1) / akv::kXcds, x = blockIdx.x % akv::kXcds, i = blockIdx.x / akv::kXcds;
@@ -65,7 +78,7 @@ struct Cut {
         const int B = a.c.shape.B, walks = a.c.shape.Hkv * a.groups, lane = threadIdx.x & 63;   // walks: per sequence
         splits = a.splits;
         if (splits) {
-            if (!OF && !stretch(unsigned(B) * walks * splits)) return false;
+            if (!OF && !deal(unsigned(B) * a.c.shape.Hkv, unsigned(a.groups) * splits)) return false;
             b = OF ? of : int(w / unsigned(walks * splits));
             first = unsigned(b) * walks * splits;
             return true;
