@@ -558,7 +558,8 @@ class BlockCache:
         return p
 
     def reserve(self, n: int = 1, keep: int = 0) -> "BlockCache":
-        """Make the workspace large enough for attention of up to n query tokens and, where keep > 0, for evictions down to `keep` tokens."""
+        """Make the workspace large enough for attention of up to n query tokens and, where keep > 0, for evictions down to `keep` tokens.  A larger
+        workspace is a new tensor: reserve before a graph is captured."""
         shp = self.struct().shape
         need = lib().akb_attention_workspace(C.byref(shp), n, int(self.score is not None))
         need_evict = lib().akb_evict_workspace(C.byref(shp), keep) if keep > 0 else 1
@@ -576,6 +577,10 @@ def _here(*tensors) -> None:
     dev = torch.cuda.current_device()
     for t in tensors:
         assert t is None or t.get_device() == dev, f"tensors of the current device (cuda:{dev}) only"
+
+
+def _nbytes(t: torch.Tensor | None) -> int:
+    return 0 if t is None else t.numel() * t.element_size()
 
 
 def akb_cache_reset(cache: BlockCache) -> None:
@@ -614,7 +619,7 @@ def akb_attention(cache: BlockCache, q: torch.Tensor, out: torch.Tensor | None =
     ws = cache.workspace if workspace is None else workspace
     _here(cache.k8, q, out, n_q, ws)
     p = cache.params(scale, 0 if out.dtype == torch.float32 else 1, int(accumulate), max_len)
-    _check(lib().akb_attention(cache.ref(), _ptr(q), _ptr(n_q), n, _ptr(out), p, _ptr(ws), ws.numel() * ws.element_size(), _stream()))
+    _check(lib().akb_attention(cache.ref(), _ptr(q), _ptr(n_q), n, _ptr(out), p, _ptr(ws), _nbytes(ws), _stream()))
     return out
 
 
@@ -631,7 +636,7 @@ def akb_evict(src: BlockCache, dst: BlockCache, keep: int, recent: int = 0, *, k
     assert kept is None or (kept.dtype == torch.int32 and tuple(kept.shape) == (src.B, src.Hkv, keep))
     ws = src.workspace if workspace is None else workspace
     _here(src.k8, dst.k8, kept, ws)
-    _check(lib().akb_evict(src.ref(), dst.ref(), keep, recent, _ptr(kept), _ptr(ws), ws.numel() * ws.element_size(), _stream()))
+    _check(lib().akb_evict(src.ref(), dst.ref(), keep, recent, _ptr(kept), _ptr(ws), _nbytes(ws), _stream()))
 
 
 def akb_unpack(cache: BlockCache) -> tuple[torch.Tensor, torch.Tensor]:
