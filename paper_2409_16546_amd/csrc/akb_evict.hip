@@ -352,7 +352,8 @@ __global__ __launch_bounds__(2 * D) void gather_kernel(akb_cache c, akb_cache d,
         for (int r = 0; r < 4; ++r) slot[r] = token[r] % kTB;
         load_tail<D, false>(c, bh, is_v, x, in_tail, slot);
     }
-    if ((blk + 1) * kTB <= count) pack_block<T, D>(d, bh * (d.shape.Ncap / kTB) + blk, is_v, x, lds);
+    // codes stored with the hint: 8 x 32 heads 8192 -> 2048 tokens 126 / 110 us, and with the step that follows 138.6 / 136.8; fewer alike
+    if ((blk + 1) * kTB <= count) pack_block<T, D, true>(d, bh * (d.shape.Ncap / kTB) + blk, is_v, x, lds);
     else store_tail<D>(d, bh, is_v, x, stays);
 }
 

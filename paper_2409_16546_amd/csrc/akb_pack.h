@@ -16,9 +16,14 @@ template <int D> struct PackLds {
     uint32_t max[2 * D / 64];
 };
 
+template <bool NT, class V> __device__ __forceinline__ void put(V v, uint8_t* p)
+{
+    if (NT) __builtin_nontemporal_store(v, reinterpret_cast<V*>(p));
+    else *reinterpret_cast<V*>(p) = v;
+}
 // A complete block: maximum over the workgroup, e, codes.  K leaves straight from the registers (8 bytes of a token's 64-channel run), V through LDS,
-// so that its 16-byte pieces are stored by neighbouring lanes.  Non-temporal stores measured 2 to 4 % ahead (8 x 8 pairs of 8192 tokens 76.7 / 75.3 us).
-template <class T, int D>
+// so that its 16-byte pieces are stored by neighbouring lanes.  NT: with the non-temporal hint.
+template <class T, int D, bool NT>
 __device__ __forceinline__ void pack_block(const akb_cache& c, size_t block, bool is_v, const u32x4_t (&x)[4], PackLds<D>& lds)
 {
     constexpr int kStride = PackLds<D>::kStride;
@@ -85,14 +90,14 @@ __device__ __forceinline__ void pack_block(const akb_cache& c, size_t block, boo
     if (!is_v) {
 #pragma unroll
         for (int r = 0; r < 4; ++r)
-            __builtin_nontemporal_store((u32x2_t{code[2 * r], code[2 * r + 1]}), reinterpret_cast<u32x2_t*>(c.k8 + block * (kTB * D) + k_place<D>(at.t0 + r, at.oct * 8)));
+            put<NT>(u32x2_t{code[2 * r], code[2 * r + 1]}, c.k8 + block * (kTB * D) + k_place<D>(at.t0 + r, at.oct * 8));
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i) lds.codes[(at.oct * 8 + i) * kStride + at.grp] = code[i];
         __syncthreads();
         for (int p = tid; p < D * 4; p += 2 * D) {   // 16-byte pieces
             const uint32_t* s = lds.codes + (p >> 2) * kStride + (p & 3) * 4;
-            __builtin_nontemporal_store((u32x4_t{s[0], s[1], s[2], s[3]}), reinterpret_cast<u32x4_t*>(c.v8 + block * (kTB * D) + p * 16));
+            put<NT>(u32x4_t{s[0], s[1], s[2], s[3]}, c.v8 + block * (kTB * D) + p * 16);
         }
     }
     if (tid == 0) c.exps[block * 2 + (is_v ? 1 : 0)] = (int8_t)e;

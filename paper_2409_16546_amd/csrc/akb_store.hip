@@ -51,7 +51,7 @@ __global__ __launch_bounds__(2 * D) void append_kernel(akb_cache c, const uint16
                 load_tail<D, true>(c, bh, is_v, x, old, token);
             }
             if (is_v) __syncthreads();   // K's block has been packed
-            pack_block<T, D>(c, bh * (Ncap / kTB) + first + j, is_v, x, lds);
+            pack_block<T, D, NT>(c, bh * (Ncap / kTB) + first + j, is_v, x, lds);
         }
         if (j == 0 && total % kTB) {   // the incomplete block: its new tokens go to the tail (what of the old ones is needed has been read)
             __syncthreads();
@@ -95,8 +95,8 @@ hipError_t launch_append(const akb_cache& c, const uint16_t* k_new, const uint16
     // between the two launches; 1024 8.8 and 14.6.  (Of one side per workgroup they would be twice as many, and gain nothing: 8 x 8 pairs 8192 tokens 77 us.)
     const bool ticketed = long(grid.x) * grid.y * grid.z <= 640;
     auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(2 * c.shape.D), 0, st, c, k_new, v_new, n_new, n, ticketed ? 1 : 0); };
-    // New tokens that are more than half of the last-level cache are read with the non-temporal hint; fewer may still lie there as they were made.  Plain / with the
-    // hint: 8 x 8 pairs 8192 tokens (268 MB) 75.3 / 68.8 us, 6 x 32 pairs up to 777 tokens (76 MB at most, read again and again) 28.9 / 33.8.
+    // New tokens that are more than half of the last-level cache are read and their codes stored with the non-temporal hint; fewer may still lie there as they were
+    // made, and their codes are wanted there next.  Plain / with the hint: 8 x 8 pairs 8192 tokens (268 MB) 76.7 / 68.8 us, 6 x 32 pairs up to 777 tokens (76 MB at most, read again and again) 28.9 / 33.8.
     const bool streamed = size_t(c.shape.B) * c.shape.Hkv * n * c.shape.D * 4 > (size_t(128) << 20);
     auto pick = [&](auto plain, auto hinted) { streamed ? launch(hinted) : launch(plain); };
     if (c.shape.dtype == AKB_FP16) c.shape.D == 64 ? pick(append_kernel<Fp16, 64, false>, append_kernel<Fp16, 64, true>) : pick(append_kernel<Fp16, 128, false>, append_kernel<Fp16, 128, true>);
