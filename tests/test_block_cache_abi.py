@@ -110,6 +110,9 @@ def test_refusals_come_before_any_launch(A):
     many = A.akb_cache(A.akb_shape(128, 64, 4, 64, 1 << 18, 0), **ADDR)
     refused(attention(c=many, n=1 << 17, size=1 << 50), "2^24")
 
+    assert L.akb_workspace_init(None, 1 << 20, None) == A.AKV_EWORKSPACE and L.akb_workspace_init(WS + 8, 1 << 20, None) == A.AKV_EWORKSPACE
+    assert L.akb_workspace_init(WS, 16, None) == A.AKV_EWORKSPACE
+
     to = {n: a + 0x100000000 for n, a in ADDR.items()}
 
     def evict(src=good, dst=None, keep=100, recent=0, kept=Q, ws=None, size=0, dshape=shape):

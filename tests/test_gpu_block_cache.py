@@ -438,6 +438,46 @@ def test_calls_on_another_stream(A):
     R.assert_attention(out, *ref.attention(q), B16, "stream")
 
 
+@pytest.mark.parametrize("n", [1, 5, 200])
+def test_a_workspace_holds_nothing_but_its_control_words(A, n):
+    """A workspace full of NaN bits, prepared, gives the bits that a fresh one gives; so does the one before it, used by calls of other sizes in between."""
+    c, ref = pair(A, 2, 8, 2, 128, 4096, B16, score=True, n=200)
+    put(A, c, ref, 4000, 1, [4000, 2222])
+    q = R.tokens(2, 8, n, 128, B16, 2, "plain").to(DEV)
+    d, _ = pair(A, 2, 8, 2, 128, 256, B16, score=True)
+    outs = []
+    for turn in range(3):
+        c.score.zero_()
+        if turn == 1:
+            c.reserve(200, 200).workspace.fill_(0xFF)
+            A.akb_workspace_init(c.workspace)
+        out = A.akb_attention(c, q, accumulate=True).clone()
+        outs.append((out, c.score.clone()))
+        A.akb_evict(c.reserve(200, 200), d, 200, 10)                                    # eviction and other attention in the same workspace
+        for other in (1, 3, 64):
+            A.akb_attention(c, R.tokens(2, 8, other, 128, B16, 3, "plain").to(DEV))
+    assert all(torch.equal(a, b) for o in outs[1:] for a, b in zip(o, outs[0]))
+
+
+def test_two_calls_at_once(A):
+    """Two streams, one cache, a workspace each."""
+    c, ref = pair(A, 2, 8, 2, 64, 4096, F16, n=64)
+    put(A, c, ref, 4000, 1, [4000, 3999])
+    qs = [R.tokens(2, 8, n, 64, F16, 2, "plain").to(DEV) for n in (1, 64)]
+    want = [A.akb_attention(c, q).clone() for q in qs]
+    spaces = [torch.empty_like(c.workspace) for _ in qs]
+    for w in spaces:
+        A.akb_workspace_init(w)
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream() for _ in qs], [[] for _ in qs]
+    for _ in range(5):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                got[i].append(A.akb_attention(c, qs[i], workspace=spaces[i]))
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, want[i]) for i in (0, 1) for o in got[i])
+
+
 def test_a_length_set_to_zero_starts_the_sequence_anew(A):
     c, ref = pair(A, 2, 2, 2, 64, 256, F16, score=True)
     put(A, c, ref, 170, 1)
