@@ -7,13 +7,10 @@
 namespace akb {
 
 using akv::align256;
-using akv::fail_msg;
 
 constexpr int kTB = AKB_TB;
 constexpr int kEMin = -100;        // least exponent of a block's scale
 constexpr float kMaxCode = 448.f;  // largest e4m3 number
-
-inline size_t blocks(const akb_shape& s) { return size_t(s.Ncap) / kTB; }
 
 // host launchers, each defined next to its kernels
 hipError_t launch_append(const akb_cache& c, const uint16_t* k_new, const uint16_t* v_new, const int32_t* n_new, int n, hipStream_t st);
@@ -66,7 +63,6 @@ struct Fp16 {
     static constexpr uint32_t kInf = 0x7C00u;
     static constexpr int kTopExp = 8;   // 256 times 2^8 is beyond the type
     __device__ static __forceinline__ float to_float(uint32_t h) { return (float)__builtin_bit_cast(_Float16, (uint16_t)h); }
-    __device__ static __forceinline__ uint32_t from_float(float f) { return __builtin_bit_cast(uint16_t, (_Float16)f); }
     template <bool HI> __device__ static __forceinline__ uint32_t cvt2(uint32_t w, float s) { return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, s, HI)); }
     __device__ static __forceinline__ uint32_t pack(float a, float b) { return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t{a, b}), f16x2_t)); }
     // two numbers over a power of two, to the nearest e4m3 numbers, in the low or the high half of a word
@@ -81,7 +77,6 @@ struct Bf16 {
     static constexpr uint32_t kInf = 0x7F80u;
     static constexpr int kTopExp = 120;
     __device__ static __forceinline__ float to_float(uint32_t h) { return bits_float(h << 16); }
-    __device__ static __forceinline__ uint32_t from_float(float f) { return __builtin_bit_cast(uint16_t, (__bf16)f); }
     template <bool HI> __device__ static __forceinline__ uint32_t cvt2(uint32_t w, float s) { return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, s, HI)); }
     __device__ static __forceinline__ uint32_t pack(float a, float b) { return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t{a, b}), bf16x2_t)); }
     template <bool HI> __device__ static __forceinline__ uint32_t code2(uint32_t old, uint32_t w, float s) { return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(__builtin_bit_cast(s16x2_t, old), __builtin_bit_cast(bf16x2_t, w), s, HI)); }
@@ -105,7 +100,7 @@ __device__ __forceinline__ int scale_exponent(float amax)
     return max(int(u >> 23) - 127 - 8 + ((u & 0x7FFFFFu) > 0x600000u ? 1 : 0), kEMin);
 }
 // x 2^-e as the conversion to e4m3 takes it: within +-448 (+-240 where the code above would stand for a number beyond the type), NaN for what is not finite
-template <class T> __device__ __forceinline__ float to_code(float x, float inv, float most)
+__device__ __forceinline__ float to_code(float x, float inv, float most)
 {
     const float y = x * inv;
     return fabsf(x) < __builtin_inff() ? fminf(fmaxf(y, -most), most) : __builtin_nanf("");

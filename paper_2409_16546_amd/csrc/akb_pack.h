@@ -77,8 +77,8 @@ __device__ __forceinline__ void pack_block(const akb_cache& c, size_t block, boo
         for (int r = 0; r < 4; ++r)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                y[r][2 * i] = to_code<T>(T::lo(x[r][i]), inv, most);
-                y[r][2 * i + 1] = to_code<T>(T::hi(x[r][i]), inv, most);
+                y[r][2 * i] = to_code(T::lo(x[r][i]), inv, most);
+                y[r][2 * i + 1] = to_code(T::hi(x[r][i]), inv, most);
             }
 #pragma unroll
         for (int r = 0; r < 4; ++r)
