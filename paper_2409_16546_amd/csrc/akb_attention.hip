@@ -83,7 +83,7 @@ template <bool NT> __device__ __forceinline__ u32x4_t load_codes(const uint8_t* 
 }
 template <int D, bool NT> struct KCodes {
     u32x4_t w[4][D / 64];
-    float s;
+    uint32_t e;   // exponents of the block's K and of its V (the scales are made where they are used: made here, the load would be waited for here)
     __device__ __forceinline__ void load(const akb_cache& c, size_t block, int lane)
     {
         const uint8_t* p = c.k8 + block * (kTB * D) + (lane & 15) * 64 + (lane >> 4) * 16;
@@ -91,18 +91,16 @@ template <int D, bool NT> struct KCodes {
         for (int t = 0; t < 4; ++t)
 #pragma unroll
             for (int i = 0; i < D / 64; ++i) w[t][i] = load_codes<NT>(p + t * (16 * D) + i * 1024);
-        s = pow2(c.exps[block * 2]);
+        e = *reinterpret_cast<const uint16_t*>(c.exps + block * 2);
     }
 };
 template <int D, bool NT> struct VCodes {
     u32x4_t w[D / 16];
-    float s;
     __device__ __forceinline__ void load(const akb_cache& c, size_t block, int lane)
     {
         const uint8_t* p = c.v8 + block * (kTB * D) + (lane & 15) * 64 + (lane >> 4) * 16;
 #pragma unroll
         for (int i = 0; i < D / 16; ++i) w[i] = load_codes<NT>(p + i * 1024);
-        s = pow2(c.exps[block * 2 + 1]);
     }
 };
 
@@ -128,8 +126,8 @@ template <class T, int D> struct RowState {
         z = 0.f;
         limit = lim;
     }
-    // S^T of 64 tokens -> weights; ph[u]: tokens 32 u .. + 31 as the operand of the second product, pl: what 16 bits lack of them
-    template <bool EXACT> __device__ __forceinline__ void weights(f32x4_t (&s)[4], int first, bool masked, float c2, int lane, u32x4_t (&ph)[2], u32x4_t (&pl)[2])
+    // S^T of 64 tokens -> weights (unit: the bits of the largest); ph[u]: tokens 32 u .. + 31 as the operand of the second product, pl: what 16 bits lack of them
+    template <bool EXACT> __device__ __forceinline__ void weights(f32x4_t (&s)[4], int first, bool masked, float c2, float unit, int lane, u32x4_t (&ph)[2], u32x4_t (&pl)[2])
     {
         float mx = -__builtin_inff();
         const int seen = limit - first - 4 * (lane >> 4);   // counted from the lane's first token
@@ -141,7 +139,7 @@ template <class T, int D> struct RowState {
                 mx = fmaxf(mx, s[t][r]);
             }
         mx = max_lane32(max_lane16(mx));
-        const float now = fmaf(mx, c2, -kWeightBits);
+        const float now = fmaf(mx, c2, -unit);
         if (__any(now > m + kSlackBits)) {
             const float up = fmaxf(m, now), a = __builtin_amdgcn_exp2f(m - (up == -__builtin_inff() ? 0.f : up));
             z *= a;
@@ -222,6 +220,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void rows_kernel(RowArgs a)
     for (; blk < whole; blk += kWaves) {
         VCodes<D, NT> vc;
         vc.load(c, block0 + blk, lane);
+        const float k_scale = pow2(int8_t(kc.e)), v_scale = pow2(int8_t(kc.e >> 8)), unit = weight_bits<T>(v_scale >= pow2(kLargeExp));
         f32x4_t s[RT][4];
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
@@ -229,7 +228,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void rows_kernel(RowArgs a)
             for (int k = 0; k < RT; ++k) s[k][t] = f32x4_t{0, 0, 0, 0};
 #pragma unroll
             for (int i = 0; i < D / 32; ++i) {
-                const u32x4_t x = cvt8<T>(kc.w[t][i >> 1][2 * (i & 1)], kc.w[t][i >> 1][2 * (i & 1) + 1], kc.s);
+                const u32x4_t x = cvt8<T>(kc.w[t][i >> 1][2 * (i & 1)], kc.w[t][i >> 1][2 * (i & 1) + 1], k_scale);
 #pragma unroll
                 for (int k = 0; k < RT; ++k) s[k][t] = T::mfma16(x, st[k].q[i], s[k][t]);
             }
@@ -239,12 +238,12 @@ __global__ __launch_bounds__(64 * kWaves, 2) void rows_kernel(RowArgs a)
         const bool masked = (blk + 1) * kTB > all_see;
         u32x4_t ph[RT][2], pl[RT][2];
 #pragma unroll
-        for (int k = 0; k < RT; ++k) st[k].template weights<EXACT>(s[k], blk * kTB, masked, a.c2, lane, ph[k], pl[k]);
+        for (int k = 0; k < RT; ++k) st[k].template weights<EXACT>(s[k], blk * kTB, masked, a.c2, unit, lane, ph[k], pl[k]);
 #pragma unroll
         for (int i = 0; i < D / 16; ++i)
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
-                const u32x4_t v = cvt8<T>(vc.w[i][2 * u], vc.w[i][2 * u + 1], vc.s);
+                const u32x4_t v = cvt8<T>(vc.w[i][2 * u], vc.w[i][2 * u + 1], v_scale);
 #pragma unroll
                 for (int k = 0; k < RT; ++k) {
                     st[k].o[i] = T::mfma16(v, ph[k][u], st[k].o[i]);
@@ -255,6 +254,11 @@ __global__ __launch_bounds__(64 * kWaves, 2) void rows_kernel(RowArgs a)
     if (blk < hi) {   // the incomplete block, in 16 bits
         const uint16_t *kt = c.k_tail + bh * kTB * D, *vt = c.v_tail + bh * kTB * D;
         const int g = lane >> 4, left = len - blk * kTB;
+        u32x4_t v[D / 16][2];
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+            for (int u = 0; u < 2; ++u) v[i][u] = *reinterpret_cast<const u32x4_t*>(vt + (16 * i + (lane & 15)) * kTB + 16 * g + 8 * u);
         f32x4_t s[RT][4] = {};
 #pragma unroll
         for (int t = 0; t < 4; ++t)
@@ -265,25 +269,32 @@ __global__ __launch_bounds__(64 * kWaves, 2) void rows_kernel(RowArgs a)
                 for (int k = 0; k < RT; ++k) s[k][t] = T::mfma16(x, st[k].q[i], s[k][t]);
             }
         if (RT == 1 && logits) store_logits(logits + size_t(blk) * kTB * rows, s[0], rows, lane & 15, lane);
+        uint32_t large = 0;
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {   // what lies behind the length may be anything: zero, so that a weight of zero makes zero of it
+                const int t = 16 * (2 * u + (e >> 1)) + 4 * g + 2 * (e & 1);
+                const uint32_t stored = t + 1 < left ? 0xFFFFFFFFu : (t < left ? 0xFFFFu : 0u);
+#pragma unroll
+                for (int i = 0; i < D / 16; ++i) {
+                    v[i][u][e] &= stored;
+                    if (T::kWide) large |= large_values(v[i][u][e]);
+                }
+            }
+        const float unit = weight_bits<T>(__any(large & kLargeValues));
         u32x4_t ph[RT][2], pl[RT][2];
 #pragma unroll
-        for (int k = 0; k < RT; ++k) st[k].template weights<EXACT>(s[k], blk * kTB, true, a.c2, lane, ph[k], pl[k]);
+        for (int k = 0; k < RT; ++k) st[k].template weights<EXACT>(s[k], blk * kTB, true, a.c2, unit, lane, ph[k], pl[k]);
 #pragma unroll
         for (int i = 0; i < D / 16; ++i)
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                u32x4_t v = *reinterpret_cast<const u32x4_t*>(vt + (16 * i + (lane & 15)) * kTB + 16 * g + 8 * u);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {   // what lies behind the length may be anything: zero, so that a weight of zero makes zero of it
-                    const int t = 16 * (2 * u + (e >> 1)) + 4 * g + 2 * (e & 1);
-                    v[e] = t + 1 < left ? v[e] : (t < left ? v[e] & 0xFFFFu : 0u);
-                }
+            for (int u = 0; u < 2; ++u)
 #pragma unroll
                 for (int k = 0; k < RT; ++k) {
-                    st[k].o[i] = T::mfma16(v, ph[k][u], st[k].o[i]);
-                    if (EXACT) st[k].o[i] = T::mfma16(v, pl[k][u], st[k].o[i]);
+                    st[k].o[i] = T::mfma16(v[i][u], ph[k][u], st[k].o[i]);
+                    if (EXACT) st[k].o[i] = T::mfma16(v[i][u], pl[k][u], st[k].o[i]);
                 }
-            }
     }
     const int part = part_floats(rows, D);
     const __amdgpu_buffer_rsrc_t parts = akv::make_rsrc(a.parts + size_t(w - split) * part_floats(min(n * G, kRows), D), uint32_t(splits) * part * 4u);

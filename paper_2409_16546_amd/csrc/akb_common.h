@@ -62,6 +62,7 @@ struct Fp16 {
     using x8 = f16x8_t;
     static constexpr uint32_t kInf = 0x7C00u;
     static constexpr int kTopExp = 8;   // 256 times 2^8 is beyond the type
+    static constexpr bool kWide = false;   // numbers as far apart as those of binary32
     __device__ static __forceinline__ float to_float(uint32_t h) { return (float)__builtin_bit_cast(_Float16, (uint16_t)h); }
     template <bool HI> __device__ static __forceinline__ uint32_t cvt2(uint32_t w, float s) { return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, s, HI)); }
     __device__ static __forceinline__ uint32_t pack(float a, float b) { return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t{a, b}), f16x2_t)); }
@@ -76,6 +77,7 @@ struct Bf16 {
     using x8 = bf16x8_t;
     static constexpr uint32_t kInf = 0x7F80u;
     static constexpr int kTopExp = 120;
+    static constexpr bool kWide = true;
     __device__ static __forceinline__ float to_float(uint32_t h) { return bits_float(h << 16); }
     template <bool HI> __device__ static __forceinline__ uint32_t cvt2(uint32_t w, float s) { return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, s, HI)); }
     __device__ static __forceinline__ uint32_t pack(float a, float b) { return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t{a, b}), bf16x2_t)); }

@@ -72,6 +72,21 @@ template <class T, int D> struct Stage {
             reinterpret_cast<u32x2_t*>(&to.x[ch >> 5][t][(ch & 31) + 32 * (g & 1)])[g >> 1] = w;
         }
     }
+    // whether the incomplete block's V has large values (in this thread's share of it)
+    __device__ __forceinline__ static bool large_tail(const uint16_t* tail, int left, int tid)
+    {
+        uint32_t large = 0;
+#pragma unroll
+        for (int p = tid; p < D * 8; p += 64 * kWaves) {           // tokens 32 (p % 2) + 4 g .. + 3 and 16 further of a channel, g = p / 2 % 4
+            const u32x4_t w = *reinterpret_cast<const u32x4_t*>(tail + p * 8);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int token = 32 * (p & 1) + 16 * (e >> 1) + 4 * (p >> 1 & 3) + 2 * (e & 1);
+                large |= large_values(w[e] & (token + 1 < left ? 0xFFFFFFFFu : (token < left ? 0xFFFFu : 0u)));
+            }
+        }
+        return large & kLargeValues;
+    }
 };
 
 template <class T, int D, bool EXACT>
@@ -79,6 +94,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prompt_kernel(RowArgs a)
 {
     __shared__ KLds<D> k_s[2];
     __shared__ VLds<D> v_s[2];
+    __shared__ bool large_s[kWaves];
     const akb_cache& c = a.c;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
     Cut cut;
@@ -139,6 +155,15 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prompt_kernel(RowArgs a)
     fetch_v(lo);
     put_k(lo, k_s[0]);
     fetch_k(lo + 1);
+    float unit = kWeightBits;
+    if (T::kWide) {   // one unit for the walk: found out here, it costs the loop a scalar register (followed from block to block, 560 us of the prompt above for 541)
+        bool some = hi > whole && Stage<T, D>::large_tail(v_tail, len - whole * kTB, threadIdx.x);
+        for (int blk = lo + int(threadIdx.x); blk < min(hi, whole); blk += 64 * kWaves) some |= c.exps[(block0 + blk) * 2 + 1] >= kLargeExp;
+        some = __any(some);
+        if (lane == 0) large_s[wave] = some;
+        lds_barrier();
+        unit = weight_bits<T>(__builtin_amdgcn_readfirstlane(large_s[0] | large_s[1] | large_s[2] | large_s[3]));
+    }
     put_v(lo, v_s[0]);
     put_k(lo + 1, k_s[1]);
     lds_barrier();
@@ -166,7 +191,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prompt_kernel(RowArgs a)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[t][r]);
             mx = max_lane32(mx);
-            const float now = fmaf(mx, a.c2, -kWeightBits);
+            const float now = fmaf(mx, a.c2, -unit);
             if (__any(now > top + kSlackBits)) {
                 const float up = fmaxf(top, now), f = __builtin_amdgcn_exp2f(top - (up == -__builtin_inff() ? 0.f : up));
                 z *= f;

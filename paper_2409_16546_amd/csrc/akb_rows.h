@@ -14,6 +14,12 @@ namespace akb {
 // In 16 bits the weights of fp16 caches lose bits below 2^-14, and end at 2^16.  They are taken relative to 2^-7 of a maximum that is moved only when a score
 // lies 2^8 above it (then up to 2^15): O and the sum are multiplied anew in few blocks instead of in every other one.
 constexpr float kWeightBits = 7.f, kSlackBits = 8.f;
+// bfloat16 values reach as far as binary32 does: a token of weight 2^7 and value 2^121 would be beyond O.  The tokens of blocks whose values pass 2^71, and of tails whose
+// values pass 2^65 (in the prompt kernel: of parts of a walk that hold such a one), have weights relative to 2^31 of their maximum: 2^22 of them, 2^(8 - 31) each, sum
+// up to half of the largest value, and the others, 2^15 each, up to 2^109.  Only they: at this unit values below 2^-95 would lose bits, and the exponentials'
+// arguments carry 2^-20 where the others' carry 2^-22.
+constexpr float kSmallWeightBits = -31.f;
+constexpr int kLargeExp = 64;       // least exponent of a block whose values pass 2^71 (448 2^63)
 constexpr int kWaves = 4;           // of a workgroup
 constexpr int kPromptRows = 128;    // of a row group of the prompt kernel
 // What one split of a row group leaves for the workgroup that joins them: per row (maximum, sum), padded to 16 bytes, then O [row][D]
@@ -35,6 +41,12 @@ struct RowArgs {
 };
 
 #if defined(__HIPCC__)
+// the unit of the weights
+template <class T> __device__ __forceinline__ float weight_bits(bool large) { return T::kWide && large ? kSmallWeightBits : kWeightBits; }
+// bits 14 and 30 of what this gives: the two numbers are 2^65 or more (their exponents begin with two ones)
+__device__ __forceinline__ uint32_t large_values(uint32_t w) { return w & (w << 1); }
+constexpr uint32_t kLargeValues = 0x40004000u;
+
 // the query token of a row, row / G: exact below 2^28 rows (there are at most 2^22 tokens of 16 rows)
 __device__ __forceinline__ int row_token(const RowArgs& a, int row) { return a.inv_g ? int(__umulhi(uint32_t(row), a.inv_g)) : row; }
 // the place of a row in q and out, [sequence][query head][n][D]; first: the pair's, of which G n rows follow
