@@ -127,6 +127,10 @@ akv_status akb_attention(const akb_cache *cache, const uint16_t *q, const int32_
  * callers that attribute time to kernels. */
 int32_t akb_attention_path(const akb_shape *shape, int32_t n, int32_t max_len, int32_t *parts);
 
+/* How the parts of that call are put together: 1 = every walk is one part, 2 = by the last workgroup of a row group, 3 = by a launch behind.  Host computation; 0
+ * on a bad shape. */
+int32_t akb_attention_join(const akb_shape *shape, int32_t n, int32_t max_len);
+
 /*
  * Evict: src's tokens (their values as they are read, their scores) go to dst, at most `keep` of each (sequence, KV head):
  * the min(recent, kept) last ones and, of the others, those of the largest score.  A NaN counts as the largest.  dst has src's

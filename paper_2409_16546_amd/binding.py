@@ -28,7 +28,7 @@ EXPORTS = ["akv_version", "akv_last_error", "akv_layout_sizes", "akv_cache_reset
            "akv_fp16_path", "akv_stream_read",
            "akw_layout_sizes", "akw_workspace_init", "akw_pack", "akw_unpack", "akw_gemv"]
 AKW_MAX_B = 4
-AKB_EXPORTS = ["akb_layout_sizes", "akb_cache_reset", "akb_append", "akb_attention_workspace", "akb_workspace_init", "akb_attention_path", "akb_attention", "akb_evict_workspace", "akb_evict",
+AKB_EXPORTS = ["akb_layout_sizes", "akb_cache_reset", "akb_append", "akb_attention_workspace", "akb_workspace_init", "akb_attention_path", "akb_attention_join", "akb_attention", "akb_evict_workspace", "akb_evict",
                "akb_unpack"]
 AKB_TB, AKB_MAX_G = 64, 16
 AKB_DTYPES = {torch.float16: 0, torch.bfloat16: 1}
@@ -162,6 +162,8 @@ def lib() -> C.CDLL:
         L.akb_workspace_init.argtypes = [C.c_void_p, C.c_size_t, C.c_void_p]
         L.akb_attention_path.restype = C.c_int32
         L.akb_attention_path.argtypes = [C.POINTER(akb_shape), C.c_int32, C.c_int32, C.POINTER(C.c_int32)]
+        L.akb_attention_join.restype = C.c_int32
+        L.akb_attention_join.argtypes = [C.POINTER(akb_shape), C.c_int32, C.c_int32]
         L.akb_attention.restype = C.c_int
         L.akb_attention.argtypes = [C.POINTER(akb_cache), C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.POINTER(akb_params), C.c_void_p, C.c_size_t,
                                     C.c_void_p]
@@ -627,6 +629,11 @@ def akb_attention_path(B: int, Hq: int, Hkv: int, D: int, Ncap: int, n: int = 1,
     """(1, 2 or 3: row groups of 16, 32, 128 rows; parts of a walk over the blocks, 0: cut by the device): what akb_attention takes."""
     shp, parts = akb_shape(B, Hq, Hkv, D, Ncap, 0), C.c_int32(0)
     return int(lib().akb_attention_path(C.byref(shp), n, max_len, C.byref(parts))), parts.value
+
+
+def akb_attention_join(B: int, Hq: int, Hkv: int, D: int, Ncap: int, n: int = 1, max_len: int = 0) -> int:
+    """How akb_attention puts the parts together: 1 nothing to do, 2 the last workgroup of a row group, 3 a launch behind."""
+    return int(lib().akb_attention_join(C.byref(akb_shape(B, Hq, Hkv, D, Ncap, 0)), n, max_len))
 
 
 def akb_evict(src: BlockCache, dst: BlockCache, keep: int, recent: int = 0, *, kept: torch.Tensor | None = None,

@@ -132,6 +132,12 @@ int32_t akb_attention_path(const akb_shape* shape, int32_t n, int32_t max_len, i
     return akb::attention_path(*shape, n, max_len > 0 ? max_len : shape->Ncap, parts);
 }
 
+int32_t akb_attention_join(const akb_shape* shape, int32_t n, int32_t max_len)
+{
+    if (!shape || !shape_ok(*shape) || n < 1 || n > shape->Ncap || max_len < 0 || max_len > shape->Ncap) return 0;
+    return akb::attention_join(*shape, n, max_len > 0 ? max_len : shape->Ncap);
+}
+
 size_t akb_evict_workspace(const akb_shape* shape, int32_t keep)
 {
     if (!shape || !shape_ok(*shape) || keep < 1) {

@@ -72,6 +72,11 @@ int attention_path(const akb_shape& s, int n, int max_len, int32_t* parts)
     if (parts) *parts = p.splits;
     return p.tiles <= 2 ? p.tiles : 3;
 }
+int attention_join(const akb_shape& s, int n, int max_len)
+{
+    const AttentionPlan p = plan(s, n, max_len, false);
+    return p.splits == 1 ? 1 : (p.ticketed ? 2 : 3);
+}
 size_t attention_tickets() { return size_t(4) * akv::compute_units() * sizeof(int32_t); }
 
 // A block of K or V as the matrix instructions take it: lane (token t % 16 or channel % 16, quarter): 16 codes

@@ -33,6 +33,7 @@ struct AttentionArgs {
 size_t attention_workspace(const akb_shape& s, int n, bool accumulate);
 size_t attention_tickets();   // bytes at the front of a workspace that are zero between calls
 int attention_path(const akb_shape& s, int n, int max_len, int32_t* parts);   // akb_attention_path
+int attention_join(const akb_shape& s, int n, int max_len);                    // akb_attention_join
 hipError_t launch_attention(const AttentionArgs& a, hipStream_t st);
 
 #if defined(__HIPCC__)

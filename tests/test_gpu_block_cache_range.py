@@ -46,7 +46,7 @@ def check(c, q, out, K, V, lens, n_q=None, start=None, tiny=0.0):
             assert not bad.any(), (b, h, bad.nonzero()[:3].tolist(), got[bad][:3].tolist(), want[bad][:3].tolist(), bound[bad][:3].tolist())
             if start is not None:
                 now, was = c.score.view(B, c.Hkv, -1)[b, h].double(), start.view(B, c.Hkv, -1)[b, h].double()
-                add, rel = p.sum(dim=0), float(eps.max())
+                add, rel = p.sum(dim=0), float(eps.max()) if m else 0.0
                 assert ((now[:L] - was[:L] - add).abs() <= rel * add + (G * m / 16 + 32) * 2.0 ** -23 * (1 + add)).all(), (b, h)
                 assert (now[L:] == was[L:]).all()
 
