@@ -417,23 +417,24 @@ hipError_t launch_unpack(const akv_cache& c, uint16_t* k_out, uint16_t* v_out, h
     return hipGetLastError();
 }
 
-// zero a buffer with 16-byte stores (a kernel rather than a memset node, so that a caller may capture it)
-__global__ __launch_bounds__(256) void zero_kernel(uint4* __restrict__ p16, size_t n16, uint8_t* __restrict__ tail,
-                                                   int ntail)
+// zero a buffer with 16-byte stores, bytes up to the first 16-byte boundary and behind the last (a kernel rather than a memset node, so that a caller may capture it)
+__global__ __launch_bounds__(256) void zero_kernel(uint8_t* __restrict__ p, int head, size_t n16, int tail)
 {
     const size_t stride = size_t(gridDim.x) * 256;
+    uint4* p16 = reinterpret_cast<uint4*>(p + head);
     for (size_t i = size_t(blockIdx.x) * 256 + threadIdx.x; i < n16; i += stride) p16[i] = make_uint4(0, 0, 0, 0);
-    if (blockIdx.x == 0 && (int)threadIdx.x < ntail) tail[threadIdx.x] = 0;
+    if (blockIdx.x == 0 && (int)threadIdx.x < head) p[threadIdx.x] = 0;
+    if (blockIdx.x == 0 && (int)threadIdx.x < tail) p[head + n16 * 16 + threadIdx.x] = 0;
 }
 
 hipError_t launch_zero(void* p, size_t bytes, hipStream_t st)
 {
     if (bytes == 0) return hipSuccess;
-    const size_t n16 = bytes / 16;   // buffers come from an allocator: 16-byte aligned
+    const size_t head = std::min<size_t>((16 - reinterpret_cast<uintptr_t>(p) % 16) % 16, bytes);   // lens and flags may be aligned to 4 bytes only
+    const size_t n16 = (bytes - head) / 16;
     size_t blocks = (n16 + 255) / 256;
     blocks = blocks < 1 ? 1 : (blocks > 8192 ? 8192 : blocks);
-    hipLaunchKernelGGL(zero_kernel, dim3((unsigned)blocks), dim3(256), 0, st, reinterpret_cast<uint4*>(p), n16,
-                       reinterpret_cast<uint8_t*>(p) + n16 * 16, int(bytes - n16 * 16));
+    hipLaunchKernelGGL(zero_kernel, dim3((unsigned)blocks), dim3(256), 0, st, static_cast<uint8_t*>(p), (int)head, n16, int(bytes - head - n16 * 16));
     return hipGetLastError();
 }
 
