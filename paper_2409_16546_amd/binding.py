@@ -516,6 +516,7 @@ class BlockCache:
     _struct: akb_cache = field(repr=False, default=None)
     _ref: object = field(repr=False, default=None)
     _params: dict = field(repr=False, default_factory=dict)
+    _replaced: list = field(repr=False, default_factory=list)
 
     def __post_init__(self):
         sz = akb_layout_sizes(self.B, self.Hq, self.Hkv, self.D, self.Ncap, self.dtype)
@@ -561,7 +562,9 @@ class BlockCache:
 
     def reserve(self, n: int = 1, keep: int = 0) -> "BlockCache":
         """Make the workspace large enough for attention of up to n query tokens and, where keep > 0, for evictions down to `keep` tokens.  A larger
-        workspace is a new tensor: reserve before a graph is captured."""
+        workspace is a new tensor, prepared on the current stream: calls on another stream have to be ordered behind that, as behind anything that makes
+        their tensors, and no graph is captured meanwhile.  The one before is kept as long as the cache, for the calls on other streams and the captured
+        graphs that use it."""
         shp = self.struct().shape
         need = lib().akb_attention_workspace(C.byref(shp), n, int(self.score is not None))
         need_evict = lib().akb_evict_workspace(C.byref(shp), keep) if keep > 0 else 1
@@ -569,6 +572,9 @@ class BlockCache:
             _check(AKV_EINVAL)
         need = max(need, need_evict)
         if self.workspace is None or self.workspace.numel() < need:
+            if self.workspace is not None:   # half as large again: what is kept stays below twice the present one
+                self._replaced.append(self.workspace)
+                need = max(need, (self.workspace.numel() * 3 // 2 + 255) // 256 * 256)
             self.workspace = torch.empty(need, dtype=torch.uint8, device=self.k8.device)
             akb_workspace_init(self.workspace)
         return self

@@ -74,3 +74,23 @@ def test_lens_and_flags_of_the_16_bit_cache_aligned_to_4_bytes(A, skip):
     assert all(torch.equal(getattr(good, n), getattr(c, n)) for n in ("k_hi", "k_mid", "k_lo", "v_hi", "v_mid", "v_lo", "colmax", "lens", "flags"))
     for t in (before, after, fbefore, fafter):
         assert (t == 0x5A5A5A5A).all()
+
+
+# --------------------------------------------------------------------------------------------------------- workspaces
+
+def test_a_replaced_workspace_stays_until_the_cache_goes(A):
+    """Calls on other streams, and captured graphs, may still write the workspace that `reserve` replaces: nobody else gets its memory."""
+    c = A.BlockCache.allocate(2, 8, 2, 128, 1024, F16, score=True)
+    old = [(c.workspace.data_ptr(), c.workspace.numel())]
+    for n in (100, 1000):
+        c.reserve(n)
+        others = [torch.empty(size, dtype=torch.uint8, device=DEV) for _, size in old for _ in range(4)]
+        for x in (*others, c.workspace):
+            for at, size in old:
+                assert x.data_ptr() + x.numel() <= at or at + size <= x.data_ptr()
+        old.append((c.workspace.data_ptr(), c.workspace.numel()))
+        del others
+    before = c.workspace
+    assert c.reserve(5).workspace is before       # large enough: the same one
+    sizes = [size for _, size in old]
+    assert sizes[2] >= 1.5 * sizes[1] >= 2.25 * sizes[0] - 2   # what is kept is never more than twice the present one
