@@ -94,3 +94,82 @@ def test_a_replaced_workspace_stays_until_the_cache_goes(A):
     assert c.reserve(5).workspace is before       # large enough: the same one
     sizes = [size for _, size in old]
     assert sizes[2] >= 1.5 * sizes[1] >= 2.25 * sizes[0] - 2   # what is kept is never more than twice the present one
+
+
+# ------------------------------------------------------------------------------ weights of calls whose bound is too small
+
+@pytest.mark.parametrize("D,B,Hq,Hkv,N,n,max_lens", [
+    (128, 2, 4, 2, 900, 1, (0, 900, 128, 1)),            # up to 16 rows: from q . k as it was left
+    (64, 2, 4, 2, 900, 5, (0, 128, 1)),
+    (128, 2, 4, 2, 900, 60, (0, 128, 1)),                # many rows, one share
+    (64, 2, 4, 2, 900, 400, (0, 640, 1)),                # ... several
+    (128, 4, 32, 8, 3001, 512, (0, 768)),                # the kernel of many rows
+    (128, 1, 2, 1, 20000, 3, (0, 64, 5000)),
+])
+@pytest.mark.parametrize("dtype,out_dtype", [(F16, F32), (B16, B16)], ids=["fp16-f32", "bf16"])
+def test_weights_beyond_the_length_bound(A, D, B, Hq, Hkv, N, n, max_lens, dtype, out_dtype):
+    """max_len is a hint: longer sequences are attended whole, and every token of theirs has its weight added."""
+    from test_gpu_block_cache_range import check
+    g = torch.Generator(device=DEV).manual_seed(N + n)
+    c = A.BlockCache.allocate(B, Hq, Hkv, D, (N + 63) // 64 * 64, dtype, score=True, n=n)
+    lens = [max(1, N - 271 * b) for b in range(B)]
+    n_q = [max(1, n - 7 * b) for b in range(B)]
+    A.akb_append(c, *(torch.randn(B, Hkv, N, D, generator=g, device=DEV).to(dtype) for _ in range(2)), i32(lens))
+    q = torch.randn(B, Hq, n, D, generator=g, device=DEV).to(dtype)
+    start = torch.rand(c.score.shape, generator=g, device=DEV)
+    K, V = A.akb_unpack(c)
+    for max_len in max_lens:
+        print(f"max_len {max_len}: {A.akb_attention_path(B, Hq, Hkv, D, c.Ncap, n, max_len)}", flush=True)
+        c.score.copy_(start)
+        out = A.akb_attention(c, q, torch.full(q.shape, 3.0, dtype=out_dtype, device=DEV), n_q=i32(n_q), accumulate=True, max_len=max_len)
+        check(c, q, out, K, V, lens, n_q, start)
+
+
+# --------------------------------------------------------------------------------------------------- far inside a plane
+
+@pytest.mark.parametrize("dtype", [F16, B16], ids=["fp16", "bf16"])
+def test_long_sequence_in_the_largest_capacity(A, dtype):
+    """70000 tokens in one head of a cache of 2^22: every block's bytes are those of the same tokens in a small cache, every call reads them where they are."""
+    from test_gpu_block_cache_range import check
+    D, N, Ncap = 128, 70000, 1 << 22
+    g = torch.Generator(device=DEV).manual_seed(1)
+    k, v = ((torch.randn(1, 1, N, D, generator=g, device=DEV) * torch.exp2(3 * torch.randn(1, 1, N, 1, generator=g, device=DEV)).clamp(max=1000)).to(dtype) for _ in range(2))
+    c = A.BlockCache.allocate(1, 2, 1, D, Ncap, dtype, score=True, n=200)
+    cuts = [0, 1, 30000, 30001, 69999, N]
+    for a, b in zip(cuts, cuts[1:]):
+        A.akb_append(c, k[:, :, a:b].contiguous(), v[:, :, a:b].contiguous())
+    assert int(c.lens) == N and not c.flags.any()
+    small = A.BlockCache.allocate(1, 2, 1, D, 256, dtype)
+    whole = N // 64
+    k8, v8, exps = c.k8.view(-1, 64 * D), c.v8.view(-1, 64 * D), c.exps.view(-1, 2)
+    for first in (0, 467, 468, 700, whole - 3):      # three blocks at a time; 30000 and 30001 lie in block 468
+        A.akb_cache_reset(small)
+        A.akb_append(small, *(x[:, :, first * 64:first * 64 + 192].contiguous() for x in (k, v)))
+        assert torch.equal(k8[first:first + 3], small.k8.view(-1, 64 * D)[:3]), first
+        assert torch.equal(v8[first:first + 3], small.v8.view(-1, 64 * D)[:3]), first
+        assert torch.equal(exps[first:first + 3], small.exps.view(-1, 2)[:3]), first
+    K, V = A.akb_unpack(c)
+    assert torch.equal(K[:, :, whole * 64:N], k[:, :, whole * 64:]) and torch.equal(V[:, :, whole * 64:N], v[:, :, whole * 64:])
+    assert not K[:, :, N:].any() and not V[:, :, N:].any()
+    K, V = K[:, :, :N].contiguous(), V[:, :, :N].contiguous()
+    for n in (1, 20, 200):
+        q = torch.randn(1, 2, n, D, generator=g, device=DEV).to(dtype)
+        start = torch.rand(c.score.shape, generator=g, device=DEV)
+        c.score.copy_(start)
+        out = A.akb_attention(c, q, accumulate=True)
+        check(c, q, out, K, V, [N], None, start)
+    # eviction: what stays, by the scores as they are now
+    keep, recent = 5000, 100
+    score = c.score[:N].clone()
+    score[1000:2000] = 0.25                          # ties
+    c.score[:N].copy_(score)
+    d = A.BlockCache.allocate(1, 2, 1, D, 5056, dtype, score=True)
+    kept = torch.zeros(1, 1, keep, dtype=torch.int32, device=DEV)
+    A.akb_evict(c.reserve(200, keep), d, keep, recent, kept=kept)
+    order = torch.sort(score[:N - recent], descending=True, stable=True).indices[:keep - recent]
+    want = torch.cat([order.sort().values, torch.arange(N - recent, N, device=DEV)])
+    assert torch.equal(kept.view(-1).long(), want)
+    assert torch.equal(d.score[:keep], score[want]) and int(d.lens) == keep
+    again = A.BlockCache.allocate(1, 2, 1, D, 5056, dtype)   # the kept values, stored anew
+    A.akb_append(again, K[:, :, want].contiguous(), V[:, :, want].contiguous())
+    assert all(torch.equal(a, b) for a, b in zip(A.akb_unpack(d), A.akb_unpack(again)))
