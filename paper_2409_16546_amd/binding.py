@@ -497,7 +497,8 @@ def akb_layout_sizes(B: int, Hq: int, Hkv: int, D: int, Ncap: int, dtype: torch.
 @dataclass
 class BlockCache:
     """Caller-owned device buffers of one block-scaled 8-bit cache (torch owns the memory; include/akb.h has the layout).  The tensors may be given
-    in any shape of the right number of bytes, or be made by ``allocate``."""
+    in any shape of the right number of bytes, or be made by ``allocate``; fields may be assigned later (a score where there was none, other planes), which
+    the next call checks and uses (``reserve`` again behind a new score: its calls want more room)."""
     B: int
     Hq: int
     Hkv: int
@@ -519,6 +520,15 @@ class BlockCache:
     _replaced: list = field(repr=False, default_factory=list)
 
     def __post_init__(self):
+        self._check_buffers()
+
+    def __setattr__(self, name, value):
+        object.__setattr__(self, name, value)
+        if name != "workspace" and name[0] != "_":   # what the struct is made of
+            object.__setattr__(self, "_struct", None)
+            object.__setattr__(self, "_ref", None)
+
+    def _check_buffers(self) -> None:
         sz = akb_layout_sizes(self.B, self.Hq, self.Hkv, self.D, self.Ncap, self.dtype)
         for name, _ in akb_sizes._fields_:
             t = getattr(self, name)
@@ -540,13 +550,14 @@ class BlockCache:
         return c.reserve(n)
 
     def struct(self) -> akb_cache:
-        if self._struct is None:   # the tensors never change after allocation
+        if self._struct is None:
+            self._check_buffers()
             self._struct = akb_cache(akb_shape(self.B, self.Hq, self.Hkv, self.D, self.Ncap, AKB_DTYPES[self.dtype]), _ptr(self.k8), _ptr(self.v8),
                                      _ptr(self.exps), _ptr(self.k_tail), _ptr(self.v_tail), _ptr(self.score), _ptr(self.lens), _ptr(self.flags))
         return self._struct
 
     def ref(self):
-        """The struct by reference, as the calls take it (made once)."""
+        """The struct by reference, as the calls take it (made once, and again when a field has been assigned)."""
         if self._ref is None:
             self._ref = C.byref(self.struct())
         return self._ref
