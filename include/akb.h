@@ -12,14 +12,18 @@
  *             (Where c 2^e would be beyond the 16-bit type, which takes a maximum within 1/16 of the type's largest
  *             number, the next smaller c is taken.)  c 2^e is a number of the 16-bit type: no step of the path rounds
  *             it again.  Powers of two, because a block can then be rebuilt from others (eviction) without its numbers
- *             being rounded anew, save those that fall below the new block's smallest.
+ *             being rounded anew, save those below 2^(e - 6), the smallest normal number of the new block, which keep
+ *             fewer than four bits (none below 2^(e - 10)), and tokens of the tail that come to lie in a complete block,
+ *             which are rounded for the first time.
  *             The tokens of the last, incomplete block are held in 16 bits (the tail) until the block is complete.  So
  *             every block is rounded once, from its own tokens, and the bytes do not depend on how the appends were cut.
  *   attend    Query token i of the n_q[b] of sequence b stands at place lens[b] - n_q[b] + i and sees the stored tokens
  *             up to and including its own place:
  *             x_t = scale (q . k_t);  p = softmax(x) over the tokens it sees;  out = sum_t p_t v_t.
- *             The query tokens are stored before they attend (akb_append first).  Sums, maxima and weights are held in
- *             binary32.
+ *             The query tokens are stored before they attend (akb_append first).  Scores, maxima, sums, and the weights
+ *             as they are summed up are held in binary32, which q . k has to lie in.  For the product with v a weight is
+ *             rounded to the 16-bit type where out has 16 bits, and is the sum of two such numbers where out is float32
+ *             (22 bits in binary16, 16 in bfloat16).  In binary16 a weight is no finer than 2^-32 of the row's largest.
  *   score     Optionally score[b][h][t] += sum of p_t over the call's query tokens and the query heads of KV head h.
  *   evict     Of each (sequence, KV head) the `recent` last tokens stay, and of the others those with the largest score
  *             (ties: the earlier token), `keep` in all, in their order.

@@ -185,7 +185,9 @@ __device__ __forceinline__ void store_logits(float* block, const f32x4_t (&s)[4]
 // One workgroup of four waves per (row group of RT row tiles, split): wave w takes every fourth block of the split, and the four states are put together
 // through LDS.  Where a row group has several splits, the last of its workgroups to arrive joins them (the parts go through memory with device scope, as
 // the partial results of the 16-bit cache's V kernel do).  EXACT: 32-bit results; the weights go into the second product as two 16-bit numbers each (their
-// sum carries 16 bits or more where one carries 8 or 11, which is what a 16-bit result keeps).
+// sum carries 16 bits or more where one carries 8 or 11, which is what a 16-bit result keeps).  A third number for bfloat16 costs 32-bit results of single tokens 1 to 5 %, of
+// drafts 9 % (8 x 8 pairs of 3000 tokens, 40 rows: 21.8 / 23.6 us), of prompts 24 % (8192 tokens: 737 / 914 us); two err by 2^-17 of a weight
+// at most.
 template <class T, int D, bool EXACT, int RT, bool NT>
 __global__ __launch_bounds__(64 * kWaves, 2) void rows_kernel(RowArgs a)
 {
