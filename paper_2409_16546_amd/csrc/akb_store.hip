@@ -91,9 +91,11 @@ hipError_t launch_append(const akb_cache& c, const uint16_t* k_new, const uint16
     if (n == 0) return hipSuccess;
     const int blocks = (kTB - 1 + n + kTB - 1) / kTB;
     const dim3 grid(blocks, c.shape.Hkv, c.shape.B);
-    // A ticket per workgroup or a launch behind: device time of one token 128 workgroups 4.1 us, 512 6.0 (64 sequences) and 7.8 (16) against 4.0 + 1.4 and the gap
-    // between the two launches; 1024 8.8 and 14.6.  (Of one side per workgroup they would be twice as many, and gain nothing: 8 x 8 pairs 8192 tokens 77 us.)
-    const bool ticketed = long(grid.x) * grid.y * grid.z <= 640;
+    // A ticket per workgroup or a launch behind, us of calls one after the other.  One block per head, where the workgroups arrive as they were launched: 512 workgroups of 64
+    // sequences 6.0 / 8.3 and of 16 sequences 7.9 / 8.3, 640 of 80 and of 20 sequences 6.2 / 8.2 and 8.3 / 8.3, 768 of 96 and of 24 6.3 / 8.3 and 10.2 / 8.3, 1024 7.1 / 8.1
+    // and 11.8 / 8.1.  Several blocks: 96 workgroups 8.2 / 10.3, 192 9.4 / 10.4, 272 11.0 / 11.6, 288 11.7 / 11.6, 384 10.8 / 10.3 and 13.1 / 11.6, 576 15.7 / 11.7.  (Of one side
+    // per workgroup they would be twice as many, and gain nothing: 8 x 8 pairs 8192 tokens 77 us.)
+    const bool ticketed = long(grid.x) * grid.y * grid.z <= (blocks == 1 ? 640 : 288);
     auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(2 * c.shape.D), 0, st, c, k_new, v_new, n_new, n, ticketed ? 1 : 0); };
     // New tokens that are more than half of the last-level cache are read and their codes stored with the non-temporal hint; fewer may still lie there as they were
     // made, and their codes are wanted there next.  Plain / with the hint: 8 x 8 pairs 8192 tokens (268 MB) 76.7 / 68.8 us, 6 x 32 pairs up to 777 tokens (76 MB at most, read again and again) 28.9 / 33.8.

@@ -173,3 +173,28 @@ def test_long_sequence_in_the_largest_capacity(A, dtype):
     again = A.BlockCache.allocate(1, 2, 1, D, 5056, dtype)   # the kept values, stored anew
     A.akb_append(again, K[:, :, want].contiguous(), V[:, :, want].contiguous())
     assert all(torch.equal(a, b) for a, b in zip(A.akb_unpack(d), A.akb_unpack(again)))
+
+
+# ------------------------------------------------------------------------ who moves the length: workgroups up to, at and beyond the lines
+
+@pytest.mark.parametrize("B,H,n", [(4, 8, 500), (4, 8, 560), (11, 8, 300), (18, 8, 65), (19, 8, 65), (20, 32, 1), (21, 31, 1), (80, 8, 1), (81, 8, 1)],
+                         ids=lambda x: str(x))
+def test_ragged_appends_with_refusals_by_ticket_and_by_launch(A, B, H, n):
+    D, Ncap = 64, max(192, (2 * n + 63) // 64 * 64)
+    print(f"B {B} H {H} n {n}: {B * H * ((63 + n + 63) // 64)} workgroups", flush=True)
+    c = A.BlockCache.allocate(B, H, H, D, Ncap, F16, score=True)
+    ref = R.Ref(B, H, H, D, Ncap, F16)
+    c.score.fill_(7.0)
+    rows = torch.Generator().manual_seed(n)
+    start = [(Ncap - n, Ncap - n + 1, Ncap, 0, 63, 64)[b % 6] for b in range(B)]   # it just fits, it does not (twice), whatever else
+    for turn in range(3):
+        n_new = start if turn == 0 else [(n, int(torch.randint(0, n + 1, (1,), generator=rows)), n, 0, n, -2, n + 9)[(b + turn) % 7] for b in range(B)]
+        m = max(start) if turn == 0 else n
+        k, v = (R.tokens(B, H, m, D, F16, 10 * turn + s) for s in (0, 1))
+        ref.append(k, v, n_new)
+        A.akb_append(c, k.to(DEV), v.to(DEV), i32(n_new))
+    assert ref.refused > 0 and c.flags.cpu().tolist() == [ref.refused, 0, 0, 0] + [0] * B
+    R.assert_same_tokens(A, c, ref)
+    score = c.score.view(B, H, Ncap).cpu()
+    for b in range(B):
+        assert not score[b, :, :ref.len(b)].any() and (score[b, :, ref.len(b):] == 7.0).all(), b
