@@ -22,8 +22,10 @@
  *             x_t = scale (q . k_t);  p = softmax(x) over the tokens it sees;  out = sum_t p_t v_t.
  *             The query tokens are stored before they attend (akb_append first).  Scores, maxima, sums, and the weights
  *             as they are summed up are held in binary32, which q . k has to lie in.  For the product with v a weight is
- *             rounded to the 16-bit type where out has 16 bits, and is the sum of two such numbers where out is float32
- *             (22 bits in binary16, 16 in bfloat16).  In binary16 a weight is no finer than 2^-32 of the row's largest.
+ *             rounded to the 16-bit type where out has 16 bits, and is the sum of two or three such numbers where out is
+ *             float32 (22 bits in binary16, 24 in bfloat16).  In binary16 a weight is no finer than 2^-32 of the row's largest.
+ *             Finite v give finite results; values of 2^65 and more (bfloat16) cost the weights beside them some bits: their
+ *             exponents carry 2^-20 instead of 2^-22, and values 2^160 below them may count as zero.
  *   score     Optionally score[b][h][t] += sum of p_t over the call's query tokens and the query heads of KV head h.
  *   evict     Of each (sequence, KV head) the `recent` last tokens stay, and of the others those with the largest score
  *             (ties: the earlier token), `keep` in all, in their order.

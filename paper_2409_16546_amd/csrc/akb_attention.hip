@@ -131,8 +131,9 @@ template <class T, int D> struct RowState {
         z = 0.f;
         limit = lim;
     }
-    // S^T of 64 tokens -> weights (unit: the bits of the largest); ph[u]: tokens 32 u .. + 31 as the operand of the second product, pl: what 16 bits lack of them
-    template <bool EXACT> __device__ __forceinline__ void weights(f32x4_t (&s)[4], int first, bool masked, float c2, float unit, int lane, u32x4_t (&ph)[2], u32x4_t (&pl)[2])
+    // S^T of 64 tokens -> weights (unit: the bits of the largest); ph[u]: tokens 32 u .. + 31 as the operand of the second product, pl: what 16 bits lack of them, pr: what
+    // those lack (bfloat16)
+    template <bool EXACT> __device__ __forceinline__ void weights(f32x4_t (&s)[4], int first, bool masked, float c2, float unit, int lane, u32x4_t (&ph)[2], u32x4_t (&pl)[2], u32x4_t (&pr)[2])
     {
         float mx = -__builtin_inff();
         const int seen = limit - first - 4 * (lane >> 4);   // counted from the lane's first token
@@ -168,7 +169,10 @@ template <class T, int D> struct RowState {
             for (int k = 0; k < 4; ++k) {
                 const float p0 = s[2 * u + (k >> 1)][2 * (k & 1)], p1 = s[2 * u + (k >> 1)][2 * (k & 1) + 1];
                 ph[u][k] = T::pack(p0, p1);
-                if (EXACT) pl[u][k] = T::pack(p0 - T::lo(ph[u][k]), p1 - T::hi(ph[u][k]));
+                if (!EXACT) continue;
+                const float l0 = p0 - T::lo(ph[u][k]), l1 = p1 - T::hi(ph[u][k]);
+                pl[u][k] = T::pack(l0, l1);
+                if (T::kWide) pr[u][k] = T::pack(l0 - T::lo(pl[u][k]), l1 - T::hi(pl[u][k]));
             }
     }
 };
@@ -184,10 +188,9 @@ __device__ __forceinline__ void store_logits(float* block, const f32x4_t (&s)[4]
 
 // One workgroup of four waves per (row group of RT row tiles, split): wave w takes every fourth block of the split, and the four states are put together
 // through LDS.  Where a row group has several splits, the last of its workgroups to arrive joins them (the parts go through memory with device scope, as
-// the partial results of the 16-bit cache's V kernel do).  EXACT: 32-bit results; the weights go into the second product as two 16-bit numbers each (their
-// sum carries 16 bits or more where one carries 8 or 11, which is what a 16-bit result keeps).  A third number for bfloat16 costs 32-bit results of single tokens 1 to 5 %, of
-// drafts 9 % (8 x 8 pairs of 3000 tokens, 40 rows: 21.8 / 23.6 us), of prompts 24 % (8192 tokens: 737 / 914 us); two err by 2^-17 of a weight
-// at most.
+// the partial results of the 16-bit cache's V kernel do).  EXACT: 32-bit results; the weights go into the second product as two binary16 numbers each (their
+// sum carries 22 bits) or three bfloat16 numbers (24; with two, 16 bits, results of few or unlike weights were up to 4.6 times as far off as 32-bit arithmetic is).  The
+// third costs single tokens 1 to 5 %, drafts 9 % (8 x 8 pairs of 3000 tokens, 40 rows: 21.8 / 23.6 us), prompts 24 % (8192 tokens: 737 / 914 us).
 template <class T, int D, bool EXACT, int RT, bool NT>
 __global__ __launch_bounds__(64 * kWaves, 2) void rows_kernel(RowArgs a)
 {
@@ -243,9 +246,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void rows_kernel(RowArgs a)
         if (blk + kWaves < whole) kc.load(c, block0 + blk + kWaves, lane);
         if (RT == 1 && logits) store_logits(logits + size_t(blk) * kTB * rows, s[0], rows, lane & 15, lane);
         const bool masked = (blk + 1) * kTB > all_see;
-        u32x4_t ph[RT][2], pl[RT][2];
+        u32x4_t ph[RT][2], pl[RT][2], pr[RT][2];
 #pragma unroll
-        for (int k = 0; k < RT; ++k) st[k].template weights<EXACT>(s[k], blk * kTB, masked, a.c2, unit, lane, ph[k], pl[k]);
+        for (int k = 0; k < RT; ++k) st[k].template weights<EXACT>(s[k], blk * kTB, masked, a.c2, unit, lane, ph[k], pl[k], pr[k]);
 #pragma unroll
         for (int i = 0; i < D / 16; ++i)
 #pragma unroll
@@ -255,6 +258,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void rows_kernel(RowArgs a)
                 for (int k = 0; k < RT; ++k) {
                     st[k].o[i] = T::mfma16(v, ph[k][u], st[k].o[i]);
                     if (EXACT) st[k].o[i] = T::mfma16(v, pl[k][u], st[k].o[i]);
+                    if (EXACT && T::kWide) st[k].o[i] = T::mfma16(v, pr[k][u], st[k].o[i]);
                 }
             }
     }
@@ -290,9 +294,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void rows_kernel(RowArgs a)
                 }
             }
         const float unit = weight_bits<T>(__any(large & kLargeValues));
-        u32x4_t ph[RT][2], pl[RT][2];
+        u32x4_t ph[RT][2], pl[RT][2], pr[RT][2];
 #pragma unroll
-        for (int k = 0; k < RT; ++k) st[k].template weights<EXACT>(s[k], blk * kTB, true, a.c2, unit, lane, ph[k], pl[k]);
+        for (int k = 0; k < RT; ++k) st[k].template weights<EXACT>(s[k], blk * kTB, true, a.c2, unit, lane, ph[k], pl[k], pr[k]);
 #pragma unroll
         for (int i = 0; i < D / 16; ++i)
 #pragma unroll
@@ -301,6 +305,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void rows_kernel(RowArgs a)
                 for (int k = 0; k < RT; ++k) {
                     st[k].o[i] = T::mfma16(v[i][u], ph[k][u], st[k].o[i]);
                     if (EXACT) st[k].o[i] = T::mfma16(v[i][u], pl[k][u], st[k].o[i]);
+                    if (EXACT && T::kWide) st[k].o[i] = T::mfma16(v[i][u], pr[k][u], st[k].o[i]);
                 }
     }
     const int part = part_floats(rows, D);

@@ -3,7 +3,7 @@
 // With many rows the products are what takes time, and turning codes into 16-bit numbers the next: a wave that does it for its own rows alone (the rows kernel)
 // spends more on that than on its softmax.  Here the four waves of a workgroup have 32 rows each and share every block: it is turned once, into LDS, in the order
 // in which 32 x 32 x 16 matrix instructions take their operands (1 KB per operand, lane after lane), while the block before is multiplied.
-// Per block and wave: 32 matrix instructions of 32 cycles for K and V together (48 with 32-bit results), 32 reads of 1 KB from LDS, and the softmax of 64 x 32 scores,
+// Per block and wave: 32 matrix instructions of 32 cycles for K and V together (with 32-bit results 48 in binary16, 64 in bfloat16), 32 reads of 1 KB from LDS, and the softmax of 64 x 32 scores,
 // 32 per lane, beside the scores of the next block.  Two workgroups of 64 KB share a compute unit.
 // A prompt of 8192 tokens, 32 query heads on 8, bfloat16: 538 us, 1020 TFLOP/s of the products that are wanted (a plain product of 8192 x 8192 matrices reaches 1207
 // here); the clock is at 1.9 GHz then.
@@ -201,7 +201,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prompt_kernel(RowArgs a)
             }
             const float base = top == -__builtin_inff() ? 0.f : top;   // nothing seen yet: all weights are 2^-inf
             clear(next);
-            u32x4_t ph[2], pl[2];
+            u32x4_t ph[2], pl[2], pr[2];
 #pragma unroll
             for (int t = 0; t < 5; ++t) {   // 16 tokens: weights of t, products of t - 1
                 if (t < 4) {
@@ -212,7 +212,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prompt_kernel(RowArgs a)
                         const float p0 = __builtin_amdgcn_exp2f(fmaf(s[t >> 1][r], a.c2, -base)), p1 = __builtin_amdgcn_exp2f(fmaf(s[t >> 1][r + 1], a.c2, -base));
                         z += p0 + p1;
                         ph[t & 1][k] = T::pack(p0, p1);
-                        if (EXACT) pl[t & 1][k] = T::pack(p0 - T::lo(ph[t & 1][k]), p1 - T::hi(ph[t & 1][k]));
+                        if (!EXACT) continue;
+                        const float l0 = p0 - T::lo(ph[t & 1][k]), l1 = p1 - T::hi(ph[t & 1][k]);
+                        pl[t & 1][k] = T::pack(l0, l1);
+                        if (T::kWide) pr[t & 1][k] = T::pack(l0 - T::lo(pl[t & 1][k]), l1 - T::hi(pl[t & 1][k]));
                     }
                 }
                 if (t > 0) {
@@ -221,6 +224,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prompt_kernel(RowArgs a)
                         const u32x4_t x = v.x[i][t - 1][lane];
                         o[i] = T::mfma32(x, ph[(t - 1) & 1], o[i]);
                         if (EXACT) o[i] = T::mfma32(x, pl[(t - 1) & 1], o[i]);
+                        if (EXACT && T::kWide) o[i] = T::mfma32(x, pr[(t - 1) & 1], o[i]);
                     }
                 }
                 // the order that the compiler keeps of its own accord has the products in a row; with two products per weight it has too few registers to choose

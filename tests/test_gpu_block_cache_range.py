@@ -121,3 +121,31 @@ def test_one_token_comes_back(A):
                 # exponent's argument, 2^-21)
                 want = v.repeat_interleave(2, dim=1).double()
                 assert ((out.double() - want).abs() <= want.abs() * 2.0 ** -19).all(), (dtype, out_dtype)
+
+
+@pytest.mark.parametrize("dtype", [F16, B16], ids=["fp16", "bf16"])
+@pytest.mark.parametrize("way", [((1, 1), 128, 8, 16, 1, 40, 1), ((1, 1), 64, 8, 16, 1, 500, 1), ((1, 4), 128, 2, 64, 4, 1000, 1), ((2, 1), 64, 4, 32, 2, 300, 2),
+                                 ((2, 2), 128, 32, 32, 8, 1100, 5), ((3, 8), 128, 8, 8, 8, 6200, 65), ((3, 8), 64, 8, 8, 8, 6200, 65)],
+                         ids=lambda w: f"kernel{w[0][0]}-parts{w[0][1]}-D{w[1]}-N{w[5]}-n{w[6]}")
+def test_32_bit_results_of_two_weights(A, way, dtype):
+    """Rows that see two tokens of weights 1 and 2^-x, x below 1, and others of none; the value of the second is 1, of the others 0: the result is 1 / (1 + 2^x).  Off by:
+    the two exponents, rounded below 8 (2^-22 each, times ln 2); the exponentials (2^-23 each); the scale, the sum of the weights, the weight itself (22 bits or more), its
+    three products, the reciprocal and the product with it (2^-24 each, twice for the weight)."""
+    path, D, B, Hq, Hkv, N, n = way
+    Ncap = (N + 63) // 64 * 64
+    assert A.akb_attention_path(B, Hq, Hkv, D, Ncap, n) == path
+    c = A.BlockCache.allocate(B, Hq, Hkv, D, Ncap, dtype, n=n)
+    k, v = (torch.zeros(B, Hkv, N, D, dtype=dtype, device=DEV) for _ in range(2))
+    k[:, :, :, 0] = -2.0 ** 14                     # times 2^-7 and more: weights below 2^-127
+    k[:, :, 0, 0], k[:, :, 1, 0] = 1.0, 0.0
+    v[:, :, 1] = 1.0
+    A.akb_append(c, k, v)
+    x = (torch.arange(B * Hq * n, device=DEV) * 37 % 127 + 1).view(B, Hq, n) / 128   # 1/128 .. 127/128, numbers of 7 bits
+    q = torch.zeros(B, Hq, n, D, dtype=dtype, device=DEV)
+    q[..., 0] = x.to(dtype)
+    scale = float(torch.tensor(0.6931471805599453, dtype=F32))
+    out = A.akb_attention(c, q, scale=scale).double()
+    want = 1 / (1 + torch.exp(x.double() * scale))[..., None]
+    worst = float(((out - want).abs() / want).max())
+    print(f"worst {worst:.2e}", flush=True)
+    assert worst <= 2 * (2.0 ** -22 * 0.6932 + 2.0 ** -23) + 9 * 2.0 ** -24 + (2.0 ** -22 if dtype == F16 else 0.0)
