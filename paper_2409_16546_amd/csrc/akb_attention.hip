@@ -3,8 +3,8 @@
 //
 // Few rows are bound by the codes: 2 D bytes per token and KV head, read once for all rows of a group.  A code becomes a number in one conversion of two (exact:
 // the block's power of two is the conversion's scale) and goes from there to the matrix instruction; one walk keeps 16 KB per wave in flight.  16 sequences x 32 heads,
-// 8192 tokens: 158 us, 6.8 TB/s, where a plain read of memory reaches 7.0.  Small calls are bound by their chain: launch, lengths, one block per wave, the
-// waves' states through LDS, the parts through memory (32 heads, 1024 tokens: 7.5 us).
+// 8192 tokens: 156 us, 6.9 TB/s, where a plain read of memory reaches 7.0.  Small calls are bound by their chain: launch, lengths, one block per wave, the
+// waves' states through LDS, the parts through memory (32 heads, 1024 tokens: 7.6 us).
 #include "akb_rows.h"
 
 namespace akb {

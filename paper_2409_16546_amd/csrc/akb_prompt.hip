@@ -5,7 +5,7 @@
 // in which 32 x 32 x 16 matrix instructions take their operands (1 KB per operand, lane after lane), while the block before is multiplied.
 // Per block and wave: 32 matrix instructions of 32 cycles for K and V together (with 32-bit results 48 in binary16, 64 in bfloat16), 32 reads of 1 KB from LDS, and the softmax of 64 x 32 scores,
 // 32 per lane, beside the scores of the next block.  Two workgroups of 64 KB share a compute unit.
-// A prompt of 8192 tokens, 32 query heads on 8, bfloat16: 538 us, 1020 TFLOP/s of the products that are wanted (a plain product of 8192 x 8192 matrices reaches 1207
+// A prompt of 8192 tokens, 32 query heads on 8, bfloat16: 541 us, 1016 TFLOP/s of the products that are wanted (a plain product of 8192 x 8192 matrices reaches 1207
 // here); the clock is at 1.9 GHz then.
 #include "akb_rows.h"
 
