@@ -29,6 +29,12 @@
  *   score     Optionally score[b][h][t] += sum of p_t over the call's query tokens and the query heads of KV head h.
  *   evict     Of each (sequence, KV head) the `recent` last tokens stay, and of the others those with the largest score
  *             (ties: the earlier token), `keep` in all, in their order.
+ *   share     Sequences that go on from one prompt: attention over a prefix that is stored, and read, once for all of them;
+ *             copies of sequences up to a place of their own; sequences cut back in place.
+ *   turn      Keys and queries as a model's projections give them, normed per head and turned by their places on the way to
+ *             the cache and to attention:
+ *             x'_d = w_d x_d / sqrt(mean_d x_d^2 + eps), and each pair (a, b) of channels of number j becomes
+ *             (a cos u - b sin u, a sin u + b cos u), u = place inv_freq_j.
  *
  * Conventions: those of akv.h (device pointers owned by the caller unless named "host", nothing is allocated or
  * synchronised, work is enqueued on the caller's stream, akv_status / akv_last_error(), 16-byte alignment of every
@@ -147,6 +153,62 @@ int32_t akb_attention_join(const akb_shape *shape, int32_t n, int32_t max_len);
  */
 akv_status akb_evict(const akb_cache *src, const akb_cache *dst, int32_t keep, int32_t recent, int32_t *kept, void *workspace, size_t workspace_bytes,
                      void *stream);
+
+/*
+ * Attention of sequences that continue shared ones: sequence b of `cache` (B of them) goes on from sequence b / (B / Bp) of `prefix` (Bp of them, Bp divides
+ * B), whose tokens count as if they stood in front of its own.  Query token i of the n_q[b] of sequence b stands at place P + lens[b] - n_q[b] + i, P its
+ * prefix's length, and sees the tokens up to and including its own place: of a sequence that has stored fewer than n_q[b] tokens, the first query tokens
+ * stand in the prefix.  prefix and cache have the same Hq, Hkv, D and dtype; neither is written.  q, n_q, out, the limit on row tiles, rows behind n_q[b], and rows that
+ * see nothing: as for akb_attention; params: as there, max_len bounds the own lengths, prefix_max_len (0: the prefix's Ncap) those of the prefix; both are hints.
+ * params->accumulate is refused: weights over a prefix belong to no one sequence.
+ * workspace: as for akb_attention, of akb_attention_shared_workspace(prefix's shape, shape, n) bytes or more.  The same call gives the same bits.
+ */
+size_t akb_attention_shared_workspace(const akb_shape *prefix, const akb_shape *shape, int32_t n);
+akv_status akb_attention_shared(const akb_cache *prefix, const akb_cache *cache, const uint16_t *q, const int32_t *n_q, int32_t n, void *out,
+                                const akb_params *params, int32_t prefix_max_len, void *workspace, size_t workspace_bytes, void *stream);
+
+/* How keys and queries are normed and turned (above).  Weights and norms are applied in binary32, angles are made in binary64, each result is rounded once. */
+typedef struct akb_rotary {
+    const uint16_t *q_norm, *k_norm; /* device [D] of the shape's type: w; NULL: not normed (each by itself)               */
+    const float *inv_freq;           /* device [rot / 2]                                                                   */
+    const int32_t *base;             /* device [n_base], or NULL: token i of sequence b stands at base[b / (B / n_base)] +
+                                        lens[b] + i: lengths of shared prefixes, counts of evicted tokens                  */
+    int32_t n_base;                  /* divides B                                                                          */
+    int32_t rot;                     /* the first rot channels turn: a multiple of 16, 0..D                                */
+    int32_t pairs;                   /* 0: pair j is channels (j, j + rot / 2); 1: channels (2 j, 2 j + 1)                 */
+    float eps;
+} akb_rotary;
+
+/* Projected tokens: device arrays of the shape's type.  Token i of sequence b has its heads at seq * b + token * i elements from the front, one after the
+ * other, D channels each.  Pointers 16-byte aligned, strides multiples of 8; one array of all three, or three. */
+typedef struct akb_tokens {
+    const uint16_t *q, *k, *v;
+    int64_t q_seq, q_token, k_seq, k_token, v_seq, v_token;
+} akb_tokens;
+
+/*
+ * Append tokens as projections give them: k is normed and turned and stored, and v stored, as akb_append stores them; q is normed and turned by the same places
+ * and goes to q_out, device [B][Hq][n][D], which is what akb_attention takes.  q and q_out may both be NULL.  n_new: as for akb_append; rows of q_out behind
+ * n_new[b], and all of a sequence that is refused, are left as they were.  q_out shares no memory with the inputs.  Not finite inputs: as for akb_append; a NaN of a
+ * token reaches the whole of its head where it is normed, and its partner where it is turned.
+ */
+akv_status akb_append_rotated(const akb_cache *cache, const akb_tokens *tokens, const int32_t *n_new, int32_t n, uint16_t *q_out, const akb_rotary *rotary,
+                              void *stream);
+
+/*
+ * Copy sequences: sequence j of dst becomes the first min(lens of the parent, upto[j]) tokens of its parent, sequence parents[j] of src.  parents: device
+ * int32 [dst B]; a number outside 0..src B - 1 leaves sequence j as it was.  NULL: every sequence its own (dst B = src B).  upto: device int32 [dst B], or NULL for all
+ * tokens.  Complete blocks are copied as they are; where a copy ends inside one, its tail takes that block's values (which rounds nothing: they are numbers
+ * of the 16-bit type), all 64 of them; scores are copied where both have one.  A sequence whose length would exceed dst's Ncap is left unchanged and dst's
+ * flags[AKV_FLAG_OVERFLOW] is incremented.  dst has src's Hkv, D and dtype, and shares no memory with src, which is not written.
+ */
+akv_status akb_fork(const akb_cache *src, const akb_cache *dst, const int32_t *parents, const int32_t *upto, void *stream);
+
+/*
+ * Cut sequences back in place: lens[b] becomes min(lens[b], max(keep[b], 0)).  Where that ends inside a complete block, the tail takes the block's
+ * values (all 64), and it is rounded anew when it is complete again.  keep: device int32 [B].
+ */
+akv_status akb_truncate(const akb_cache *cache, const int32_t *keep, void *stream);
 
 /* The values as they are read: device [B][Hkv][Ncap][D] of the shape's type, zeros behind a sequence's length.  Either output may be NULL. */
 akv_status akb_unpack(const akb_cache *cache, uint16_t *k_out, uint16_t *v_out, void *stream);

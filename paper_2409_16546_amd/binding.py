@@ -29,7 +29,7 @@ EXPORTS = ["akv_version", "akv_last_error", "akv_layout_sizes", "akv_cache_reset
            "akw_layout_sizes", "akw_workspace_init", "akw_pack", "akw_unpack", "akw_gemv"]
 AKW_MAX_B = 4
 AKB_EXPORTS = ["akb_layout_sizes", "akb_cache_reset", "akb_append", "akb_attention_workspace", "akb_workspace_init", "akb_attention_path", "akb_attention_join", "akb_attention", "akb_evict_workspace", "akb_evict",
-               "akb_unpack"]
+               "akb_attention_shared_workspace", "akb_attention_shared", "akb_append_rotated", "akb_fork", "akb_truncate", "akb_unpack"]
 AKB_TB, AKB_MAX_G = 64, 16
 AKB_DTYPES = {torch.float16: 0, torch.bfloat16: 1}
 
@@ -94,6 +94,15 @@ class akb_sizes(C.Structure):
 
 class akb_params(C.Structure):
     _fields_ = [("scale", C.c_float), ("out_dtype", C.c_int32), ("accumulate", C.c_int32), ("max_len", C.c_int32)]
+
+
+class akb_rotary(C.Structure):
+    _fields_ = [("q_norm", C.c_void_p), ("k_norm", C.c_void_p), ("inv_freq", C.c_void_p), ("base", C.c_void_p), ("n_base", C.c_int32), ("rot", C.c_int32),
+                ("pairs", C.c_int32), ("eps", C.c_float)]
+
+
+class akb_tokens(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("q", "k", "v")] + [(n, C.c_int64) for n in ("q_seq", "q_token", "k_seq", "k_token", "v_seq", "v_token")]
 
 
 _lib = None
@@ -171,6 +180,17 @@ def lib() -> C.CDLL:
         L.akb_evict_workspace.argtypes = [C.POINTER(akb_shape), C.c_int32]
         L.akb_evict.restype = C.c_int
         L.akb_evict.argtypes = [C.POINTER(akb_cache), C.POINTER(akb_cache), C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
+        L.akb_attention_shared_workspace.restype = C.c_size_t
+        L.akb_attention_shared_workspace.argtypes = [C.POINTER(akb_shape), C.POINTER(akb_shape), C.c_int32]
+        L.akb_attention_shared.restype = C.c_int
+        L.akb_attention_shared.argtypes = [C.POINTER(akb_cache), C.POINTER(akb_cache), C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.POINTER(akb_params), C.c_int32,
+                                           C.c_void_p, C.c_size_t, C.c_void_p]
+        L.akb_append_rotated.restype = C.c_int
+        L.akb_append_rotated.argtypes = [C.POINTER(akb_cache), C.POINTER(akb_tokens), C.c_void_p, C.c_int32, C.c_void_p, C.POINTER(akb_rotary), C.c_void_p]
+        L.akb_fork.restype = C.c_int
+        L.akb_fork.argtypes = [C.POINTER(akb_cache), C.POINTER(akb_cache), C.c_void_p, C.c_void_p, C.c_void_p]
+        L.akb_truncate.restype = C.c_int
+        L.akb_truncate.argtypes = [C.POINTER(akb_cache), C.c_void_p, C.c_void_p]
         L.akb_unpack.restype = C.c_int
         L.akb_unpack.argtypes = [C.POINTER(akb_cache), C.c_void_p, C.c_void_p, C.c_void_p]
         _lib = L
@@ -571,17 +591,19 @@ class BlockCache:
             p = self._params[values] = C.byref(akb_params(*values))
         return p
 
-    def reserve(self, n: int = 1, keep: int = 0) -> "BlockCache":
-        """Make the workspace large enough for attention of up to n query tokens and, where keep > 0, for evictions down to `keep` tokens.  A larger
+    def reserve(self, n: int = 1, keep: int = 0, prefix: "BlockCache | None" = None) -> "BlockCache":
+        """Make the workspace large enough for attention of up to n query tokens and, where keep > 0, for evictions down to `keep` tokens and, with a prefix, for
+        attention of up to n query tokens that goes on from it.  A larger
         workspace is a new tensor, prepared on the current stream: calls on another stream have to be ordered behind that, as behind anything that makes
         their tensors, and no graph is captured meanwhile.  The one before is kept as long as the cache, for the calls on other streams and the captured
         graphs that use it."""
         shp = self.struct().shape
         need = lib().akb_attention_workspace(C.byref(shp), n, int(self.score is not None))
         need_evict = lib().akb_evict_workspace(C.byref(shp), keep) if keep > 0 else 1
-        if not need or not need_evict:
+        need_shared = lib().akb_attention_shared_workspace(C.byref(prefix.struct().shape), C.byref(shp), n) if prefix is not None else 1
+        if not need or not need_evict or not need_shared:
             _check(AKV_EINVAL)
-        need = max(need, need_evict)
+        need = max(need, need_evict, need_shared)
         if self.workspace is None or self.workspace.numel() < need:
             if self.workspace is not None:   # half as large again: what is kept stays below twice the present one
                 self._replaced.append(self.workspace)
@@ -661,6 +683,74 @@ def akb_evict(src: BlockCache, dst: BlockCache, keep: int, recent: int = 0, *, k
     ws = src.workspace if workspace is None else workspace
     _here(src.k8, dst.k8, kept, ws)
     _check(lib().akb_evict(src.ref(), dst.ref(), keep, recent, _ptr(kept), _ptr(ws), _nbytes(ws), _stream()))
+
+
+def akb_attention_shared(prefix: BlockCache, cache: BlockCache, q: torch.Tensor, out: torch.Tensor | None = None, *, n_q: torch.Tensor | None = None,
+                         scale: float = 0.0, max_len: int = 0, prefix_max_len: int = 0, workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """akb_attention of sequences that go on from shared ones: sequence b of ``cache`` from sequence b // (B / prefix's B) of ``prefix``.  The cache's workspace has to
+    be large enough (``cache.reserve(n, prefix=prefix)``)."""
+    shape = q.shape
+    n = 1 if len(shape) == 3 else shape[2]
+    assert q.dtype == cache.dtype and shape == ((cache.B, cache.Hq, cache.D) if len(shape) == 3 else (cache.B, cache.Hq, n, cache.D))
+    assert n_q is None or (n_q.dtype == torch.int32 and n_q.shape == (cache.B,))
+    if out is None:
+        out = (torch.empty if n_q is None else torch.zeros)(shape, dtype=torch.float32, device=q.device)
+    assert out.dtype in (torch.float32, cache.dtype) and out.shape == shape
+    ws = cache.workspace if workspace is None else workspace
+    _here(prefix.k8, cache.k8, q, out, n_q, ws)
+    p = cache.params(scale, 0 if out.dtype == torch.float32 else 1, 0, max_len)
+    _check(lib().akb_attention_shared(prefix.ref(), cache.ref(), _ptr(q), _ptr(n_q), n, _ptr(out), p, prefix_max_len, _ptr(ws), _nbytes(ws), _stream()))
+    return out
+
+
+def _projected(t: torch.Tensor | None, cache: BlockCache, n: int, heads: int) -> tuple:
+    """(address, strides of a sequence and of a token) of projected tokens [B, n, heads, D], whose heads lie one after the other."""
+    if t is None:
+        return None, 0, 0
+    assert t.dtype == cache.dtype and t.shape == (cache.B, n, heads, cache.D), f"[{cache.B}, {n}, {heads}, {cache.D}] of {cache.dtype} is wanted"
+    seq, token, head, channel = t.stride()
+    assert t.is_cuda and channel == 1 and (head == cache.D or heads == 1), "device-resident tensors whose heads lie one after the other only"
+    return t.data_ptr(), seq if cache.B > 1 else 0, token if n > 1 else 0
+
+
+def akb_append_rotated(cache: BlockCache, q: torch.Tensor | None, k: torch.Tensor, v: torch.Tensor, q_out: torch.Tensor | None = None, *, inv_freq: torch.Tensor | None,
+                       n_new: torch.Tensor | None = None, q_norm: torch.Tensor | None = None, k_norm: torch.Tensor | None = None, eps: float = 1e-6, pairs: bool = False,
+                       base: torch.Tensor | None = None) -> torch.Tensor | None:
+    """Projected tokens q [B, n, Hq, D], k and v [B, n, Hkv, D] of the cache's type (slices of one tensor, or three): k is normed and turned and stored with v, q
+    normed and turned, in q_out [B, Hq, n, D], which is returned (q None: None).  inv_freq: float32 [rot / 2] for rot channels that turn, or None for none;
+    q_norm, k_norm: weights [D] of the cache's type, or None; base: int32 [n_base], n_base dividing B, added to the places, or None; n_new: int32 [B] or None."""
+    n = k.shape[1]
+    assert inv_freq is None or (inv_freq.dtype == torch.float32 and inv_freq.dim() == 1)
+    for w in (q_norm, k_norm):
+        assert w is None or (w.dtype == cache.dtype and w.shape == (cache.D,))
+    for t in (base, n_new):
+        assert t is None or (t.dtype == torch.int32 and t.dim() == 1)
+    assert n_new is None or n_new.shape == (cache.B,)
+    x = akb_tokens()
+    (x.q, x.q_seq, x.q_token), (x.k, x.k_seq, x.k_token), (x.v, x.v_seq, x.v_token) = _projected(q, cache, n, cache.Hq), _projected(k, cache, n, cache.Hkv), _projected(v, cache, n, cache.Hkv)
+    if q is not None and q_out is None:
+        q_out = (torch.empty if n_new is None else torch.zeros)(cache.B, cache.Hq, n, cache.D, dtype=cache.dtype, device=q.device)
+    assert q_out is None or (q_out.dtype == cache.dtype and q_out.shape == (cache.B, cache.Hq, n, cache.D))
+    _here(cache.k8, q, k, v, q_out, inv_freq, n_new, q_norm, k_norm, base)
+    r = akb_rotary(_ptr(q_norm), _ptr(k_norm), _ptr(inv_freq), _ptr(base), 0 if base is None else base.numel(), 0 if inv_freq is None else 2 * inv_freq.numel(), int(pairs), eps)
+    _check(lib().akb_append_rotated(cache.ref(), C.byref(x), _ptr(n_new), n, _ptr(q_out), C.byref(r), _stream()))
+    return q_out
+
+
+def akb_fork(src: BlockCache, dst: BlockCache, parents: torch.Tensor | None = None, upto: torch.Tensor | None = None) -> None:
+    """Sequence j of dst becomes the first upto[j] tokens (None: all) of sequence parents[j] of src (None: j); int32 [dst.B] on the device.  A parent that
+    src does not have leaves sequence j as it was."""
+    for t in (parents, upto):
+        assert t is None or (t.dtype == torch.int32 and t.shape == (dst.B,))
+    _here(src.k8, dst.k8, parents, upto)
+    _check(lib().akb_fork(src.ref(), dst.ref(), _ptr(parents), _ptr(upto), _stream()))
+
+
+def akb_truncate(cache: BlockCache, keep: torch.Tensor) -> None:
+    """Cut every sequence back to its first keep[b] tokens, in place; int32 [B] on the device."""
+    assert keep.dtype == torch.int32 and keep.shape == (cache.B,)
+    _here(cache.k8, keep)
+    _check(lib().akb_truncate(cache.ref(), _ptr(keep), _stream()))
 
 
 def akb_unpack(cache: BlockCache) -> tuple[torch.Tensor, torch.Tensor]:

@@ -9,7 +9,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libakv.so")
 SOURCES = ["akv_api.hip", "akv_append.hip", "akv_decode_split.hip", "akv_decode_head.hip", "akv_fp16.hip", "akw_gemv.hip",
-           "akb_api.hip", "akb_store.hip", "akb_attention.hip", "akb_prompt.hip", "akb_evict.hip"]
+           "akb_api.hip", "akb_store.hip", "akb_attention.hip", "akb_prompt.hip", "akb_evict.hip", "akb_shared.hip", "akb_rotary.hip",
+           "akb_fork.hip"]
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
     "-ffp-contract=off",                                   # the decision path is written op by op; FMAs are explicit

@@ -54,6 +54,45 @@ void sizes_of(const akb_shape& s, akb_sizes* out)
     out->flags = (AKV_NFLAGS + size_t(s.B)) * sizeof(int32_t);
 }
 
+// sequences of shape s that go on from those of f
+bool shares_ok(const akb_shape& f, const akb_shape& s) { return s.B % f.B == 0 && s.Hq == f.Hq && s.Hkv == f.Hkv && s.D == f.D && s.dtype == f.dtype; }
+
+// whether src and dst share memory (scores where dst's is written)
+bool share_memory(const akb_cache& src, const akb_cache& dst)
+{
+    akb_sizes a, b;
+    sizes_of(src.shape, &a);
+    sizes_of(dst.shape, &b);
+    const struct { const void *p; size_t n; } from[] = {{src.k8, a.k8}, {src.v8, a.v8}, {src.exps, a.exps}, {src.k_tail, a.k_tail}, {src.v_tail, a.v_tail}, {src.score, src.score ? a.score : 0}, {src.lens, a.lens}},
+                 to[] = {{dst.k8, b.k8}, {dst.v8, b.v8}, {dst.exps, b.exps}, {dst.k_tail, b.k_tail}, {dst.v_tail, b.v_tail}, {dst.score, dst.score ? b.score : 0}, {dst.lens, b.lens}};
+    for (const auto& x : from)
+        for (const auto& y : to) {
+            const uintptr_t xp = reinterpret_cast<uintptr_t>(x.p), yp = reinterpret_cast<uintptr_t>(y.p);
+            if (x.n && y.n && xp < yp + y.n && yp < xp + x.n) return true;
+        }
+    return false;
+}
+
+// what attention's arguments have to be, whichever caches they are for
+akv_status check_attention(const akb_shape& s, const akb_params& p, const uint16_t* q, const int32_t* n_q, int32_t n, const void* out)
+{
+    if (n < 0 || n > s.Ncap) return fail(AKV_EINVAL, "n = %d out of range 0..Ncap", n);
+    const size_t tiles = size_t(s.B) * s.Hkv * ((size_t(n) * (s.Hq / s.Hkv) + 15) / 16);
+    if (tiles >= (size_t(1) << 24)) return fail(AKV_EINVAL, "%zu tiles of 16 query rows: 2^24 or more", tiles);
+    if (p.out_dtype != 0 && p.out_dtype != 1) return fail(AKV_EINVAL, "out_dtype = %d is neither 0 (f32) nor 1 (the cache's 16-bit type)", p.out_dtype);
+    if (p.max_len < 0 || p.max_len > s.Ncap) return fail(AKV_EINVAL, "max_len = %d out of range 0..Ncap", p.max_len);
+    if (!std::isfinite(p.scale)) return fail(AKV_EINVAL, "scale is not finite");
+    if (n == 0) return AKV_OK;
+    if (!q || !out) return fail(AKV_EINVAL, "q / out is NULL");
+    if (!aligned(q, 16) || !aligned(out, 16) || !aligned(n_q, 4)) return fail(AKV_EINVAL, "q and out must be 16-byte aligned, n_q 4-byte aligned");
+    return AKV_OK;
+}
+float scale_bits(const akb_params& p, int D)
+{
+    const double scale = p.scale > 0.f ? (double)p.scale : 1.0 / std::sqrt((double)D);
+    return (float)(scale * 1.4426950408889634);
+}
+
 }  // namespace
 
 extern "C" {
@@ -109,20 +148,12 @@ akv_status akb_attention(const akb_cache* cache, const uint16_t* q, const int32_
     const akb_shape& s = cache->shape;
     akb_params p = {};
     if (params) p = *params;
-    if (n < 0 || n > s.Ncap) return fail(AKV_EINVAL, "n = %d out of range 0..Ncap", n);
-    const size_t tiles = size_t(s.B) * s.Hkv * ((size_t(n) * (s.Hq / s.Hkv) + 15) / 16);
-    if (tiles >= (size_t(1) << 24)) return fail(AKV_EINVAL, "%zu tiles of 16 query rows: 2^24 or more", tiles);
-    if (p.out_dtype != 0 && p.out_dtype != 1) return fail(AKV_EINVAL, "out_dtype = %d is neither 0 (f32) nor 1 (the cache's 16-bit type)", p.out_dtype);
-    if (p.max_len < 0 || p.max_len > s.Ncap) return fail(AKV_EINVAL, "max_len = %d out of range 0..Ncap", p.max_len);
-    if (!std::isfinite(p.scale)) return fail(AKV_EINVAL, "scale is not finite");
     if (p.accumulate && !cache->score) return fail(AKV_EINVAL, "accumulate is set and the cache has no score");
+    if (akv_status st = check_attention(s, p, q, n_q, n, out)) return st;
     if (n == 0) return AKV_OK;
-    if (!q || !out) return fail(AKV_EINVAL, "q / out is NULL");
-    if (!aligned(q, 16) || !aligned(out, 16) || !aligned(n_q, 4)) return fail(AKV_EINVAL, "q and out must be 16-byte aligned, n_q 4-byte aligned");
     if (akv_status st = check_workspace(workspace, workspace_bytes, akb::attention_workspace(s, n, p.accumulate != 0))) return st;
-    const double scale = p.scale > 0.f ? (double)p.scale : 1.0 / std::sqrt((double)s.D);
     const akb::AttentionArgs a{*cache, q, n_q, n, out, p.out_dtype, p.accumulate != 0, p.max_len > 0 ? p.max_len : s.Ncap,
-                               (float)(scale * 1.4426950408889634), static_cast<char*>(workspace)};
+                               scale_bits(p, s.D), static_cast<char*>(workspace)};
     return hip_result(akb::launch_attention(a, static_cast<hipStream_t>(stream)), "attention launch");
 }
 
@@ -157,20 +188,88 @@ akv_status akb_evict(const akb_cache* src, const akb_cache* dst, int32_t keep, i
     if (!src->score) return fail(AKV_EINVAL, "src has no score");
     if (keep < 1 || keep > d.Ncap) return fail(AKV_EINVAL, "keep = %d out of range 1..dst Ncap", keep);
     if (recent < 0 || recent > keep) return fail(AKV_EINVAL, "recent = %d out of range 0..keep", recent);
-    akb_sizes a, b;
-    sizes_of(s, &a);
-    sizes_of(d, &b);
-    const struct { const void *p; size_t n; } from[] = {{src->k8, a.k8}, {src->v8, a.v8}, {src->exps, a.exps}, {src->k_tail, a.k_tail}, {src->v_tail, a.v_tail}, {src->score, a.score}, {src->lens, a.lens}},
-                 to[] = {{dst->k8, b.k8}, {dst->v8, b.v8}, {dst->exps, b.exps}, {dst->k_tail, b.k_tail}, {dst->v_tail, b.v_tail}, {dst->score, dst->score ? b.score : 0}, {dst->lens, b.lens}};
-    for (const auto& x : from)
-        for (const auto& y : to) {
-            const uintptr_t xp = reinterpret_cast<uintptr_t>(x.p), yp = reinterpret_cast<uintptr_t>(y.p);
-            if (y.n && xp < yp + y.n && yp < xp + x.n) return fail(AKV_EINVAL, "src and dst share memory");
-        }
+    if (share_memory(*src, *dst)) return fail(AKV_EINVAL, "src and dst share memory");
     if (!aligned(kept, 4)) return fail(AKV_EINVAL, "kept must be 4-byte aligned");
     if (akv_status st = check_workspace(workspace, workspace_bytes, akb_evict_workspace(&s, keep))) return st;
     char* ws = static_cast<char*>(workspace) + akv::align256(akb::attention_tickets());   // (what lies in front is attention's between calls)
     return hip_result(akb::launch_evict(*src, *dst, keep, recent, kept, ws, static_cast<hipStream_t>(stream)), "evict launch");
+}
+
+size_t akb_attention_shared_workspace(const akb_shape* prefix, const akb_shape* shape, int32_t n)
+{
+    if (!prefix || !shape || !shape_ok(*prefix) || !shape_ok(*shape) || n < 0 || n > shape->Ncap || !shares_ok(*prefix, *shape)) {
+        fail(AKV_EINVAL, "bad shapes, shapes of caches that do not go together, or n out of range 0..Ncap");
+        return 0;
+    }
+    return akb::shared_workspace(*prefix, *shape, n);
+}
+
+akv_status akb_attention_shared(const akb_cache* prefix, const akb_cache* cache, const uint16_t* q, const int32_t* n_q, int32_t n, void* out,
+                                const akb_params* params, int32_t prefix_max_len, void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (akv_status st = check_cache(prefix)) return st;
+    if (akv_status st = check_cache(cache)) return st;
+    const akb_shape &f = prefix->shape, &s = cache->shape;
+    if (!shares_ok(f, s))
+        return fail(AKV_EINVAL, "prefix and cache do not go together: B %d/%d (the first divides the second), Hq %d/%d, Hkv %d/%d, D %d/%d, dtype %d/%d", f.B, s.B, f.Hq, s.Hq, f.Hkv,
+                    s.Hkv, f.D, s.D, f.dtype, s.dtype);
+    akb_params p = {};
+    if (params) p = *params;
+    if (p.accumulate) return fail(AKV_EINVAL, "accumulate is set: a shared prefix has no scores of one sequence");
+    if (prefix_max_len < 0 || prefix_max_len > f.Ncap) return fail(AKV_EINVAL, "prefix_max_len = %d out of range 0..the prefix's Ncap", prefix_max_len);
+    if (akv_status st = check_attention(s, p, q, n_q, n, out)) return st;
+    if (n == 0) return AKV_OK;
+    if (akv_status st = check_workspace(workspace, workspace_bytes, akb::shared_workspace(f, s, n))) return st;
+    const akb::AttentionArgs a{*cache, q, n_q, n, out, p.out_dtype, 0, p.max_len > 0 ? p.max_len : s.Ncap, scale_bits(p, s.D), static_cast<char*>(workspace)};
+    return hip_result(akb::launch_shared(*prefix, prefix_max_len > 0 ? prefix_max_len : f.Ncap, a, static_cast<hipStream_t>(stream)), "shared attention launch");
+}
+
+akv_status akb_append_rotated(const akb_cache* cache, const akb_tokens* tokens, const int32_t* n_new, int32_t n, uint16_t* q_out, const akb_rotary* rotary,
+                              void* stream)
+{
+    if (akv_status st = check_cache(cache)) return st;
+    if (!tokens || !rotary) return fail(AKV_EINVAL, "tokens / rotary is NULL");
+    const akb_shape& s = cache->shape;
+    const akb_tokens& x = *tokens;
+    const akb_rotary& r = *rotary;
+    if (n < 0 || n > s.Ncap) return fail(AKV_EINVAL, "n = %d out of range 0..Ncap", n);
+    if (r.rot < 0 || r.rot > s.D || r.rot % 16 != 0) return fail(AKV_EINVAL, "rot = %d is no multiple of 16 in 0..D", r.rot);
+    if (r.rot > 0 && !r.inv_freq) return fail(AKV_EINVAL, "inv_freq is NULL");
+    if (r.base && (r.n_base < 1 || s.B % r.n_base != 0)) return fail(AKV_EINVAL, "n_base = %d does not divide B = %d", r.n_base, s.B);
+    if ((r.q_norm || r.k_norm) && !(std::isfinite(r.eps) && r.eps >= 0.f)) return fail(AKV_EINVAL, "eps is negative or not finite");
+    if (n == 0) return AKV_OK;
+    if (!x.k || !x.v) return fail(AKV_EINVAL, "k / v is NULL");
+    if (!x.q != !q_out) return fail(AKV_EINVAL, "one of q and q_out is NULL, the other is not");
+    if (!aligned(x.q, 16) || !aligned(x.k, 16) || !aligned(x.v, 16) || !aligned(q_out, 16) || !aligned(r.q_norm, 16) || !aligned(r.k_norm, 16) || !aligned(r.inv_freq, 4) ||
+        !aligned(r.base, 4) || !aligned(n_new, 4))
+        return fail(AKV_EINVAL, "tokens, q_out and norms must be 16-byte aligned, inv_freq, base and n_new 4-byte aligned");
+    for (const int64_t stride : {x.q_seq, x.q_token, x.k_seq, x.k_token, x.v_seq, x.v_token})
+        if (stride % 8 != 0 || stride < 0) return fail(AKV_EINVAL, "strides must be multiples of 8 elements, not negative");
+    const struct { const uint16_t* p; int64_t seq, token; int heads; } in[] = {{x.q, x.q_seq, x.q_token, s.Hq}, {x.k, x.k_seq, x.k_token, s.Hkv}, {x.v, x.v_seq, x.v_token, s.Hkv}};
+    for (const auto& i : in)
+        if (q_out && i.p < q_out + size_t(s.B) * s.Hq * n * s.D && q_out < i.p + i.seq * (s.B - 1) + i.token * (n - 1) + int64_t(i.heads) * s.D)
+            return fail(AKV_EINVAL, "q_out shares memory with the tokens");
+    return hip_result(akb::launch_append_rotated(*cache, x, n_new, n, q_out, r, static_cast<hipStream_t>(stream)), "append launch");
+}
+
+akv_status akb_fork(const akb_cache* src, const akb_cache* dst, const int32_t* parents, const int32_t* upto, void* stream)
+{
+    if (akv_status st = check_cache(src)) return st;
+    if (akv_status st = check_cache(dst)) return st;
+    const akb_shape &s = src->shape, &d = dst->shape;
+    if (s.Hkv != d.Hkv || s.D != d.D || s.dtype != d.dtype) return fail(AKV_EINVAL, "src and dst differ: Hkv %d/%d, D %d/%d, dtype %d/%d", s.Hkv, d.Hkv, s.D, d.D, s.dtype, d.dtype);
+    if (!parents && s.B != d.B) return fail(AKV_EINVAL, "parents is NULL and src and dst differ: B %d/%d", s.B, d.B);
+    if (!aligned(parents, 4) || !aligned(upto, 4)) return fail(AKV_EINVAL, "parents and upto must be 4-byte aligned");
+    if (share_memory(*src, *dst)) return fail(AKV_EINVAL, "src and dst share memory");
+    return hip_result(akb::launch_fork(*src, *dst, parents, upto, static_cast<hipStream_t>(stream)), "fork launch");
+}
+
+akv_status akb_truncate(const akb_cache* cache, const int32_t* keep, void* stream)
+{
+    if (akv_status st = check_cache(cache)) return st;
+    if (!keep) return fail(AKV_EINVAL, "keep is NULL");
+    if (!aligned(keep, 4)) return fail(AKV_EINVAL, "keep must be 4-byte aligned");
+    return hip_result(akb::launch_truncate(*cache, keep, static_cast<hipStream_t>(stream)), "truncate launch");
 }
 
 akv_status akb_unpack(const akb_cache* cache, uint16_t* k_out, uint16_t* v_out, void* stream)

@@ -29,7 +29,7 @@ struct AttentionPlan {
 };
 // Parts of each of `items` walks: none where they fill the slots, or where a wave has two blocks at most (32 heads, 500 tokens 8.4 / 7.2 us; 1024 tokens in four parts,
 // two, one 7.5 / 9.0 / 9.2); at most 2 slots parts in all, which is what the workspace has room for.
-static long parts_of(long items, long blocks, long slots)
+long parts_of(long items, long blocks, long slots)
 {
     return items >= slots || blocks <= 2 * kWaves ? 1 : std::max(1L, std::min({(slots + items - 1) / items, (blocks + kWaves - 1) / kWaves, 2 * slots / items}));
 }
@@ -603,6 +603,21 @@ __global__ __launch_bounds__(256) void score_join_kernel(RowArgs a, int shares, 
     }
 }
 
+template <class T, int D> static hipError_t join(const RowArgs& r, int group_rows, hipStream_t st)
+{
+    const akb_shape& s = r.c.shape;
+    const int rows_all = r.n * (s.Hq / s.Hkv);
+    auto go = [&](auto kernel, int rows) { hipLaunchKernelGGL(kernel, dim3((rows_all + rows - 1) / rows, s.B * s.Hkv), dim3(256), 0, st, r, group_rows); };
+    if (r.splits && r.splits <= 4) go(join_kernel<T, D, 1>, 1024 / D);
+    else go(join_kernel<T, D, 8>, 128 / D);
+    return hipGetLastError();
+}
+hipError_t launch_join(const RowArgs& r, int group_rows, hipStream_t st)
+{
+    if (r.c.shape.dtype == AKB_FP16) return r.c.shape.D == 64 ? join<Fp16, 64>(r, group_rows, st) : join<Fp16, 128>(r, group_rows, st);
+    return r.c.shape.D == 64 ? join<Bf16, 64>(r, group_rows, st) : join<Bf16, 128>(r, group_rows, st);
+}
+
 template <class T, int D> static hipError_t launch(const RowArgs& r, const AttentionPlan& p, float* sums, int max_len, hipStream_t st)
 {
     const akb_shape& s = r.c.shape;
@@ -618,13 +633,8 @@ template <class T, int D> static hipError_t launch(const RowArgs& r, const Atten
         r.out_dtype == 0 ? rows(rows_kernel<T, D, true, 1, false>) : rows(rows_kernel<T, D, false, 1, false>);
     }
     if (hipError_t e = hipGetLastError()) return e;
-    if (r.splits != 1 && !r.tickets) {
-        const int rows_all = r.n * (s.Hq / s.Hkv);
-        auto join = [&](auto kernel, int rows) { hipLaunchKernelGGL(kernel, dim3((rows_all + rows - 1) / rows, s.B * s.Hkv), dim3(256), 0, st, r, 16 * tiles); };
-        if (r.splits && r.splits <= 4) join(join_kernel<T, D, 1>, 1024 / D);
-        else join(join_kernel<T, D, 8>, 128 / D);
-        if (hipError_t e = hipGetLastError()) return e;
-    }
+    if (r.splits != 1 && !r.tickets)
+        if (hipError_t e = join<T, D>(r, 16 * tiles, st)) return e;
     const int blocks = (max_len + kTB - 1) / kTB;
     if (r.logits) hipLaunchKernelGGL(score_logits_kernel, dim3((blocks + 15) / 16, s.Hkv, s.B), dim3(256), 0, st, r);
     else if (r.stats) {

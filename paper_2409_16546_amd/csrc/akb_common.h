@@ -35,6 +35,13 @@ size_t attention_tickets();   // bytes at the front of a workspace that are zero
 int attention_path(const akb_shape& s, int n, int max_len, int32_t* parts);   // akb_attention_path
 int attention_join(const akb_shape& s, int n, int max_len);                    // akb_attention_join
 hipError_t launch_attention(const AttentionArgs& a, hipStream_t st);
+size_t shared_workspace(const akb_shape& prefix, const akb_shape& s, int n);
+hipError_t launch_shared(const akb_cache& prefix, int prefix_max_len, const AttentionArgs& a, hipStream_t st);
+bool append_ticketed(const akb_shape& s, int n);   // the appends' workgroups move the lengths themselves
+hipError_t launch_append_lens(const akb_cache& c, const int32_t* n_new, int n, hipStream_t st);   // otherwise: behind them
+hipError_t launch_append_rotated(const akb_cache& c, const akb_tokens& x, const int32_t* n_new, int n, uint16_t* q_out, const akb_rotary& r, hipStream_t st);
+hipError_t launch_fork(const akb_cache& src, const akb_cache& dst, const int32_t* parents, const int32_t* upto, hipStream_t st);
+hipError_t launch_truncate(const akb_cache& c, const int32_t* keep, hipStream_t st);
 
 #if defined(__HIPCC__)
 using akv::bits_float;

@@ -89,9 +89,12 @@ template <class T, int D> struct Stage {
     }
 };
 
-template <class T, int D, bool EXACT>
-__global__ __launch_bounds__(64 * kWaves, 2) void prompt_kernel(RowArgs a)
+// Args: RowArgs, or SharedArgs, where a walk goes over the blocks of the prefix and then over the sequence's own (akb_rows.h): which of them a block is one of is the same for
+// the whole workgroup.
+template <class T, int D, bool EXACT, class Args>
+__global__ __launch_bounds__(64 * kWaves, 2) void prompt_kernel(Args a)
 {
+    constexpr bool kShared = std::is_same<Args, SharedArgs>::value;
     __shared__ KLds<D> k_s[2];
     __shared__ VLds<D> v_s[2];
     __shared__ bool large_s[kWaves];
@@ -106,12 +109,19 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prompt_kernel(RowArgs a)
     const int len = seq_len(c, b), m = a.n_q ? min(max(a.n_q[b], 0), n) : n;
     const int row0 = group * kPromptRows, rows = min(kPromptRows, m * G - row0);
     if (rows <= 0) return;
-    const int nb = (max(row_limit(a, row0 + rows - 1, G, m, len), 0) + kTB - 1) / kTB;
+    const int shared = [&] { if constexpr (kShared) return seq_len(a.prefix, b / a.per); else return 0; }();   // tokens of the prefix
+    const int shared_blocks = (shared + kTB - 1) / kTB, gap = shared_blocks * kTB - shared;
+    // the tokens that a row sees, as a place
+    auto limit_of = [&](int row) {
+        const int own = row_limit(a, row, G, m, len);
+        return kShared && row < m * G ? shared + own + (own > 0 ? gap : 0) : own;
+    };
+    const int nb = (max(limit_of(row0 + rows - 1), 0) + kTB - 1) / kTB;
     const int lo = (int)(long(nb) * split / splits), hi = (int)(long(nb) * (split + 1) / splits);
     const int first_row = row0 + wave * kWaveRows, row = first_row + (lane & 31);
     const int wave_rows = min(kWaveRows, row0 + rows - first_row);   // may be below 1: the wave only helps to turn blocks
-    const int all_see = row_limit(a, first_row, G, m, len), most_see = wave_rows > 0 ? row_limit(a, first_row + wave_rows - 1, G, m, len) : 0;
-    const int limit = row_limit(a, row, G, m, len);
+    const int all_see = limit_of(first_row), most_see = wave_rows > 0 ? limit_of(first_row + wave_rows - 1) : 0;
+    const int limit = limit_of(row);
     auto place = [&](int row) { return row_place(a, bh, G, row, D); };   // of a row in q and out
     u32x4_t q[D / 16];
 #pragma unroll
@@ -126,16 +136,34 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prompt_kernel(RowArgs a)
     const size_t block0 = bh * (c.shape.Ncap / kTB);
     const int whole = len / kTB;   // blocks in 8 bits
     const uint16_t *k_tail = c.k_tail + bh * kTB * D, *v_tail = c.v_tail + bh * kTB * D;
+    const size_t shared_bh = [&]() -> size_t { if constexpr (kShared) return size_t(b / a.per) * c.shape.Hkv + bh % c.shape.Hkv; else return 0; }();
+    // Block blk of the walk: where its codes or its tail lie, and its tokens
+    auto in_prefix = [&](int blk) { return kShared && blk < shared_blocks; };
+    auto coded = [&](int blk) { return in_prefix(blk) ? (blk + 1) * kTB <= shared : blk - shared_blocks < whole; };
+    auto left = [&](int blk) { return in_prefix(blk) ? shared - blk * kTB : len - (blk - shared_blocks) * kTB; };
+    auto place_of = [&](int blk) -> size_t {
+        if constexpr (kShared) if (in_prefix(blk)) return shared_bh * (a.prefix.shape.Ncap / kTB) + blk;
+        return block0 + (blk - shared_blocks);
+    };
+    // the prefix's plane, or the sequence's own
+    auto of = [&](int blk, auto mine, auto theirs) { if constexpr (kShared) return in_prefix(blk) ? theirs() : mine(); else return mine(); };
+    auto k8_of = [&](int blk) { return of(blk, [&] { return c.k8; }, [&] { if constexpr (kShared) return a.prefix.k8; else return c.k8; }); };
+    auto v8_of = [&](int blk) { return of(blk, [&] { return c.v8; }, [&] { if constexpr (kShared) return a.prefix.v8; else return c.v8; }); };
+    auto exps_of = [&](int blk) { return of(blk, [&] { return c.exps; }, [&] { if constexpr (kShared) return a.prefix.exps; else return c.exps; }); };
+    auto k_tail_of = [&](int blk) -> const uint16_t* { return of(blk, [&] { return k_tail; }, [&]() -> const uint16_t* { if constexpr (kShared) return a.prefix.k_tail + shared_bh * kTB * D; else return k_tail; }); };
+    auto v_tail_of = [&](int blk) -> const uint16_t* { return of(blk, [&] { return v_tail; }, [&]() -> const uint16_t* { if constexpr (kShared) return a.prefix.v_tail + shared_bh * kTB * D; else return v_tail; }); };
     Stage<T, D> ks, vs;
-    auto fetch_k = [&](int blk) { if (blk < min(hi, whole)) ks.load(c.k8, c.exps, block0 + blk, wave, lane); };
-    auto fetch_v = [&](int blk) { if (blk < min(hi, whole)) vs.load(c.v8, c.exps + 1, block0 + blk, wave, lane); };
+    auto fetch_k = [&](int blk) { if (blk < hi && coded(blk)) ks.load(k8_of(blk), exps_of(blk), place_of(blk), wave, lane); };
+    auto fetch_v = [&](int blk) { if (blk < hi && coded(blk)) vs.load(v8_of(blk), exps_of(blk) + 1, place_of(blk), wave, lane); };
     auto put_k = [&](int blk, KLds<D>& to) {
-        if (blk < min(hi, whole)) ks.store(to, wave, lane);
-        else if (blk < hi) Stage<T, D>::store_tail(k_tail, len - blk * kTB, to, threadIdx.x);
+        if (blk >= hi) return;
+        if (coded(blk)) ks.store(to, wave, lane);
+        else Stage<T, D>::store_tail(k_tail_of(blk), left(blk), to, threadIdx.x);
     };
     auto put_v = [&](int blk, VLds<D>& to) {
-        if (blk < min(hi, whole)) vs.store(to, wave, lane);
-        else if (blk < hi) Stage<T, D>::store_tail(v_tail, len - blk * kTB, to, threadIdx.x);
+        if (blk >= hi) return;
+        if (coded(blk)) vs.store(to, wave, lane);
+        else Stage<T, D>::store_tail(v_tail_of(blk), left(blk), to, threadIdx.x);
     };
     // steps 2 j, 2 j + 1 of the first product of the block in `k`
     auto product = [&](f32x16_t (&s)[2], const KLds<D>& k, int j) {
@@ -157,8 +185,11 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prompt_kernel(RowArgs a)
     fetch_k(lo + 1);
     float unit = kWeightBits;
     if (T::kWide) {   // one unit for the walk: found out here, it costs the loop a scalar register (followed from block to block, 560 us of the prompt above for 541)
-        bool some = hi > whole && Stage<T, D>::large_tail(v_tail, len - whole * kTB, threadIdx.x);
-        for (int blk = lo + int(threadIdx.x); blk < min(hi, whole); blk += 64 * kWaves) some |= c.exps[(block0 + blk) * 2 + 1] >= kLargeExp;
+        auto tail_is_large = [&](int blk) { return blk >= lo && blk < hi && !coded(blk) && Stage<T, D>::large_tail(v_tail_of(blk), left(blk), threadIdx.x); };
+        bool some = tail_is_large(shared_blocks + whole);
+        if (kShared) some |= tail_is_large(shared_blocks - 1);
+        for (int blk = lo + int(threadIdx.x); blk < hi; blk += 64 * kWaves)
+            if (coded(blk)) some |= exps_of(blk)[place_of(blk) * 2 + 1] >= kLargeExp;
         some = __any(some);
         if (lane == 0) large_s[wave] = some;
         lds_barrier();
@@ -177,8 +208,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prompt_kernel(RowArgs a)
         fetch_k(blk + 2);
         fetch_v(blk + 1);
         if (blk * kTB < most_see) {   // some row of the wave sees it
-            if ((blk + 1) * kTB > all_see) {
-                const int seen = limit - blk * kTB - 4 * half;   // counted from the lane's first token
+            const bool partial = kShared && blk == shared_blocks - 1 && gap > 0;   // the prefix's incomplete block
+            if ((blk + 1) * kTB > all_see || partial) {
+                const int seen = (partial ? min(limit, shared) : limit) - blk * kTB - 4 * half;   // counted from the lane's first token
 #pragma unroll
                 for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -270,16 +302,18 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prompt_kernel(RowArgs a)
         }
 }
 
-template <class T, int D> static void launch(const RowArgs& r, int grid, hipStream_t st)
+template <class T, int D, class Args> static hipError_t launch(const Args& r, int grid, hipStream_t st)
 {
     auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(akv::xcd_grid(grid)), dim3(64 * kWaves), 0, st, r); };
-    r.out_dtype == 0 ? go(prompt_kernel<T, D, true>) : go(prompt_kernel<T, D, false>);
-}
-hipError_t launch_prompt(const RowArgs& r, int grid, hipStream_t st)
-{
-    if (r.c.shape.dtype == AKB_FP16) r.c.shape.D == 64 ? launch<Fp16, 64>(r, grid, st) : launch<Fp16, 128>(r, grid, st);
-    else r.c.shape.D == 64 ? launch<Bf16, 64>(r, grid, st) : launch<Bf16, 128>(r, grid, st);
+    r.out_dtype == 0 ? go(prompt_kernel<T, D, true, Args>) : go(prompt_kernel<T, D, false, Args>);
     return hipGetLastError();
 }
+template <class Args> static hipError_t launch_typed(const Args& r, int grid, hipStream_t st)
+{
+    if (r.c.shape.dtype == AKB_FP16) return r.c.shape.D == 64 ? launch<Fp16, 64>(r, grid, st) : launch<Fp16, 128>(r, grid, st);
+    return r.c.shape.D == 64 ? launch<Bf16, 64>(r, grid, st) : launch<Bf16, 128>(r, grid, st);
+}
+hipError_t launch_prompt(const RowArgs& r, int grid, hipStream_t st) { return launch_typed(r, grid, st); }
+hipError_t launch_prompt_shared(const SharedArgs& r, int grid, hipStream_t st) { return launch_typed(r, grid, st); }
 
 }  // namespace akb

@@ -40,6 +40,13 @@ struct RowArgs {
     float *parts, *logits, *stats;   // logits: q . k of the one row group, [sequence, KV head][block][tile][row][16]; stats: (maximum, 1 / sum) per row; or NULL
 };
 
+// Sequences that go on from shared ones: sequence b from sequence b / per of `prefix`.  In a walk over both the prefix's blocks come first: token t of a sequence's own stands at
+// place 64 ceil(P / 64) + t, and the places between P and there are nobody's.
+struct SharedArgs : RowArgs {
+    akb_cache prefix;
+    int per;
+};
+
 #if defined(__HIPCC__)
 // the unit of the weights
 template <class T> __device__ __forceinline__ float weight_bits(bool large) { return T::kWide && large ? kSmallWeightBits : kWeightBits; }
@@ -174,5 +181,9 @@ struct Joined {
 #endif
 
 hipError_t launch_prompt(const RowArgs& r, int grid, hipStream_t st);   // row groups of kPromptRows
+hipError_t launch_prompt_shared(const SharedArgs& r, int grid, hipStream_t st);
+hipError_t launch_join(const RowArgs& r, int group_rows, hipStream_t st);   // the parts of every walk put together by a launch
+// Parts of each of `items` walks over `blocks` blocks, of which `slots` run at a time
+long parts_of(long items, long blocks, long slots);
 
 }  // namespace akb

@@ -86,16 +86,28 @@ __global__ __launch_bounds__(256) void append_lens_kernel(akb_cache c, const int
     }
 }
 
+// Who moves the lengths of an append of n tokens: the workgroups' tickets, or a launch behind.
+// A ticket per workgroup or a launch behind, us of calls one after the other.  One block per head, where the workgroups arrive as they were launched: 512 workgroups of 64
+// sequences 6.0 / 8.3 and of 16 sequences 7.9 / 8.3, 640 of 80 and of 20 sequences 6.2 / 8.2 and 8.3 / 8.3, 768 of 96 and of 24 6.3 / 8.3 and 10.2 / 8.3, 1024 7.1 / 8.1
+// and 11.8 / 8.1.  Several blocks: 96 workgroups 8.2 / 10.3, 192 9.4 / 10.4, 272 11.0 / 11.6, 288 11.7 / 11.6, 384 10.8 / 10.3 and 13.1 / 11.6, 576 15.7 / 11.7.  (Of one side
+// per workgroup they would be twice as many, and gain nothing: 8 x 8 pairs 8192 tokens 77 us.)
+bool append_ticketed(const akb_shape& s, int n)
+{
+    const int blocks = (kTB - 1 + n + kTB - 1) / kTB;
+    return long(blocks) * s.Hkv * s.B <= (blocks == 1 ? 640 : 288);
+}
+hipError_t launch_append_lens(const akb_cache& c, const int32_t* n_new, int n, hipStream_t st)
+{
+    hipLaunchKernelGGL(append_lens_kernel, dim3(1), dim3(256), 0, st, c, n_new, n);
+    return hipGetLastError();
+}
+
 hipError_t launch_append(const akb_cache& c, const uint16_t* k_new, const uint16_t* v_new, const int32_t* n_new, int n, hipStream_t st)
 {
     if (n == 0) return hipSuccess;
     const int blocks = (kTB - 1 + n + kTB - 1) / kTB;
     const dim3 grid(blocks, c.shape.Hkv, c.shape.B);
-    // A ticket per workgroup or a launch behind, us of calls one after the other.  One block per head, where the workgroups arrive as they were launched: 512 workgroups of 64
-    // sequences 6.0 / 8.3 and of 16 sequences 7.9 / 8.3, 640 of 80 and of 20 sequences 6.2 / 8.2 and 8.3 / 8.3, 768 of 96 and of 24 6.3 / 8.3 and 10.2 / 8.3, 1024 7.1 / 8.1
-    // and 11.8 / 8.1.  Several blocks: 96 workgroups 8.2 / 10.3, 192 9.4 / 10.4, 272 11.0 / 11.6, 288 11.7 / 11.6, 384 10.8 / 10.3 and 13.1 / 11.6, 576 15.7 / 11.7.  (Of one side
-    // per workgroup they would be twice as many, and gain nothing: 8 x 8 pairs 8192 tokens 77 us.)
-    const bool ticketed = long(grid.x) * grid.y * grid.z <= (blocks == 1 ? 640 : 288);
+    const bool ticketed = append_ticketed(c.shape, n);
     auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(2 * c.shape.D), 0, st, c, k_new, v_new, n_new, n, ticketed ? 1 : 0); };
     // New tokens that are more than half of the last-level cache are read and their codes stored with the non-temporal hint; fewer may still lie there as they were
     // made, and their codes are wanted there next.  Plain / with the hint: 8 x 8 pairs 8192 tokens (268 MB) 76.7 / 68.8 us, 6 x 32 pairs up to 777 tokens (76 MB at most, read again and again) 28.9 / 33.8.
@@ -104,8 +116,7 @@ hipError_t launch_append(const akb_cache& c, const uint16_t* k_new, const uint16
     if (c.shape.dtype == AKB_FP16) c.shape.D == 64 ? pick(append_kernel<Fp16, 64, false>, append_kernel<Fp16, 64, true>) : pick(append_kernel<Fp16, 128, false>, append_kernel<Fp16, 128, true>);
     else c.shape.D == 64 ? pick(append_kernel<Bf16, 64, false>, append_kernel<Bf16, 64, true>) : pick(append_kernel<Bf16, 128, false>, append_kernel<Bf16, 128, true>);
     if (hipError_t e = hipGetLastError()) return e;
-    if (!ticketed) hipLaunchKernelGGL(append_lens_kernel, dim3(1), dim3(256), 0, st, c, n_new, n);
-    return hipGetLastError();
+    return ticketed ? hipSuccess : launch_append_lens(c, n_new, n, st);
 }
 
 // The append of a block backwards: one workgroup of 2 D threads per (block, side, KV head, sequence).
