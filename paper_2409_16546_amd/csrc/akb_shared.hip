@@ -1,38 +1,298 @@
 // Attention of sequences that go on from shared ones (rules and layout: include/akb.h; rows and parts: akb_rows.h).
-#include "akb_rows.h"
+//
+// Few rows per sequence: the rows of all sequences of a prefix are the rows of one walk over it (a step of 64 sequences with four heads per KV head: 256 rows that read a
+// prefix once instead of 64 times four), each sequence's own tokens are a walk of their own, and a launch behind puts a row's parts of both together.  Both kinds of
+// walk are workgroups of one launch, those over prefixes first.
+// Many rows per sequence (chunks behind a document): one walk over the prefix's blocks and the own ones, by the prompt kernel.  Its products are what takes time, and
+// they do not get fewer by sharing.
+#include "akb_prompt_walk.h"
+#include "akb_rows_walk.h"
 
 namespace akb {
 
-// One walk per (sequence, KV head, row group of 128) over the prefix and the sequence's own blocks, cut where the walks are few.
-struct SharedPlan {
-    int groups, splits;
-    size_t parts, total;   // offset into the workspace, its size
+// One kind of walk: over prefixes (the rows of `per` sequences) or over the sequences' own tokens (per = 1)
+struct Side {
+    akb_cache c;
+    int per, groups, splits;
+    float* parts;   // [pair][row group][split]
 };
+struct StepArgs {
+    Side side[2];       // prefix, own
+    unsigned items;     // workgroups of side 0
+    const uint16_t* q;
+    const int32_t* n_q;
+    int n, G, out_dtype;
+    void* out;
+    float c2;
+};
+// rows of a row group of TILES tiles (8: the prompt walk)
+constexpr int tile_rows(int tiles) { return 16 * tiles; }
+
+// A row of a side: sequence of the batch, query token, head of the group
+struct StepRow {
+    int b, token, head;
+    __device__ __forceinline__ StepRow(const StepArgs& a, const Side& s, int first_b, int row)
+    {
+        const int per_seq = a.n * a.G, j = s.per == 1 ? 0 : row / per_seq, r = row - j * per_seq;
+        b = first_b + j;
+        token = r / a.G;
+        head = r - token * a.G;
+    }
+};
+__device__ __forceinline__ int queries(const StepArgs& a, int b) { return a.n_q ? min(max(a.n_q[b], 0), a.n) : a.n; }
+
+template <class T, int D, bool EXACT, int TILES, bool PREFIX>
+__device__ __forceinline__ void step_walk(const StepArgs& a, unsigned item, char* lds)
+{
+    const Side& s = a.side[PREFIX ? 0 : 1];
+    const akb_cache& c = s.c;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const unsigned per_pair = s.groups * s.splits, pair = item / per_pair, in_pair = item - pair * per_pair;
+    const int split = in_pair / s.groups, group = in_pair - split * s.groups;   // (the row groups of a part beside each other: they read the same blocks)
+    const int p = pair / c.shape.Hkv, h = pair - p * c.shape.Hkv, first_b = p * s.per;
+    const int len = seq_len(c, p), row0 = group * tile_rows(TILES), all_rows = s.per * a.n * a.G;
+    const akb_cache& own = a.side[1].c;
+    int keys = len;
+    if (!PREFIX) {   // (of one sequence: the row groups behind its last row have nothing to do)
+        const int m = queries(a, first_b);
+        if (row0 >= m * a.G) return;
+        const StepRow last(a, s, first_b, min(row0 + tile_rows(TILES), m * a.G) - 1);
+        keys = max(len - m + last.token + 1, 0);
+    }
+    const int nb = (keys + kTB - 1) / kTB, lo = (int)(long(nb) * split / s.splits), hi = (int)(long(nb) * (split + 1) / s.splits);
+    // where a row's query lies (NULL: nobody's), and the tokens that it sees
+    auto row_of = [&](int row, int& limit) -> const uint16_t* {
+        limit = PREFIX ? len : 0;   // (a row that nobody wants: no mask on its account)
+        if (row >= all_rows) return nullptr;
+        const StepRow r(a, s, first_b, row);
+        const int m = queries(a, r.b);
+        if (r.token >= m) return nullptr;
+        limit = PREFIX ? len + min(0, seq_len(own, r.b) - m + r.token + 1) : len - m + r.token + 1;
+        return a.q + ((size_t(r.b) * c.shape.Hkv * a.G + h * a.G + r.head) * a.n + r.token) * D;
+    };
+    float* part = s.parts + (size_t(pair * s.groups + group) * s.splits + split) * part_floats(tile_rows(TILES), D);
+    if constexpr (TILES <= 2) {
+        float(*o_s)[kTileRows][D + 4] = reinterpret_cast<float(*)[kTileRows][D + 4]>(lds);
+        float(*m_s)[kTileRows] = reinterpret_cast<float(*)[kTileRows]>(lds + sizeof(float) * kWaves * kTileRows * (D + 4));
+        float(*z_s)[kTileRows] = m_s + kWaves;
+        RowState<T, D> st[TILES];
+        int all_see = len;
+#pragma unroll
+        for (int k = 0; k < TILES; ++k) {
+            int limit;
+            const uint16_t* q = row_of(row0 + 16 * k + (lane & 15), limit);
+            st[k].init(q, limit, lane);
+            if (__any(limit < len)) all_see = 0;
+        }
+        walk_rows<T, D, EXACT, TILES, false>(c, pair, st, lo, hi, len, all_see, a.c2, lane, wave, nullptr, 0);
+        const int rows = min(tile_rows(TILES), all_rows - row0);
+#pragma unroll
+        for (int k = 0; k < TILES; ++k) {
+            if (16 * k >= rows) break;
+            if (k) __syncthreads();   // the tile before has been put together
+            const float z = akv::add_lane32(akv::add_lane16(st[k].z));
+            if (lane < 16) {
+                m_s[wave][lane] = st[k].m;
+                z_s[wave][lane] = z;
+            }
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i) *reinterpret_cast<f32x4_t*>(&o_s[wave][lane & 15][16 * i + 4 * (lane >> 4)]) = st[k].o[i];
+            __syncthreads();
+            for (int e = threadIdx.x; e < min(16, rows - 16 * k) * (D / 4); e += 64 * kWaves) {   // four channels of a row
+                const int r = e / (D / 4), d = e % (D / 4) * 4;
+                Joined j;
+                j.top = m_s[0][r];
+#pragma unroll
+                for (int w = 1; w < kWaves; ++w) j.top = fmaxf(j.top, m_s[w][r]);
+                const float base = j.top == -__builtin_inff() ? 0.f : j.top;
+#pragma unroll
+                for (int w = 0; w < kWaves; ++w) {
+                    const float f = __builtin_amdgcn_exp2f(m_s[w][r] - base);
+                    j.z = fmaf(z_s[w][r], f, j.z);
+                    j.o += *reinterpret_cast<const f32x4_t*>(&o_s[w][r][d]) * f;
+                }
+                *reinterpret_cast<f32x4_t*>(part + part_head(tile_rows(TILES)) + (16 * k + r) * D + d) = j.o;
+                if (d == 0) {
+                    part[2 * (16 * k + r)] = j.top;
+                    part[2 * (16 * k + r) + 1] = j.z;
+                }
+            }
+        }
+    } else {
+        const int half = lane >> 5, r = wave * kWaveRows + (lane & 31);
+        int limit;
+        const uint16_t* row = row_of(row0 + r, limit);
+        u32x4_t q[D / 16];
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) q[i] = row ? *reinterpret_cast<const u32x4_t*>(row + 16 * i + 8 * half) : u32x4_t{0, 0, 0, 0};
+        const int all_see = __any(limit < len) ? 0 : len, most_see = row0 + wave * kWaveRows < all_rows ? len : 0;
+        f32x16_t o[D / 32];
+        float top, z;
+        walk_prompt<T, D, EXACT>(*reinterpret_cast<PromptLds<D>*>(lds), OneSequence<D>(c, pair, len), lo, hi, q, limit, all_see, most_see, a.c2, wave, lane, o, top, z);
+        if (row0 + r >= all_rows) return;
+        z = akv::add_lane32(z);
+        if (half == 0) {
+            part[2 * r] = top;
+            part[2 * r + 1] = z;
+        }
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                *reinterpret_cast<f32x4_t*>(part + part_head(tile_rows(TILES)) + r * D + 32 * i + 8 * k + 4 * half) = f32x4_t{o[i][4 * k], o[i][4 * k + 1], o[i][4 * k + 2], o[i][4 * k + 3]};
+    }
+}
+
+template <class T, int D, bool EXACT, int PREFIX_TILES, int OWN_TILES>
+__global__ __launch_bounds__(64 * kWaves, 2) void step_kernel(StepArgs a)
+{
+    constexpr size_t kRowsLds = sizeof(float) * kWaves * kTileRows * (D + 4 + 2), kLds = PREFIX_TILES > 2 ? std::max(sizeof(PromptLds<D>), kRowsLds) : kRowsLds;
+    __shared__ __align__(16) char lds[kLds];
+    // the walks of a (sequence, KV head) of the prefix on one XCD, whose L2 they share, where the pairs are a multiple of the XCDs
+    unsigned w = blockIdx.x;
+    if (w < a.items) {
+        const unsigned pairs = a.side[0].c.shape.B * a.side[0].c.shape.Hkv, per_pair = a.side[0].groups * a.side[0].splits;
+        if (pairs % akv::kXcds == 0) {
+            const unsigned x = w % akv::kXcds, i = w / akv::kXcds;
+            w = (x + akv::kXcds * (i / per_pair)) * per_pair + i % per_pair;
+        }
+        step_walk<T, D, EXACT, PREFIX_TILES, true>(a, w, lds);
+    } else {
+        step_walk<T, D, EXACT, OWN_TILES, false>(a, w - a.items, lds);
+    }
+}
+
+// A row's parts of both sides put together: a thread has four channels of a row in every `SLICES`-th part, a workgroup kRows rows of a (sequence, KV head) per turn.
+template <class T, int D, int SLICES>
+__global__ __launch_bounds__(256) void step_join_kernel(StepArgs a, int prefix_rows, int own_rows, unsigned turns, unsigned per_pair)
+{
+    constexpr int kRun = D / 4, kRows = 256 / (kRun * SLICES);
+    __shared__ float x_s[256][6];
+    const int tid = threadIdx.x, per_seq = a.n * a.G;
+    const int Hkv = a.side[1].c.shape.Hkv;
+    for (unsigned turn = blockIdx.x; turn < turns; turn += gridDim.x) {
+        const unsigned pair = turn / per_pair, first = (turn - pair * per_pair) * kRows;
+        const int b = pair / Hkv, h = pair - b * Hkv, m = queries(a, b);
+        if (int(first) >= m * a.G) continue;
+        const int row = first + tid / (kRun * SLICES), slice = tid / kRun % SLICES, d = tid % kRun * 4;
+        Joined j;
+        if (row < m * a.G) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const Side& s = a.side[i];
+                const int tile = i == 0 ? prefix_rows : own_rows, p = b / s.per, at = row + (b - p * s.per) * per_seq, group = at / tile, r = at - group * tile;
+                const float* parts = s.parts + size_t((size_t(p) * Hkv + h) * s.groups + group) * s.splits * part_floats(tile, D);
+#pragma unroll 4
+                for (int k = slice; k < s.splits; k += SLICES) {
+                    const float* x = parts + size_t(k) * part_floats(tile, D);
+                    j.add(x[2 * r], x[2 * r + 1], *reinterpret_cast<const f32x4_t*>(x + part_head(tile) + r * D + d));
+                }
+            }
+        }
+        if (SLICES > 1) {
+            j.put(x_s[tid]);
+            __syncthreads();
+            if (slice == 0)
+                for (int s = 1; s < SLICES; ++s) j.add(x_s[tid + s * kRun]);
+            __syncthreads();   // (the next turn writes there)
+        }
+        if (row >= m * a.G || slice) continue;
+        const int token = row / a.G, head = row - token * a.G;
+        const float inv = j.z == 0.f ? 0.f : 1.f / j.z;   // zero: the row sees nothing
+        store_row<T>(a.out, a.out_dtype, ((size_t(pair) * a.G + head) * a.n + token) * D + d, j.o * inv);
+    }
+}
+
+// How a call is cut.
+struct SharedPlan {
+    bool one_walk;              // prefix and own blocks by one walk
+    int tiles[2], groups[2], splits[2];
+    size_t parts[2], total;     // offsets into the workspace, its size
+};
+constexpr int kOneWalkRows = 96;   // of a sequence, from which on one walk goes over both
 static SharedPlan plan(const akb_shape& f, const akb_shape& s, int n, int max_len, int prefix_max_len)
 {
-    SharedPlan p;
-    const long slots = 2L * akv::compute_units(), rows = long(n) * (s.Hq / s.Hkv), pairs = long(s.B) * s.Hkv;
-    const long blocks = (prefix_max_len + kTB - 1) / kTB + (max_len + kTB - 1) / kTB;
-    p.groups = int((rows + kPromptRows - 1) / kPromptRows);
-    p.splits = int(parts_of(pairs * p.groups, blocks, slots));
-    p.parts = align256(attention_tickets());
-    p.total = p.parts + align256(size_t(2 * slots) * part_floats((int)std::min(rows, long(kPromptRows)), s.D) * sizeof(float));
+    SharedPlan p = {};
+    const int per = s.B / f.B;
+    const long slots = 2L * akv::compute_units(), seq_rows = long(n) * (s.Hq / s.Hkv);
+    const long blocks[2] = {(prefix_max_len + kTB - 1) / kTB, (max_len + kTB - 1) / kTB}, pairs[2] = {long(f.B) * s.Hkv, long(s.B) * s.Hkv}, rows[2] = {per * seq_rows, seq_rows};
+    p.one_walk = seq_rows >= kOneWalkRows;
+    size_t at = align256(attention_tickets());
+    if (p.one_walk) {
+        p.groups[1] = int((seq_rows + kPromptRows - 1) / kPromptRows);
+        p.splits[1] = int(parts_of(pairs[1] * p.groups[1], blocks[0] + blocks[1], slots));
+        p.parts[1] = at;
+        p.total = at + align256(size_t(2 * slots) * part_floats((int)std::min(seq_rows, long(kPromptRows)), s.D) * sizeof(float));
+        return p;
+    }
+    for (int i = 0; i < 2; ++i) {
+        constexpr int kPromptTiles = kPromptRows / 16;
+        const long prompt_items = pairs[i] * ((rows[i] + kPromptRows - 1) / kPromptRows);
+        p.tiles[i] = rows[i] <= 16 && i == 1 ? 1 : (i == 0 && rows[i] > 64 && blocks[i] >= 12 * parts_of(prompt_items, blocks[i], slots) ? kPromptTiles : 2);
+        p.groups[i] = int((rows[i] + tile_rows(p.tiles[i]) - 1) / tile_rows(p.tiles[i]));
+        p.splits[i] = int(parts_of(pairs[i] * p.groups[i], blocks[i], slots));
+        p.parts[i] = at;
+        at += align256(size_t(pairs[i]) * p.groups[i] * p.splits[i] * part_floats(tile_rows(p.tiles[i]), s.D) * sizeof(float));
+    }
+    p.total = at;
     return p;
 }
-size_t shared_workspace(const akb_shape& f, const akb_shape& s, int n) { return plan(f, s, std::max(n, 1), s.Ncap, f.Ncap).total; }
+// For calls of up to n query tokens: no kind of call needs more than this, whatever its number of tokens up to n and its bounds of the lengths.  Parts of walks that are
+// cut are at most 2 slots, of 128 rows or fewer; a walk that is not cut has its rows, filled up to a row group.
+size_t shared_workspace(const akb_shape& f, const akb_shape& s, int n)
+{
+    const size_t slots = 2 * size_t(akv::compute_units()), G = s.Hq / s.Hkv, per = s.B / f.B;
+    const size_t seq_rows = std::min(size_t(std::max(n, 1)) * G, size_t(kOneWalkRows));   // (beyond, no more is needed)
+    size_t total = align256(attention_tickets());
+    const size_t pairs[2] = {size_t(f.B) * s.Hkv, size_t(s.B) * s.Hkv}, rows[2] = {per * seq_rows, seq_rows};
+    for (int i = 0; i < 2; ++i) {
+        const size_t cut = 2 * slots * part_floats(kPromptRows, s.D), whole = pairs[i] * ((rows[i] + kPromptRows - 1) / kPromptRows) * part_floats(kPromptRows, s.D);
+        total += align256(std::max(cut, whole) * sizeof(float));
+    }
+    return total;
+}
+
+template <class T, int D> static hipError_t launch(const StepArgs& a, const SharedPlan& p, unsigned items, hipStream_t st)
+{
+    auto go = [&](auto f32, auto b16) {
+        if (a.out_dtype == 0) hipLaunchKernelGGL(f32, dim3(items), dim3(64 * kWaves), 0, st, a);
+        else hipLaunchKernelGGL(b16, dim3(items), dim3(64 * kWaves), 0, st, a);
+    };
+    if (p.tiles[0] == 2 && p.tiles[1] == 1) go(step_kernel<T, D, true, 2, 1>, step_kernel<T, D, false, 2, 1>);
+    else if (p.tiles[0] == 2) go(step_kernel<T, D, true, 2, 2>, step_kernel<T, D, false, 2, 2>);
+    else if (p.tiles[1] == 1) go(step_kernel<T, D, true, 8, 1>, step_kernel<T, D, false, 8, 1>);
+    else go(step_kernel<T, D, true, 8, 2>, step_kernel<T, D, false, 8, 2>);
+    if (hipError_t e = hipGetLastError()) return e;
+    auto join = [&](auto kernel, int rows) {
+        const unsigned per_pair = (a.n * a.G + rows - 1) / rows, turns = per_pair * a.side[1].c.shape.B * a.side[1].c.shape.Hkv;
+        hipLaunchKernelGGL(kernel, dim3(std::min(turns, 1u << 20)), dim3(256), 0, st, a, tile_rows(p.tiles[0]), tile_rows(p.tiles[1]), turns, per_pair);
+    };
+    if (p.splits[0] + p.splits[1] <= 8) join(step_join_kernel<T, D, 1>, 1024 / D);
+    else join(step_join_kernel<T, D, 8>, 128 / D);
+    return hipGetLastError();
+}
 
 hipError_t launch_shared(const akb_cache& prefix, int prefix_max_len, const AttentionArgs& a, hipStream_t st)
 {
     const akb_shape& s = a.c.shape;
     const SharedPlan p = plan(prefix.shape, s, a.n, a.max_len, prefix_max_len);
-    const int G = s.Hq / s.Hkv, grid = s.B * s.Hkv * p.groups * p.splits;
-    SharedArgs r;
-    static_cast<RowArgs&>(r) = RowArgs{a.c, a.q, a.n_q, a.n, p.groups, p.splits, grid, a.out_dtype, a.out, a.c2, uint32_t(G > 1 ? ((uint64_t(1) << 32) + G - 1) / G : 0), nullptr,
-                                       reinterpret_cast<float*>(a.ws + p.parts), nullptr, nullptr};
-    r.prefix = prefix;
-    r.per = s.B / prefix.shape.B;
-    if (hipError_t e = launch_prompt_shared(r, grid, st)) return e;
-    return p.splits > 1 ? launch_join(r, kPromptRows, st) : hipSuccess;
+    const int G = s.Hq / s.Hkv, per = s.B / prefix.shape.B;
+    if (p.one_walk) {
+        const int grid = s.B * s.Hkv * p.groups[1] * p.splits[1];
+        SharedArgs r;
+        static_cast<RowArgs&>(r) = RowArgs{a.c, a.q, a.n_q, a.n, p.groups[1], p.splits[1], grid, a.out_dtype, a.out, a.c2, uint32_t(G > 1 ? ((uint64_t(1) << 32) + G - 1) / G : 0), nullptr,
+                                           reinterpret_cast<float*>(a.ws + p.parts[1]), nullptr, nullptr};
+        r.prefix = prefix;
+        r.per = per;
+        if (hipError_t e = launch_prompt_shared(r, grid, st)) return e;
+        return p.splits[1] > 1 ? launch_join(r, kPromptRows, st) : hipSuccess;
+    }
+    auto side = [&](int i, const akb_cache& c, int per) { return Side{c, per, p.groups[i], p.splits[i], reinterpret_cast<float*>(a.ws + p.parts[i])}; };
+    StepArgs r{{side(0, prefix, per), side(1, a.c, 1)}, 0, a.q, a.n_q, a.n, G, a.out_dtype, a.out, a.c2};
+    r.items = unsigned(prefix.shape.B) * s.Hkv * p.groups[0] * p.splits[0];
+    const unsigned items = r.items + unsigned(s.B) * s.Hkv * p.groups[1] * p.splits[1];
+    if (s.dtype == AKB_FP16) return s.D == 64 ? launch<Fp16, 64>(r, p, items, st) : launch<Fp16, 128>(r, p, items, st);
+    return s.D == 64 ? launch<Bf16, 64>(r, p, items, st) : launch<Bf16, 128>(r, p, items, st);
 }
 
 }  // namespace akb
