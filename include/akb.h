@@ -167,7 +167,7 @@ size_t akb_attention_shared_workspace(const akb_shape *prefix, const akb_shape *
 akv_status akb_attention_shared(const akb_cache *prefix, const akb_cache *cache, const uint16_t *q, const int32_t *n_q, int32_t n, void *out,
                                 const akb_params *params, int32_t prefix_max_len, void *workspace, size_t workspace_bytes, void *stream);
 
-/* How keys and queries are normed and turned (above).  Weights and norms are applied in binary32, angles are made in binary64, each result is rounded once. */
+/* How keys and queries are normed and turned (above): with angles made in binary64, keys in binary64 and queries in binary32, each result rounded once, to the 16-bit type. */
 typedef struct akb_rotary {
     const uint16_t *q_norm, *k_norm; /* device [D] of the shape's type: w; NULL: not normed (each by itself)               */
     const float *inv_freq;           /* device [rot / 2]                                                                   */
@@ -189,8 +189,8 @@ typedef struct akb_tokens {
 /*
  * Append tokens as projections give them: k is normed and turned and stored, and v stored, as akb_append stores them; q is normed and turned by the same places
  * and goes to q_out, device [B][Hq][n][D], which is what akb_attention takes.  q and q_out may both be NULL.  n_new: as for akb_append; rows of q_out behind
- * n_new[b], and all of a sequence that is refused, are left as they were.  q_out shares no memory with the inputs.  Not finite inputs: as for akb_append; a NaN of a
- * token reaches the whole of its head where it is normed, and its partner where it is turned.
+ * n_new[b], and all of a sequence that is refused, are left as they were.  q_out shares no memory with the inputs.  Not finite inputs: as for akb_append; one
+ * reaches the whole of its token's head where that is normed, and its partner where it is turned.
  */
 akv_status akb_append_rotated(const akb_cache *cache, const akb_tokens *tokens, const int32_t *n_new, int32_t n, uint16_t *q_out, const akb_rotary *rotary,
                               void *stream);

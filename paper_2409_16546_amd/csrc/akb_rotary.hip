@@ -1,4 +1,9 @@
 // Tokens from a model's projections into the block-scaled 8-bit cache: norms per head, rotary positions, the append (rules and layout: include/akb.h).
+//
+// Keys are normed and turned in 64 bits and rounded once, to the 16-bit type: their largest number decides a block's exponent, and a number next to a border would get another
+// code where 32 bits round twice.  Queries are normed and turned in 32 bits, by the same angles.
+// A row (a token of a head) lies in D / 8 lanes, eight channels in each; a workgroup has a block's 64 tokens, 16 rows at a time.  Sine and cosine are made by their power series
+// for a thread's first token (half of them by the lane of the other channels of the pairs), and turned on by 16 tokens, in 64 bits, for the next.
 #include "akb_pack.h"
 
 namespace akb {
@@ -11,122 +16,126 @@ struct TurnArgs {
     int n;
     uint16_t* q_out;
     int ticketed;
+    int apart;   // the query heads of a KV head have a workgroup of their own
 };
+typedef double f64x2_t __attribute__((ext_vector_type(2)));
 
-// sin and cos of place x freq.  The angle is made and brought into +-pi/4 in 64 bits (a place of 10^6 leaves 32 bits no digits behind the point), then the sums
-// of their power series, cut where the next term is below 2^-28.
-__device__ __forceinline__ void sin_cos(double place, float freq, float& s, float& c)
+// cos, sin of place x freq: the angle brought into +-pi/4 (pi / 2 in two parts), then the sums of the power series, cut where the next term is below 2^-50.
+__device__ __forceinline__ f64x2_t cos_sin(double place, float freq)
 {
     constexpr double kTwoOverPi = 0.63661977236758134308, kHalfPi = 1.57079632679489661923, kHalfPiRest = 6.123233995736766e-17;
-    const double u = place * double(freq), k = __builtin_rint(u * kTwoOverPi);
-    const float r = float(fma(-k, kHalfPiRest, fma(-k, kHalfPi, u))), r2 = r * r;
+    const double u = place * double(freq), k = __builtin_rint(u * kTwoOverPi), r = fma(-k, kHalfPiRest, fma(-k, kHalfPi, u)), r2 = r * r;
     const int quarter = int(k - 4.0 * __builtin_floor(k * 0.25));
-    float a = fmaf(r2, 1.f / 362880.f, -1.f / 5040.f);
-    a = fmaf(r2, a, 1.f / 120.f);
-    a = fmaf(r2, a, -1.f / 6.f);
-    a = fmaf(r * r2, a, r);
-    float b = fmaf(r2, -1.f / 3628800.f, 1.f / 40320.f);
-    b = fmaf(r2, b, -1.f / 720.f);
-    b = fmaf(r2, b, 1.f / 24.f);
-    b = fmaf(r2, b, -0.5f);
-    b = fmaf(r2, b, 1.f);
-    const float p = quarter & 1 ? b : a, q = quarter & 1 ? a : b;
-    s = quarter & 2 ? -p : p;
-    c = (quarter + 1) & 2 ? -q : q;
+    double a = 1.0 / 1307674368000.0, b = 1.0 / 20922789888000.0;   // -r^15 / 15!, r^16 / 16!
+    a = fma(r2, -a, 1.0 / 6227020800.0);
+    a = fma(r2, a, -1.0 / 39916800.0);
+    a = fma(r2, a, 1.0 / 362880.0);
+    a = fma(r2, a, -1.0 / 5040.0);
+    a = fma(r2, a, 1.0 / 120.0);
+    a = fma(r2, a, -1.0 / 6.0);
+    a = fma(r * r2, a, r);
+    b = fma(r2, b, -1.0 / 87178291200.0);
+    b = fma(r2, b, 1.0 / 479001600.0);
+    b = fma(r2, b, -1.0 / 3628800.0);
+    b = fma(r2, b, 1.0 / 40320.0);
+    b = fma(r2, b, -1.0 / 720.0);
+    b = fma(r2, b, 1.0 / 24.0);
+    b = fma(r2, b, -0.5);
+    b = fma(r2, b, 1.0);
+    const double s = quarter & 1 ? b : a, c = quarter & 1 ? a : b;
+    return f64x2_t{(quarter + 1) & 2 ? -c : c, quarter & 2 ? -s : s};
 }
 
-// What a thread's eight channels of four tokens are multiplied with: x_d c_d + x_partner s_d
-template <int D> struct Turn {
-    float c[4][8], s[4][8];
-    int partner;   // the lane that has the partners, or this one
-    bool any, pairs;
-    __device__ __forceinline__ void init(const akb_rotary& r, int oct, int lane)
+// Which pair each of a thread's eight channels belongs to, and where the other channel of it is.  NEXT: pairs of neighbours (akb_rotary.pairs).
+template <int D, bool NEXT> struct Pairs {
+    int first, partner;   // number of the first channel's pair; the lane that has the partners, or this one
+    bool any;
+    uint32_t minus;       // sign bit where these channels are the first of their pairs, which take their partners times -sin (NEXT: every other one is)
+    __device__ __forceinline__ Pairs(int rot, int oct, int lane)
     {
-        pairs = r.pairs != 0;
-        const int half = r.rot / 16;   // octets
-        any = oct * 8 < r.rot;
-        partner = !any || pairs ? lane : (oct < half ? lane + half : lane - half);
+        const int half = rot / 16;   // octets
+        const bool low = oct < half;
+        any = oct * 8 < rot;
+        partner = !any || NEXT ? lane : (low ? lane + half : lane - half);
+        first = !any ? 0 : (NEXT ? oct * 4 : (low ? oct : oct - half) * 8);
+        minus = low ? 0x80000000u : 0u;
     }
-    // of the token at `place`
-    __device__ __forceinline__ void angles(const akb_rotary& r, int oct, int i, double place)
+    // a partner's number with the sign that its sine has
+    __device__ __forceinline__ float signed_for(int e, float v) const { return NEXT ? (e & 1 ? v : -v) : bits_float(float_bits(v) ^ minus); }
+    __device__ __forceinline__ u32x4_t others(const u32x4_t& x) const
     {
+        u32x4_t p;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            c[i][e] = 1.f;
-            s[i][e] = -0.f;   // (a channel that does not turn keeps its sign of zero)
-        }
-        if (!any) return;
-        if (pairs) {
-#pragma unroll
-            for (int e = 0; e < 8; e += 2) {
-                sin_cos(place, r.inv_freq[oct * 4 + e / 2], s[i][e + 1], c[i][e]);
-                s[i][e] = -s[i][e + 1];
-                c[i][e + 1] = c[i][e];
-            }
-        } else {
-            const int half = r.rot / 16;
-            const bool low = oct < half;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                sin_cos(place, r.inv_freq[(low ? oct : oct - half) * 8 + e], s[i][e], c[i][e]);
-                if (low) s[i][e] = -s[i][e];
-            }
-        }
+        for (int k = 0; k < 4; ++k) p[k] = NEXT ? x[k] >> 16 | x[k] << 16 : uint32_t(__shfl(int(x[k]), partner));
+        return p;
     }
 };
+// cos, sin of one token more
+__device__ __forceinline__ f64x2_t turn_on(f64x2_t cs, f64x2_t on) { return f64x2_t{fma(cs[0], on[0], -cs[1] * on[1]), fma(cs[1], on[0], cs[0] * on[1])}; }
+// What is made from x is made again behind this, not kept from turn to turn of a loop: the registers are few
+template <class V> __device__ __forceinline__ void forget(V& x) { asm volatile("" : "+v"(x)); }
 
-// 1 / sqrt(mean of squares + eps) of a head whose channels lie in D / 8 lanes, eight in each.  Summed in 64 bits, where squares of every finite number have room;
-// the root in 32 bits of a number between 1 and 4.
-template <class T, int D> __device__ __forceinline__ float norm_scale(const u32x4_t& x, float eps)
+template <class T> __device__ __forceinline__ float channel(const u32x4_t& x, int e) { return e & 1 ? T::hi(x[e >> 1]) : T::lo(x[e >> 1]); }
+
+// v of the lane that CTRL (a permutation of the lanes of 16) names
+template <int CTRL> __device__ __forceinline__ float dpp(float v) { return bits_float(uint32_t(__builtin_amdgcn_update_dpp(0, int(float_bits(v)), CTRL, 0xF, 0xF, true))); }
+template <int CTRL> __device__ __forceinline__ double dpp(double v)
+{
+    const u32x2_t w = __builtin_bit_cast(u32x2_t, v);
+    const uint32_t lo = w.x, hi = w.y;
+    return __builtin_bit_cast(double, u32x2_t{uint32_t(__builtin_amdgcn_update_dpp(0, int(lo), CTRL, 0xF, 0xF, true)), uint32_t(__builtin_amdgcn_update_dpp(0, int(hi), CTRL, 0xF, 0xF, true))});
+}
+// the sum over a row's D / 8 lanes, in each of them
+template <int D, class V> __device__ __forceinline__ V row_sum(V v)
+{
+    v += dpp<0xB1>(v);    // neighbours
+    v += dpp<0x4E>(v);    // pairs of them
+    v += dpp<0x141>(v);   // fours: mirrored in eight lanes
+    if (D == 128) v += dpp<0x128>(v);   // eights: turned by eight lanes
+    return v;
+}
+// 1 / sqrt(mean of a row's squares + eps): in 64 bits, where squares of every finite number have room, ..
+template <class T, int D> __device__ __forceinline__ double norm_scale(const u32x4_t& x, float eps)
 {
     double sum = 0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const double a = T::lo(x[i]), b = T::hi(x[i]);
-        sum = fma(a, a, sum);
-        sum = fma(b, b, sum);
-    }
-#pragma unroll
-    for (int d = 1; d < D / 8; d *= 2) sum += __shfl_xor(sum, d);
-    const double m = sum * (1.0 / D) + double(eps);
-    const int e = (__builtin_amdgcn_frexp_exp(m) - 1) >> 1;   // m 4^-e: in 1 .. 4
-    return ldexpf(1.f / sqrtf(float(ldexp(m, -2 * e))), -e);
-}
-
-// Eight channels of a token, normed where there is a weight (`w`: this thread's, and its partners'), turned
-template <class T, int D> __device__ __forceinline__ u32x4_t turned(const u32x4_t& x, const Turn<D>& t, int i, bool normed, float eps, const float (&w)[8], const float (&wp)[8])
-{
-    const float scale = normed ? norm_scale<T, D>(x, eps) : 1.f;
-    u32x4_t p = x;
-    if (!t.pairs)
-#pragma unroll
-        for (int k = 0; k < 4; ++k) p[k] = __shfl(int(x[k]), t.partner);
-    float y[8];
-#pragma unroll
     for (int e = 0; e < 8; ++e) {
-        const int f = t.pairs ? e ^ 1 : e;
-        float a = e & 1 ? T::hi(x[e >> 1]) : T::lo(x[e >> 1]), b = f & 1 ? T::hi(p[f >> 1]) : T::lo(p[f >> 1]);
-        if (normed) {
-            a = a * scale * w[e];
-            b = b * scale * wp[e];
-        }
-        y[e] = fmaf(t.any ? b : 0.f, t.s[i][e], a * t.c[i][e]);
+        const double a = channel<T>(x, e);
+        sum = fma(a, a, sum);
     }
-    return u32x4_t{T::pack(y[0], y[1]), T::pack(y[2], y[3]), T::pack(y[4], y[5]), T::pack(y[6], y[7])};
+    const double m = fma(row_sum<D>(sum), 1.0 / D, double(eps));
+    double y = __builtin_amdgcn_rsq(m);
+    y = y * fma(-0.5 * m * y, y, 1.5);
+    return y * fma(-0.5 * m * y, y, 1.5);
+}
+// .. and in 32, unless the squares have none there
+template <class T, int D> __device__ __forceinline__ float norm_scale32(const u32x4_t& x, float eps)
+{
+    float sum = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sum = fmaf(channel<T>(x, e), channel<T>(x, e), sum);
+    sum = row_sum<D>(sum);
+    if (__any(!(sum > 0x1p-100f && sum < 0x1p120f))) return float(norm_scale<T, D>(x, eps));
+    return __builtin_amdgcn_rsqf(fmaf(sum, 1.f / D, eps));
 }
 
 // As append_kernel (akb_store.hip), with K turned on its way in; and the query heads of the KV head, whose tokens' angles are the same.
-template <class T, int D>
-__global__ __launch_bounds__(2 * D) void append_rotated_kernel(TurnArgs a)
+// NT: with the non-temporal hint.
+template <class T, int D, bool NEXT, bool NT>
+__global__ __launch_bounds__(2 * D, 3) void append_rotated_kernel(TurnArgs a)
 {
+    constexpr int kRow = 2 * D + 16;   // bytes of a turned key in LDS: shifted by four banks from token to token
     __shared__ PackLds<D> lds;
+    __shared__ __align__(16) uint8_t rows_s[kTB * kRow];
+    __shared__ f64x2_t on_s[D / 2];    // cos, sin of 16 tokens
     const akb_cache& c = a.c;
-    const int tid = threadIdx.x, lane = tid & 63, h = blockIdx.y, b = blockIdx.z, j = blockIdx.x;
+    const int tid = threadIdx.x, lane = tid & 63, h = a.apart ? blockIdx.y >> 1 : blockIdx.y, b = blockIdx.z, j = blockIdx.x;
+    const bool do_q = a.q_out && (!a.apart || (blockIdx.y & 1)), do_kv = !a.apart || !(blockIdx.y & 1);
     const int Hkv = c.shape.Hkv, Ncap = c.shape.Ncap, G = c.shape.Hq / Hkv, n = a.n;
     const int len = seq_len(c, b), cnt = a.n_new ? min(max(a.n_new[b], 0), n) : n;
     if (cnt == 0) return;
     if (len + cnt > Ncap) {   // the sequence is left unchanged
-        if (a.ticketed && j == 0 && h == 0 && tid == 0) atomicAdd(&c.flags[AKV_FLAG_OVERFLOW], 1);
+        if (a.ticketed && j == 0 && blockIdx.y == 0 && tid == 0) atomicAdd(&c.flags[AKV_FLAG_OVERFLOW], 1);
         return;
     }
     int ticket = -1;
@@ -136,92 +145,167 @@ __global__ __launch_bounds__(2 * D) void append_rotated_kernel(TurnArgs a)
     }
     const size_t bh = size_t(b) * Hkv + h;
     const int first = len / kTB, had = len % kTB, total = had + cnt;   // counted from the start of block `first`
-    const double place0 = double(a.r.base ? a.r.base[b / (c.shape.B / a.r.n_base)] : 0) + double(first * kTB);
+    const double place0 = double(a.r.base ? a.r.base[b / (c.shape.B / a.r.n_base)] : 0) + double(first) * kTB;
     const BlockLane<D> at(tid);
     const int t0 = at.t0;
-    Turn<D> turn;
-    turn.init(a.r, at.oct, lane);
-    float w[8], wp[8];
-    auto weights = [&](const uint16_t* norm) {
-        if (!norm) return;
-        const u32x4_t x = *reinterpret_cast<const u32x4_t*>(norm + at.oct * 8);
-        u32x4_t p = x;
-        if (!turn.pairs)
-#pragma unroll
-            for (int k = 0; k < 4; ++k) p[k] = __shfl(int(x[k]), turn.partner);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const int f = turn.pairs ? e ^ 1 : e;
-            w[e] = e & 1 ? T::hi(x[e >> 1]) : T::lo(x[e >> 1]);
-            wp[e] = f & 1 ? T::hi(p[f >> 1]) : T::lo(p[f >> 1]);
-        }
-    };
+    const Pairs<D, NEXT> pairs(a.r.rot, at.oct, lane);
     auto fresh = [&](int t) { return t >= had && t < total; };   // token t counted from the start of block `first`
-    auto angles = [&](int w0) {
+    auto get = [&](const uint16_t* p) -> u32x4_t { return NT ? __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(p)) : *reinterpret_cast<const u32x4_t*>(p); };
+    // The new tokens among the 64 from w0 on: keys to LDS (for a complete block) or to the tail; queries to q_out
+    auto turn_rows = [&](int w0, bool keys, bool to_tail, bool queries) {
+        const int begin = max(had - w0, 0), end = min(total - w0, kTB) - 1;
+        if (begin / 16 != end / 16) {   // (otherwise nothing is turned on)
+            if (tid < a.r.rot / 2) on_s[tid] = cos_sin(16.0, a.r.inv_freq[tid]);
+            __syncthreads();
+        }
+        u32x4_t kw = {}, kwo = {}, qw = {}, qwo = {};   // the weights of the channels, and of their partners
+        if (a.r.k_norm) kwo = pairs.others(kw = *reinterpret_cast<const u32x4_t*>(a.r.k_norm + at.oct * 8));
+        if (a.r.q_norm) qwo = pairs.others(qw = *reinterpret_cast<const u32x4_t*>(a.r.q_norm + at.oct * 8));
+        // a wave's rows that are new lie one behind the other: the first, and its loads, here (the power series' constants would fill the loop's registers)
+        int i = 0;
+        while (i < 4 && !__any(fresh(w0 + 16 * i + at.grp))) ++i;
+        if (i == 4) return;
+        u32x4_t k, q[4];
+        auto fetch = [&](int t, int g0) {   // the query rows of four heads
 #pragma unroll
-        for (int r = 0; r < 4; ++r) turn.angles(a.r, at.oct, r, place0 + double(w0 + t0 + r));
-    };
-    auto load = [&](const uint16_t* x, int64_t seq, int64_t token, int head, int w0, u32x4_t (&to)[4]) {
+            for (int g = 0; g < 4; ++g)
+                q[g] = fresh(t) && g0 + g < G ? get(a.x.q + b * a.x.q_seq + (t - had) * a.x.q_token + (h * G + g0 + g) * D + at.oct * 8) : u32x4_t{0, 0, 0, 0};
+        };
+        auto fetch_row = [&](int t) {
+            if (keys) k = fresh(t) ? get(a.x.k + b * a.x.k_seq + (t - had) * a.x.k_token + h * D + at.oct * 8) : u32x4_t{0, 0, 0, 0};
+            if (queries) fetch(t, 0);
+        };
+        fetch_row(w0 + 16 * i + at.grp);
+        f64x2_t cs[8];
+        {   // (NEXT: a thread's channels are four pairs; otherwise eight, of which its partner makes the other four)
+            f64x2_t made[4];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int t = w0 + t0 + r;
-            to[r] = fresh(t) ? *reinterpret_cast<const u32x4_t*>(x + b * seq + (t - had) * token + head * D + at.oct * 8) : u32x4_t{0, 0, 0, 0};
+            for (int e = 0; e < 4; ++e)
+                made[e] = pairs.any ? cos_sin(place0 + double(w0 + 16 * i + at.grp), a.r.inv_freq[pairs.first + e + (NEXT || pairs.minus ? 0 : 4)]) : f64x2_t{1.0, 0.0};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if (NEXT) {
+                    cs[2 * e] = cs[2 * e + 1] = made[e];
+                } else {
+                    const f64x2_t other = {__shfl(made[e][0], pairs.partner), __shfl(made[e][1], pairs.partner)};
+                    cs[e] = pairs.minus ? made[e] : other;
+                    cs[4 + e] = pairs.minus ? other : made[e];
+                }
+            }
+        }
+#pragma unroll 1
+        for (;;) {
+            const int t = w0 + 16 * i + at.grp;
+            const bool mine = fresh(t);
+            int pair0 = pairs.first;
+            forget(pair0);
+            forget(kw);
+            forget(kwo);
+            forget(qw);
+            forget(qwo);
+            if (keys) {
+                const u32x4_t o = pairs.others(k);
+                const double scale = a.r.k_norm ? norm_scale<T, D>(k, a.r.eps) : 1.0;
+                float y[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    double u = channel<T>(k, e);
+                    if (a.r.k_norm) u *= double(channel<T>(kw, e)) * scale;
+                    if (pairs.any) {
+                        double v = pairs.signed_for(e, channel<T>(o, e));
+                        if (a.r.k_norm) v *= double(channel<T>(kwo, e)) * scale;
+                        u = fma(v, cs[e][1], u * cs[e][0]);
+                    }
+                    y[e] = float(u);
+                    if (e & 1) __builtin_amdgcn_sched_barrier(0);
+                }
+                const u32x4_t z = {T::pack(y[0], y[1]), T::pack(y[2], y[3]), T::pack(y[4], y[5]), T::pack(y[6], y[7])};
+                if (!to_tail) *reinterpret_cast<u32x4_t*>(rows_s + (t - w0) * kRow + at.oct * 16) = z;
+                else if (mine) *reinterpret_cast<u32x4_t*>(c.k_tail + (bh * kTB + (t - w0)) * D + at.oct * 8) = z;
+            }
+            if (queries) {
+            float cw[8], sw[8];   // cosine times a channel's weight, sine times its partner's
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                cw[e] = float(cs[e][0]) * (a.r.q_norm ? channel<T>(qw, e) : 1.f);
+                sw[e] = float(cs[e][1]) * pairs.signed_for(e, a.r.q_norm ? channel<T>(qwo, e) : 1.f);
+            }
+            for (int g0 = 0;;) {
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    if (g0 + g >= G) break;
+                    const u32x4_t o = pairs.others(q[g]);
+                    const float scale = a.r.q_norm ? norm_scale32<T, D>(q[g], a.r.eps) : 1.f;
+                    float y[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const float u = channel<T>(q[g], e) * scale;
+                        y[e] = pairs.any ? fmaf(channel<T>(o, e) * scale, sw[e], u * cw[e]) : u * cw[e];
+                    }
+                    if (!mine) continue;
+                    const u32x4_t z = {T::pack(y[0], y[1]), T::pack(y[2], y[3]), T::pack(y[4], y[5]), T::pack(y[6], y[7])};
+                    u32x4_t* out = reinterpret_cast<u32x4_t*>(a.q_out + ((bh * G + g0 + g) * n + (t - had)) * D + at.oct * 8);
+                    if (NT) __builtin_nontemporal_store(z, out);
+                    else *out = z;
+                }
+                if ((g0 += 4) >= G) break;
+                fetch(t, g0);
+            }
+            }
+            if (++i == 4 || !__any(fresh(t + 16))) break;
+            fetch_row(t + 16);
+            if (pairs.any)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) cs[e] = turn_on(cs[e], on_s[pair0 + (NEXT ? e >> 1 : e)]);
         }
     };
-    auto load_k = [&](int w0, u32x4_t (&to)[4]) {   // (the angles are those of w0)
-        load(a.x.k, a.x.k_seq, a.x.k_token, h, w0, to);
+    auto load_v = [&](int w0, u32x4_t (&to)[4]) {
+        const uint16_t* p = a.x.v + b * a.x.v_seq + (w0 + t0 - had) * a.x.v_token + h * D + at.oct * 8;
 #pragma unroll
-        for (int r = 0; r < 4; ++r) to[r] = turned<T, D>(to[r], turn, r, a.r.k_norm, a.r.eps, w, wp);
+        for (int r = 0; r < 4; ++r) to[r] = fresh(w0 + t0 + r) ? get(p + r * a.x.v_token) : u32x4_t{0, 0, 0, 0};
     };
-    if (j * kTB < total) angles(j * kTB);
-    weights(a.r.k_norm);
-    const bool complete = (j + 1) * kTB <= total, tail = j == 0 && total % kTB;
+    const bool some = j * kTB < total, complete = (j + 1) * kTB <= total;
+    // the incomplete block goes to the tail by the workgroup that has it, or, where the tail holds what the first block takes, by the workgroup of that
     const int last = total / kTB * kTB;
+    const bool tail = total % kTB && (had > 0 ? j == 0 : j * kTB == last), tail_here = tail && j * kTB == last;
     u32x4_t x[4];
+    if (some) turn_rows(j * kTB, do_kv && (complete || tail_here), tail_here, do_q);
+    if (do_kv && complete) {
+        __syncthreads();
 #pragma unroll
-    for (int side = 0; side < 2; ++side) {
-        const bool is_v = side == 1;
-        if (complete) {
-            if (is_v) load(a.x.v, a.x.v_seq, a.x.v_token, h, j * kTB, x);
-            else load_k(j * kTB, x);
+        for (int side = 0; side < 2; ++side) {
+            const bool is_v = side == 1;
+            if (is_v) {
+                load_v(j * kTB, x);
+            } else {
+#pragma unroll
+                for (int r = 0; r < 4; ++r) x[r] = *reinterpret_cast<const u32x4_t*>(rows_s + (t0 + r) * kRow + at.oct * 16);
+            }
             if (j == 0 && had > 0) {
                 const bool old[4] = {t0 < had, t0 + 1 < had, t0 + 2 < had, t0 + 3 < had};
                 const int token[4] = {t0, t0 + 1, t0 + 2, t0 + 3};
                 load_tail<D, true>(c, bh, is_v, x, old, token);
             }
             if (is_v) __syncthreads();   // K's block has been packed
-            pack_block<T, D, false>(c, bh * (Ncap / kTB) + first + j, is_v, x, lds);
+            pack_block<T, D, NT>(c, bh * (Ncap / kTB) + first + j, is_v, x, lds);
         }
     }
-    if (a.q_out && j * kTB < total) {
-        weights(a.r.q_norm);
-        for (int g = 0; g < G; ++g) {
-            load(a.x.q, a.x.q_seq, a.x.q_token, h * G + g, j * kTB, x);
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                x[r] = turned<T, D>(x[r], turn, r, a.r.q_norm, a.r.eps, w, wp);
-                const int t = j * kTB + t0 + r;
-                if (fresh(t)) *reinterpret_cast<u32x4_t*>(a.q_out + ((bh * G + g) * n + (t - had)) * D + at.oct * 8) = x[r];
-            }
+    if (do_kv && tail) {   // its new tokens go to the tail (what of the old ones is needed has been read)
+        if (!tail_here) {
+            __syncthreads();
+            turn_rows(last, true, true, false);
         }
-    }
-    if (tail) {   // the incomplete block: its new tokens go to the tail (what of the old ones is needed has been read)
-        __syncthreads();
         bool store[4];
 #pragma unroll
         for (int r = 0; r < 4; ++r) store[r] = fresh(last + t0 + r);
-        if (last) angles(last);
-        weights(a.r.k_norm);
-        load_k(last, x);
-        store_tail<D>(c, bh, false, x, store);
-        load(a.x.v, a.x.v_seq, a.x.v_token, h, last, x);
+        load_v(last, x);
         store_tail<D>(c, bh, true, x, store);
     }
-    if (c.score && tid < kTB) {   // the new tokens' scores
+    if (do_kv && c.score && tid < kTB) {   // the new tokens' scores
         const int t = j * kTB + tid;
         if (fresh(t)) c.score[bh * Ncap + first * kTB + t] = 0.f;
     }
-    if (ticket == int(gridDim.x) * Hkv - 1) {   // the last workgroup of the sequence (thread 0 of it)
+    if (ticket == int(gridDim.x * gridDim.y) - 1) {   // the last workgroup of the sequence (thread 0 of it)
         c.flags[AKV_NFLAGS + b] = 0;
         c.lens[b] = len + cnt;
     }
@@ -230,12 +314,23 @@ __global__ __launch_bounds__(2 * D) void append_rotated_kernel(TurnArgs a)
 hipError_t launch_append_rotated(const akb_cache& c, const akb_tokens& x, const int32_t* n_new, int n, uint16_t* q_out, const akb_rotary& r, hipStream_t st)
 {
     const int blocks = (kTB - 1 + n + kTB - 1) / kTB;
-    const dim3 grid(blocks, c.shape.Hkv, c.shape.B);
+    const bool apart = q_out && blocks == 1 && c.shape.Hkv <= 32767;
+    const dim3 grid(blocks, c.shape.Hkv * (apart ? 2 : 1), c.shape.B);
     const bool ticketed = append_ticketed(c.shape, n);
-    const TurnArgs a{c, x, r, n_new, n, q_out, ticketed ? 1 : 0};
+    // as in the append: large calls pass the last-level cache by
+    const bool streamed = (size_t(q_out ? 2 * c.shape.Hq : 0) + 2 * size_t(c.shape.Hkv)) * c.shape.B * n * c.shape.D * 2 > (size_t(128) << 20);
+    const TurnArgs a{c, x, r, n_new, n, q_out, ticketed ? 1 : 0, apart ? 1 : 0};
     auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(2 * c.shape.D), 0, st, a); };
-    if (c.shape.dtype == AKB_FP16) c.shape.D == 64 ? launch(append_rotated_kernel<Fp16, 64>) : launch(append_rotated_kernel<Fp16, 128>);
-    else c.shape.D == 64 ? launch(append_rotated_kernel<Bf16, 64>) : launch(append_rotated_kernel<Bf16, 128>);
+    auto pick = [&](auto type, auto width) {
+        using T = decltype(type);
+        constexpr int D = decltype(width)::value;
+        if (r.pairs) streamed ? launch(append_rotated_kernel<T, D, true, true>) : launch(append_rotated_kernel<T, D, true, false>);
+        else streamed ? launch(append_rotated_kernel<T, D, false, true>) : launch(append_rotated_kernel<T, D, false, false>);
+    };
+    using D64 = std::integral_constant<int, 64>;
+    using D128 = std::integral_constant<int, 128>;
+    if (c.shape.dtype == AKB_FP16) c.shape.D == 64 ? pick(Fp16(), D64()) : pick(Fp16(), D128());
+    else c.shape.D == 64 ? pick(Bf16(), D64()) : pick(Bf16(), D128());
     if (hipError_t e = hipGetLastError()) return e;
     return ticketed ? hipSuccess : launch_append_lens(c, n_new, n, st);
 }
