@@ -16,7 +16,7 @@ struct TurnArgs {
     int n;
     uint16_t* q_out;
     int ticketed;
-    int apart;   // the query heads of a KV head have a workgroup of their own
+    int blocks, rows;   // of a sequence: workgroups that turn 64 tokens of a KV head and its query heads (blocks x KV heads), and those that turn 16 rows of few tokens
 };
 typedef double f64x2_t __attribute__((ext_vector_type(2)));
 
@@ -48,15 +48,16 @@ __device__ __forceinline__ f64x2_t cos_sin(double place, float freq)
 
 // Which pair each of a thread's eight channels belongs to, and where the other channel of it is.  NEXT: pairs of neighbours (akb_rotary.pairs).
 template <int D, bool NEXT> struct Pairs {
-    int first, partner;   // number of the first channel's pair; the lane that has the partners, or this one
+    int first, step;      // number of the first channel's pair; how many octets (lanes) further the partners are
+    int lane;
     bool any;
     uint32_t minus;       // sign bit where these channels are the first of their pairs, which take their partners times -sin (NEXT: every other one is)
-    __device__ __forceinline__ Pairs(int rot, int oct, int lane)
+    __device__ __forceinline__ Pairs(int rot, int oct, int lane_) : lane(lane_)
     {
         const int half = rot / 16;   // octets
         const bool low = oct < half;
         any = oct * 8 < rot;
-        partner = !any || NEXT ? lane : (low ? lane + half : lane - half);
+        step = !any || NEXT ? 0 : (low ? half : -half);
         first = !any ? 0 : (NEXT ? oct * 4 : (low ? oct : oct - half) * 8);
         minus = low ? 0x80000000u : 0u;
     }
@@ -66,7 +67,7 @@ template <int D, bool NEXT> struct Pairs {
     {
         u32x4_t p;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) p[k] = NEXT ? x[k] >> 16 | x[k] << 16 : uint32_t(__shfl(int(x[k]), partner));
+        for (int k = 0; k < 4; ++k) p[k] = NEXT ? x[k] >> 16 | x[k] << 16 : uint32_t(__shfl(int(x[k]), lane + step));
         return p;
     }
 };
@@ -108,41 +109,51 @@ template <class T, int D> __device__ __forceinline__ double norm_scale(const u32
     y = y * fma(-0.5 * m * y, y, 1.5);
     return y * fma(-0.5 * m * y, y, 1.5);
 }
-// .. and in 32, unless the squares have none there
-template <class T, int D> __device__ __forceinline__ float norm_scale32(const u32x4_t& x, float eps)
+// .. and in 32, unless the squares of some row of the wave have none there (far)
+template <class T, int D> __device__ __forceinline__ float norm_scale32(const u32x4_t& x, float eps, bool& far)
 {
     float sum = 0.f;
 #pragma unroll
     for (int e = 0; e < 8; ++e) sum = fmaf(channel<T>(x, e), channel<T>(x, e), sum);
     sum = row_sum<D>(sum);
-    if (__any(!(sum > 0x1p-100f && sum < 0x1p120f))) return float(norm_scale<T, D>(x, eps));
+    far = __any(!(sum > 0x1p-100f && sum < 0x1p120f));
+    if (far) return float(norm_scale<T, D>(x, eps));
     return __builtin_amdgcn_rsqf(fmaf(sum, 1.f / D, eps));
 }
 
 // As append_kernel (akb_store.hip), with K turned on its way in; and the query heads of the KV head, whose tokens' angles are the same.
 // NT: with the non-temporal hint.
 template <class T, int D, bool NEXT, bool NT>
-__global__ __launch_bounds__(2 * D, 3) void append_rotated_kernel(TurnArgs a)
+__global__ __launch_bounds__(2 * D, NEXT ? 3 : 4) void append_rotated_kernel(TurnArgs a)
 {
+    constexpr int kHeads = 2;          // that are asked for at a time
     constexpr int kRow = 2 * D + 16;   // bytes of a turned key in LDS: shifted by four banks from token to token
     __shared__ PackLds<D> lds;
     __shared__ __align__(16) uint8_t rows_s[kTB * kRow];
     __shared__ f64x2_t on_s[D / 2];    // cos, sin of 16 tokens
+    __shared__ u32x4_t norm_s[2][D / 8];   // the norms' weights, of queries and of keys
     const akb_cache& c = a.c;
-    const int tid = threadIdx.x, lane = tid & 63, h = a.apart ? blockIdx.y >> 1 : blockIdx.y, b = blockIdx.z, j = blockIdx.x;
-    const bool do_q = a.q_out && (!a.apart || (blockIdx.y & 1)), do_kv = !a.apart || !(blockIdx.y & 1);
-    const int Hkv = c.shape.Hkv, Ncap = c.shape.Ncap, G = c.shape.Hq / Hkv, n = a.n;
+    const int tid = threadIdx.x, lane = tid & 63, b = blockIdx.y;
+    const int Hkv = c.shape.Hkv, walks = a.blocks * Hkv;
+    const bool in_rows = int(blockIdx.x) >= walks;
+    // (a head's blocks one behind the other: the heads of a block beside each other 162 us of 4 x 8192 tokens for 151)
+    const int h = blockIdx.x / a.blocks, j = blockIdx.x % a.blocks;
+    const int Ncap = c.shape.Ncap, G = c.shape.Hq / Hkv, n = a.n;
     const int len = seq_len(c, b), cnt = a.n_new ? min(max(a.n_new[b], 0), n) : n;
     if (cnt == 0) return;
     if (len + cnt > Ncap) {   // the sequence is left unchanged
-        if (a.ticketed && j == 0 && blockIdx.y == 0 && tid == 0) atomicAdd(&c.flags[AKV_FLAG_OVERFLOW], 1);
+        if (a.ticketed && blockIdx.x == 0 && tid == 0) atomicAdd(&c.flags[AKV_FLAG_OVERFLOW], 1);
         return;
     }
-    int ticket = -1;
-    if (a.ticketed) {   // drawn once all waves of the workgroup have read the length, looked at when it leaves
-        __syncthreads();
-        if (tid == 0) ticket = atomicAdd(&c.flags[AKV_NFLAGS + b], 1);
+    if (tid < 2 * (D / 8)) {
+        const uint16_t* norm = tid < D / 8 ? a.r.q_norm : a.r.k_norm;
+        if (norm) norm_s[0][tid] = *reinterpret_cast<const u32x4_t*>(norm + tid % (D / 8) * 8);
     }
+    __syncthreads();
+    int ticket = -1;   // drawn once all waves of the workgroup have read the length, looked at when it leaves
+    if (a.ticketed && tid == 0) ticket = atomicAdd(&c.flags[AKV_NFLAGS + b], 1);
+    const bool few = a.rows > 0 && len % kTB + cnt < kTB;   // few: the rows' workgroups turn the keys and store the values, too
+    const bool do_q = a.q_out && a.rows == 0, do_kv = !in_rows && !few;
     const size_t bh = size_t(b) * Hkv + h;
     const int first = len / kTB, had = len % kTB, total = had + cnt;   // counted from the start of block `first`
     const double place0 = double(a.r.base ? a.r.base[b / (c.shape.B / a.r.n_base)] : 0) + double(first) * kTB;
@@ -151,6 +162,69 @@ __global__ __launch_bounds__(2 * D, 3) void append_rotated_kernel(TurnArgs a)
     const Pairs<D, NEXT> pairs(a.r.rot, at.oct, lane);
     auto fresh = [&](int t) { return t >= had && t < total; };   // token t counted from the start of block `first`
     auto get = [&](const uint16_t* p) -> u32x4_t { return NT ? __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(p)) : *reinterpret_cast<const u32x4_t*>(p); };
+    // cos, sin of a thread's pairs at a place (NEXT: its channels are four pairs; otherwise eight, of which its partner makes the other four)
+    auto first_turns = [&](double place, f64x2_t (&cs)[8]) {
+        f64x2_t made[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) made[e] = pairs.any ? cos_sin(place, a.r.inv_freq[pairs.first + e + (NEXT || pairs.minus ? 0 : 4)]) : f64x2_t{1.0, 0.0};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if (NEXT) {
+                cs[2 * e] = cs[2 * e + 1] = made[e];
+            } else {
+                const f64x2_t other = {__shfl(made[e][0], lane + pairs.step), __shfl(made[e][1], lane + pairs.step)};
+                cs[e] = pairs.minus ? made[e] : other;
+                cs[4 + e] = pairs.minus ? other : made[e];
+            }
+        }
+    };
+    // eight channels of a key (octet `oct`)
+    auto turn_key = [&](const u32x4_t& k, const f64x2_t (&cs)[8], int oct) {
+        const u32x4_t w = norm_s[1][oct], wo = NEXT ? pairs.others(w) : norm_s[1][oct + pairs.step];   // the norm's weights, those of the partners
+        const u32x4_t o = pairs.others(k);
+        const double scale = a.r.k_norm ? norm_scale<T, D>(k, a.r.eps) : 1.0;
+        float y[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            double u = channel<T>(k, e);
+            if (a.r.k_norm) u *= double(channel<T>(w, e)) * scale;
+            if (pairs.any) {
+                double v = pairs.signed_for(e, channel<T>(o, e));
+                if (a.r.k_norm) v *= double(channel<T>(wo, e)) * scale;
+                u = fma(v, cs[e][1], u * cs[e][0]);
+            }
+            y[e] = float(u);
+            if (e & 1) __builtin_amdgcn_sched_barrier(0);   // (all eight at a time do not fit the registers)
+        }
+        return u32x4_t{T::pack(y[0], y[1]), T::pack(y[2], y[3]), T::pack(y[4], y[5]), T::pack(y[6], y[7])};
+    };
+    // ... of queries: cosine times a channel's weight, sine times its partner's
+    auto query_turns = [&](const f64x2_t (&cs)[8], int oct, float (&cw)[8], float (&sw)[8]) {
+        const u32x4_t w = norm_s[0][oct], wo = NEXT ? pairs.others(w) : norm_s[0][oct + pairs.step];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            cw[e] = float(cs[e][0]) * (a.r.q_norm ? channel<T>(w, e) : 1.f);
+            sw[e] = float(cs[e][1]) * pairs.signed_for(e, a.r.q_norm ? channel<T>(wo, e) : 1.f);
+        }
+    };
+    auto turn_query_by = [&](const u32x4_t& q, const float (&cw)[8], const float (&sw)[8]) {
+        const u32x4_t o = pairs.others(q);
+        bool far = false;
+        const float scale = a.r.q_norm ? norm_scale32<T, D>(q, a.r.eps, far) : 1.f;
+        float y[8];
+        if (far) {   // numbers that leave a product no room
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y[e] = channel<T>(q, e) * scale * cw[e] + (pairs.any ? channel<T>(o, e) * scale * sw[e] : 0.f);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                y[e] = channel<T>(q, e) * cw[e];
+                if (pairs.any) y[e] = fmaf(channel<T>(o, e), sw[e], y[e]);
+                y[e] *= scale;
+            }
+        }
+        return u32x4_t{T::pack(y[0], y[1]), T::pack(y[2], y[3]), T::pack(y[4], y[5]), T::pack(y[6], y[7])};
+    };
     // The new tokens among the 64 from w0 on: keys to LDS (for a complete block) or to the tail; queries to q_out
     auto turn_rows = [&](int w0, bool keys, bool to_tail, bool queries) {
         const int begin = max(had - w0, 0), end = min(total - w0, kTB) - 1;
@@ -158,17 +232,14 @@ __global__ __launch_bounds__(2 * D, 3) void append_rotated_kernel(TurnArgs a)
             if (tid < a.r.rot / 2) on_s[tid] = cos_sin(16.0, a.r.inv_freq[tid]);
             __syncthreads();
         }
-        u32x4_t kw = {}, kwo = {}, qw = {}, qwo = {};   // the weights of the channels, and of their partners
-        if (a.r.k_norm) kwo = pairs.others(kw = *reinterpret_cast<const u32x4_t*>(a.r.k_norm + at.oct * 8));
-        if (a.r.q_norm) qwo = pairs.others(qw = *reinterpret_cast<const u32x4_t*>(a.r.q_norm + at.oct * 8));
         // a wave's rows that are new lie one behind the other: the first, and its loads, here (the power series' constants would fill the loop's registers)
         int i = 0;
         while (i < 4 && !__any(fresh(w0 + 16 * i + at.grp))) ++i;
         if (i == 4) return;
-        u32x4_t k, q[4];
-        auto fetch = [&](int t, int g0) {   // the query rows of four heads
+        u32x4_t k, q[kHeads];
+        auto fetch = [&](int t, int g0) {   // the query rows of some heads
 #pragma unroll
-            for (int g = 0; g < 4; ++g)
+            for (int g = 0; g < kHeads; ++g)
                 q[g] = fresh(t) && g0 + g < G ? get(a.x.q + b * a.x.q_seq + (t - had) * a.x.q_token + (h * G + g0 + g) * D + at.oct * 8) : u32x4_t{0, 0, 0, 0};
         };
         auto fetch_row = [&](int t) {
@@ -177,80 +248,35 @@ __global__ __launch_bounds__(2 * D, 3) void append_rotated_kernel(TurnArgs a)
         };
         fetch_row(w0 + 16 * i + at.grp);
         f64x2_t cs[8];
-        {   // (NEXT: a thread's channels are four pairs; otherwise eight, of which its partner makes the other four)
-            f64x2_t made[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                made[e] = pairs.any ? cos_sin(place0 + double(w0 + 16 * i + at.grp), a.r.inv_freq[pairs.first + e + (NEXT || pairs.minus ? 0 : 4)]) : f64x2_t{1.0, 0.0};
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                if (NEXT) {
-                    cs[2 * e] = cs[2 * e + 1] = made[e];
-                } else {
-                    const f64x2_t other = {__shfl(made[e][0], pairs.partner), __shfl(made[e][1], pairs.partner)};
-                    cs[e] = pairs.minus ? made[e] : other;
-                    cs[4 + e] = pairs.minus ? other : made[e];
-                }
-            }
-        }
+        first_turns(place0 + double(w0 + 16 * i + at.grp), cs);
 #pragma unroll 1
         for (;;) {
             const int t = w0 + 16 * i + at.grp;
             const bool mine = fresh(t);
-            int pair0 = pairs.first;
+            int pair0 = pairs.first, oct = at.oct;
             forget(pair0);
-            forget(kw);
-            forget(kwo);
-            forget(qw);
-            forget(qwo);
+            forget(oct);
             if (keys) {
-                const u32x4_t o = pairs.others(k);
-                const double scale = a.r.k_norm ? norm_scale<T, D>(k, a.r.eps) : 1.0;
-                float y[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    double u = channel<T>(k, e);
-                    if (a.r.k_norm) u *= double(channel<T>(kw, e)) * scale;
-                    if (pairs.any) {
-                        double v = pairs.signed_for(e, channel<T>(o, e));
-                        if (a.r.k_norm) v *= double(channel<T>(kwo, e)) * scale;
-                        u = fma(v, cs[e][1], u * cs[e][0]);
-                    }
-                    y[e] = float(u);
-                    if (e & 1) __builtin_amdgcn_sched_barrier(0);
-                }
-                const u32x4_t z = {T::pack(y[0], y[1]), T::pack(y[2], y[3]), T::pack(y[4], y[5]), T::pack(y[6], y[7])};
+                const u32x4_t z = turn_key(k, cs, oct);
                 if (!to_tail) *reinterpret_cast<u32x4_t*>(rows_s + (t - w0) * kRow + at.oct * 16) = z;
                 else if (mine) *reinterpret_cast<u32x4_t*>(c.k_tail + (bh * kTB + (t - w0)) * D + at.oct * 8) = z;
             }
             if (queries) {
-            float cw[8], sw[8];   // cosine times a channel's weight, sine times its partner's
+                float cw[8], sw[8];
+                query_turns(cs, oct, cw, sw);
+                for (int g0 = 0;;) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                cw[e] = float(cs[e][0]) * (a.r.q_norm ? channel<T>(qw, e) : 1.f);
-                sw[e] = float(cs[e][1]) * pairs.signed_for(e, a.r.q_norm ? channel<T>(qwo, e) : 1.f);
-            }
-            for (int g0 = 0;;) {
-#pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    if (g0 + g >= G) break;
-                    const u32x4_t o = pairs.others(q[g]);
-                    const float scale = a.r.q_norm ? norm_scale32<T, D>(q[g], a.r.eps) : 1.f;
-                    float y[8];
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const float u = channel<T>(q[g], e) * scale;
-                        y[e] = pairs.any ? fmaf(channel<T>(o, e) * scale, sw[e], u * cw[e]) : u * cw[e];
+                    for (int g = 0; g < kHeads; ++g) {
+                        if (g0 + g >= G) break;
+                        const u32x4_t z = turn_query_by(q[g], cw, sw);
+                        if (!mine) continue;
+                        u32x4_t* out = reinterpret_cast<u32x4_t*>(a.q_out + ((bh * G + g0 + g) * n + (t - had)) * D + at.oct * 8);
+                        if (NT) __builtin_nontemporal_store(z, out);
+                        else *out = z;
                     }
-                    if (!mine) continue;
-                    const u32x4_t z = {T::pack(y[0], y[1]), T::pack(y[2], y[3]), T::pack(y[4], y[5]), T::pack(y[6], y[7])};
-                    u32x4_t* out = reinterpret_cast<u32x4_t*>(a.q_out + ((bh * G + g0 + g) * n + (t - had)) * D + at.oct * 8);
-                    if (NT) __builtin_nontemporal_store(z, out);
-                    else *out = z;
+                    if ((g0 += kHeads) >= G) break;
+                    fetch(t, g0);
                 }
-                if ((g0 += 4) >= G) break;
-                fetch(t, g0);
-            }
             }
             if (++i == 4 || !__any(fresh(t + 16))) break;
             fetch_row(t + 16);
@@ -264,7 +290,32 @@ __global__ __launch_bounds__(2 * D, 3) void append_rotated_kernel(TurnArgs a)
 #pragma unroll
         for (int r = 0; r < 4; ++r) to[r] = fresh(w0 + t0 + r) ? get(p + r * a.x.v_token) : u32x4_t{0, 0, 0, 0};
     };
-    const bool some = j * kTB < total, complete = (j + 1) * kTB <= total;
+    if (in_rows) {   // row by row: the query heads, the KV heads' keys and, where the tail takes them, values of each token
+        const int heads = c.shape.Hq + 2 * Hkv, row = (blockIdx.x - walks) * 16 + at.grp, i = row / heads, s = row - i * heads;
+        const bool is_q = s < c.shape.Hq, is_k = !is_q && s < c.shape.Hq + Hkv;
+        if (i < cnt && (is_q ? a.q_out != nullptr : few)) {
+            const int head = is_q ? s : (is_k ? s - c.shape.Hq : s - c.shape.Hq - Hkv);
+            const u32x4_t v = get(is_q ? a.x.q + b * a.x.q_seq + i * a.x.q_token + head * D + at.oct * 8
+                                       : (is_k ? a.x.k + b * a.x.k_seq + i * a.x.k_token : a.x.v + b * a.x.v_seq + i * a.x.v_token) + head * D + at.oct * 8);
+            if (is_q || is_k) {
+                f64x2_t cs[8];
+                first_turns(place0 + double(had + i), cs);
+                if (is_q) {
+                    float cw[8], sw[8];
+                    query_turns(cs, at.oct, cw, sw);
+                    *reinterpret_cast<u32x4_t*>(a.q_out + ((size_t(b) * c.shape.Hq + head) * n + i) * D + at.oct * 8) = turn_query_by(v, cw, sw);
+                } else {
+                    *reinterpret_cast<u32x4_t*>(c.k_tail + ((size_t(b) * Hkv + head) * kTB + had + i) * D + at.oct * 8) = turn_key(v, cs, at.oct);
+                }
+            } else {
+                uint16_t* to = c.v_tail + ((size_t(b) * Hkv + head) * D + at.oct * 8) * kTB + v_place(had + i);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) to[e * kTB] = (uint16_t)(v[e >> 1] >> (16 * (e & 1)));
+                if (c.score && at.oct == 0) c.score[(size_t(b) * Hkv + head) * Ncap + len + i] = 0.f;
+            }
+        }
+    }
+    const bool some = !in_rows && (do_q || do_kv) && j * kTB < total, complete = (j + 1) * kTB <= total;
     // the incomplete block goes to the tail by the workgroup that has it, or, where the tail holds what the first block takes, by the workgroup of that
     const int last = total / kTB * kTB;
     const bool tail = total % kTB && (had > 0 ? j == 0 : j * kTB == last), tail_here = tail && j * kTB == last;
@@ -305,21 +356,23 @@ __global__ __launch_bounds__(2 * D, 3) void append_rotated_kernel(TurnArgs a)
         const int t = j * kTB + tid;
         if (fresh(t)) c.score[bh * Ncap + first * kTB + t] = 0.f;
     }
-    if (ticket == int(gridDim.x * gridDim.y) - 1) {   // the last workgroup of the sequence (thread 0 of it)
+    if (ticket == int(gridDim.x) - 1) {   // the last workgroup of the sequence (thread 0 of it)
         c.flags[AKV_NFLAGS + b] = 0;
         c.lens[b] = len + cnt;
     }
 }
 
+constexpr int kFewTokens = 8;
 hipError_t launch_append_rotated(const akb_cache& c, const akb_tokens& x, const int32_t* n_new, int n, uint16_t* q_out, const akb_rotary& r, hipStream_t st)
 {
     const int blocks = (kTB - 1 + n + kTB - 1) / kTB;
-    const bool apart = q_out && blocks == 1 && c.shape.Hkv <= 32767;
-    const dim3 grid(blocks, c.shape.Hkv * (apart ? 2 : 1), c.shape.B);
+    // Few tokens: row by row, which leaves little to a workgroup
+    const int rows = n <= kFewTokens ? (n * (c.shape.Hq + 2 * c.shape.Hkv) + 15) / 16 : 0;
+    const dim3 grid(blocks * c.shape.Hkv + rows, c.shape.B);
     const bool ticketed = append_ticketed(c.shape, n);
     // as in the append: large calls pass the last-level cache by
     const bool streamed = (size_t(q_out ? 2 * c.shape.Hq : 0) + 2 * size_t(c.shape.Hkv)) * c.shape.B * n * c.shape.D * 2 > (size_t(128) << 20);
-    const TurnArgs a{c, x, r, n_new, n, q_out, ticketed ? 1 : 0, apart ? 1 : 0};
+    const TurnArgs a{c, x, r, n_new, n, q_out, ticketed ? 1 : 0, blocks, rows};
     auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(2 * c.shape.D), 0, st, a); };
     auto pick = [&](auto type, auto width) {
         using T = decltype(type);
