@@ -2,6 +2,8 @@
 //
 // Keys are normed and turned in 64 bits and rounded once, to the 16-bit type: their largest number decides a block's exponent, and a number next to a border would get another
 // code where 32 bits round twice.  Queries are normed and turned in 32 bits, by the same angles.
+// Bound by memory where it is large (4 x 8192 tokens of 32 + 16 heads: 738 MB in 151 us, 4.9 TB/s, what a plain copy of as much in as out reaches; without norms and with 16
+// channels turned 147), by the chain of loads, sums and stores of a workgroup where it is small.
 // A row (a token of a head) lies in D / 8 lanes, eight channels in each; a workgroup has a block's 64 tokens, 16 rows at a time.  Sine and cosine are made by their power series
 // for a thread's first token (half of them by the lane of the other channels of the pairs), and turned on by 16 tokens, in 64 bits, for the next.
 #include "akb_pack.h"
@@ -16,7 +18,9 @@ struct TurnArgs {
     int n;
     uint16_t* q_out;
     int ticketed;
-    int blocks, rows;   // of a sequence: workgroups that turn 64 tokens of a KV head and its query heads (blocks x KV heads), and those that turn 16 rows of few tokens
+    // Workgroups of a sequence: `blocks` x KV heads, each of which has 64 tokens of a KV head and, unless `apart`, of its query heads; where apart, as many for the query
+    // heads; where the tokens are few, `rows` that have 16 rows each
+    int blocks, apart, rows;
 };
 typedef double f64x2_t __attribute__((ext_vector_type(2)));
 
@@ -134,11 +138,10 @@ __global__ __launch_bounds__(2 * D, NEXT ? 3 : 4) void append_rotated_kernel(Tur
     __shared__ u32x4_t norm_s[2][D / 8];   // the norms' weights, of queries and of keys
     const akb_cache& c = a.c;
     const int tid = threadIdx.x, lane = tid & 63, b = blockIdx.y;
-    const int Hkv = c.shape.Hkv, walks = a.blocks * Hkv;
-    const bool in_rows = int(blockIdx.x) >= walks;
+    const int Hkv = c.shape.Hkv, walks = a.blocks * Hkv, Ncap = c.shape.Ncap, G = c.shape.Hq / Hkv, n = a.n;
+    const bool behind = int(blockIdx.x) >= walks, in_rows = behind && a.rows > 0;
     // (a head's blocks one behind the other: the heads of a block beside each other 162 us of 4 x 8192 tokens for 151)
-    const int h = blockIdx.x / a.blocks, j = blockIdx.x % a.blocks;
-    const int Ncap = c.shape.Ncap, G = c.shape.Hq / Hkv, n = a.n;
+    const int walk = behind ? blockIdx.x - walks : blockIdx.x, h = walk / a.blocks, j = walk % a.blocks;
     const int len = seq_len(c, b), cnt = a.n_new ? min(max(a.n_new[b], 0), n) : n;
     if (cnt == 0) return;
     if (len + cnt > Ncap) {   // the sequence is left unchanged
@@ -153,7 +156,7 @@ __global__ __launch_bounds__(2 * D, NEXT ? 3 : 4) void append_rotated_kernel(Tur
     int ticket = -1;   // drawn once all waves of the workgroup have read the length, looked at when it leaves
     if (a.ticketed && tid == 0) ticket = atomicAdd(&c.flags[AKV_NFLAGS + b], 1);
     const bool few = a.rows > 0 && len % kTB + cnt < kTB;   // few: the rows' workgroups turn the keys and store the values, too
-    const bool do_q = a.q_out && a.rows == 0, do_kv = !in_rows && !few;
+    const bool do_q = a.q_out && a.rows == 0 && behind == (a.apart != 0), do_kv = !behind && !few;
     const size_t bh = size_t(b) * Hkv + h;
     const int first = len / kTB, had = len % kTB, total = had + cnt;   // counted from the start of block `first`
     const double place0 = double(a.r.base ? a.r.base[b / (c.shape.B / a.r.n_base)] : 0) + double(first) * kTB;
@@ -242,11 +245,11 @@ __global__ __launch_bounds__(2 * D, NEXT ? 3 : 4) void append_rotated_kernel(Tur
             for (int g = 0; g < kHeads; ++g)
                 q[g] = fresh(t) && g0 + g < G ? get(a.x.q + b * a.x.q_seq + (t - had) * a.x.q_token + (h * G + g0 + g) * D + at.oct * 8) : u32x4_t{0, 0, 0, 0};
         };
-        auto fetch_row = [&](int t) {
+        auto fetch_key = [&](int t) {
             if (keys) k = fresh(t) ? get(a.x.k + b * a.x.k_seq + (t - had) * a.x.k_token + h * D + at.oct * 8) : u32x4_t{0, 0, 0, 0};
-            if (queries) fetch(t, 0);
         };
-        fetch_row(w0 + 16 * i + at.grp);
+        fetch_key(w0 + 16 * i + at.grp);
+        if (queries) fetch(w0 + 16 * i + at.grp, 0);
         f64x2_t cs[8];
         first_turns(place0 + double(w0 + 16 * i + at.grp), cs);
 #pragma unroll 1
@@ -279,7 +282,8 @@ __global__ __launch_bounds__(2 * D, NEXT ? 3 : 4) void append_rotated_kernel(Tur
                 }
             }
             if (++i == 4 || !__any(fresh(t + 16))) break;
-            fetch_row(t + 16);
+            fetch_key(t + 16);
+            if (queries) fetch(t + 16, 0);
             if (pairs.any)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) cs[e] = turn_on(cs[e], on_s[pair0 + (NEXT ? e >> 1 : e)]);
@@ -291,7 +295,7 @@ __global__ __launch_bounds__(2 * D, NEXT ? 3 : 4) void append_rotated_kernel(Tur
         for (int r = 0; r < 4; ++r) to[r] = fresh(w0 + t0 + r) ? get(p + r * a.x.v_token) : u32x4_t{0, 0, 0, 0};
     };
     if (in_rows) {   // row by row: the query heads, the KV heads' keys and, where the tail takes them, values of each token
-        const int heads = c.shape.Hq + 2 * Hkv, row = (blockIdx.x - walks) * 16 + at.grp, i = row / heads, s = row - i * heads;
+        const int heads = c.shape.Hq + 2 * Hkv, row = walk * 16 + at.grp, i = row / heads, s = row - i * heads;
         const bool is_q = s < c.shape.Hq, is_k = !is_q && s < c.shape.Hq + Hkv;
         if (i < cnt && (is_q ? a.q_out != nullptr : few)) {
             const int head = is_q ? s : (is_k ? s - c.shape.Hq : s - c.shape.Hq - Hkv);
@@ -366,13 +370,16 @@ constexpr int kFewTokens = 8;
 hipError_t launch_append_rotated(const akb_cache& c, const akb_tokens& x, const int32_t* n_new, int n, uint16_t* q_out, const akb_rotary& r, hipStream_t st)
 {
     const int blocks = (kTB - 1 + n + kTB - 1) / kTB;
-    // Few tokens: row by row, which leaves little to a workgroup
+    // Few tokens: row by row, 16 to a workgroup, which leaves little to any: 64 sequences of one token 22 / 12 us
     const int rows = n <= kFewTokens ? (n * (c.shape.Hq + 2 * c.shape.Hkv) + 15) / 16 : 0;
-    const dim3 grid(blocks * c.shape.Hkv + rows, c.shape.B);
+    // Workgroups of two waves (D = 64) that fit the card in a round or two leave the query heads to others: chunks of 777 tokens of 6 sequences, 4 x 4 heads 25.1 / 19.4 us; of four waves no
+    // gain (2 x 8 heads at D = 128 24.9 / 25.7)
+    const bool apart = rows == 0 && q_out && c.shape.D == 64 && long(blocks) * c.shape.Hkv * c.shape.B <= 1024;
+    const dim3 grid(blocks * c.shape.Hkv * (apart ? 2 : 1) + rows, c.shape.B);
     const bool ticketed = append_ticketed(c.shape, n);
     // as in the append: large calls pass the last-level cache by
     const bool streamed = (size_t(q_out ? 2 * c.shape.Hq : 0) + 2 * size_t(c.shape.Hkv)) * c.shape.B * n * c.shape.D * 2 > (size_t(128) << 20);
-    const TurnArgs a{c, x, r, n_new, n, q_out, ticketed ? 1 : 0, blocks, rows};
+    const TurnArgs a{c, x, r, n_new, n, q_out, ticketed ? 1 : 0, blocks, apart ? 1 : 0, rows};
     auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(2 * c.shape.D), 0, st, a); };
     auto pick = [&](auto type, auto width) {
         using T = decltype(type);
