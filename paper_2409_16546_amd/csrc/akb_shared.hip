@@ -209,6 +209,8 @@ struct SharedPlan {
     int tiles[2], groups[2], splits[2];
     size_t parts[2], total;     // offsets into the workspace, its size
 };
+// parts of each of `walks` walks that make up about `target` workgroups
+static long cut_into(long walks, long blocks, long target) { return std::max(1L, std::min((target + walks / 2) / walks, (blocks + kWaves - 1) / kWaves)); }
 constexpr int kOneWalkRows = 96;   // of a sequence, from which on one walk goes over both
 static SharedPlan plan(const akb_shape& f, const akb_shape& s, int n, int max_len, int prefix_max_len)
 {
@@ -225,20 +227,29 @@ static SharedPlan plan(const akb_shape& f, const akb_shape& s, int n, int max_le
         p.total = at + align256(size_t(2 * slots) * part_floats((int)std::min(seq_rows, long(kPromptRows)), s.D) * sizeof(float));
         return p;
     }
+    // Parts: a walk is cut so that each kind makes about one workgroup per compute unit (and no part is shorter than a block per wave): two prefix walks on a unit take from each other most of what they
+    // gain, and own walks fill the second place.  Both kinds to fill both places / one each, us: 16 x 64 heads 13000 + 3001 tokens 80 / 59, 4 x 32 heads 32768 + 100 21.3 / 19.1, 8 x 8
+    // heads 8192 + 2000 17.8 / 15.5, 8 prefixes of 8 x 32 heads 8192 + 500 43 / 38.  Row walks of more than about 30 us at that (1.9 us per four blocks) are cut further: 64 x 32 heads 32768 + 1000 68 / 62.6.
+    // Prefix walks of many rows take the prompt walk, which turns a block once for 128 of them, unless its parts were short: 640 rows 66.9 / 58.9 us, 1024 49.2 / 47.1, but 256 62.6 / 65.7 and 26.3 / 27.1
+    // (row walk / prompt walk).
+    const long units = slots / 2;
     for (int i = 0; i < 2; ++i) {
         constexpr int kPromptTiles = kPromptRows / 16;
-        const long prompt_items = pairs[i] * ((rows[i] + kPromptRows - 1) / kPromptRows);
-        p.tiles[i] = rows[i] <= 16 && i == 1 ? 1 : (i == 0 && rows[i] > 64 && blocks[i] >= 12 * parts_of(prompt_items, blocks[i], slots) ? kPromptTiles : 2);
+        const long prompt_walks = pairs[i] * ((rows[i] + kPromptRows - 1) / kPromptRows);
+        const bool prompt = i == 0 && rows[i] > 384 && blocks[i] >= 12 * cut_into(prompt_walks, blocks[i], units);
+        p.tiles[i] = prompt ? kPromptTiles : (i == 1 && rows[i] <= 16 ? 1 : 2);
         p.groups[i] = int((rows[i] + tile_rows(p.tiles[i]) - 1) / tile_rows(p.tiles[i]));
-        p.splits[i] = int(parts_of(pairs[i] * p.groups[i], blocks[i], slots));
+        const long walks = pairs[i] * p.groups[i];
+        const bool longer = i == 0 && !prompt && walks * blocks[i] > units * 64;
+        p.splits[i] = int(cut_into(walks, blocks[i], longer ? units * 7 / 4 : units));
         p.parts[i] = at;
-        at += align256(size_t(pairs[i]) * p.groups[i] * p.splits[i] * part_floats(tile_rows(p.tiles[i]), s.D) * sizeof(float));
+        at += align256(size_t(walks) * p.splits[i] * part_floats(tile_rows(p.tiles[i]), s.D) * sizeof(float));
     }
     p.total = at;
     return p;
 }
 // For calls of up to n query tokens: no kind of call needs more than this, whatever its number of tokens up to n and its bounds of the lengths.  Parts of walks that are
-// cut are at most 2 slots, of 128 rows or fewer; a walk that is not cut has its rows, filled up to a row group.
+// cut are fewer than 2 slots, of 128 rows or fewer; a walk that is not cut has its rows, filled up to a row group.
 size_t shared_workspace(const akb_shape& f, const akb_shape& s, int n)
 {
     const size_t slots = 2 * size_t(akv::compute_units()), G = s.Hq / s.Hkv, per = s.B / f.B;
