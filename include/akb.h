@@ -161,11 +161,17 @@ akv_status akb_evict(const akb_cache *src, const akb_cache *dst, int32_t keep, i
  * stand in the prefix.  prefix and cache have the same Hq, Hkv, D and dtype; neither is written.  q, n_q, out, the limit on row tiles, rows behind n_q[b], and rows that
  * see nothing: as for akb_attention; params: as there, max_len bounds the own lengths, prefix_max_len (0: the prefix's Ncap) those of the prefix; both are hints.
  * params->accumulate is refused: weights over a prefix belong to no one sequence.
- * workspace: as for akb_attention, of akb_attention_shared_workspace(prefix's shape, shape, n) bytes or more.  The same call gives the same bits.
+ * workspace: as for akb_attention, of akb_attention_shared_workspace(prefix's shape, shape, n) bytes or more (enough for calls of up to n query tokens; host
+ * computation, 0 on bad shapes).  The same call gives the same bits.
  */
 size_t akb_attention_shared_workspace(const akb_shape *prefix, const akb_shape *shape, int32_t n);
 akv_status akb_attention_shared(const akb_cache *prefix, const akb_cache *cache, const uint16_t *q, const int32_t *n_q, int32_t n, void *out,
                                 const akb_params *params, int32_t prefix_max_len, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Which kernels akb_attention_shared takes for n query tokens: 1 = walks over the prefixes for the rows of all their sequences by row groups of 32, walks over own tokens beside
+ * them; 2 = the same with row groups of 128 over the prefixes; 3 = one walk of a sequence's rows over its prefix and its own tokens.  parts: NULL, or a host pointer that receives
+ * two numbers, the parts that a walk over a prefix and one over own tokens are cut into (3: twice those of the one walk).  Host computation; 0 on bad shapes. */
+int32_t akb_attention_shared_path(const akb_shape *prefix, const akb_shape *shape, int32_t n, int32_t max_len, int32_t prefix_max_len, int32_t *parts);
 
 /* How keys and queries are normed and turned (above): with angles made in binary64, keys in binary64 and queries in binary32, each result rounded once, to the 16-bit type. */
 typedef struct akb_rotary {

@@ -29,7 +29,7 @@ EXPORTS = ["akv_version", "akv_last_error", "akv_layout_sizes", "akv_cache_reset
            "akw_layout_sizes", "akw_workspace_init", "akw_pack", "akw_unpack", "akw_gemv"]
 AKW_MAX_B = 4
 AKB_EXPORTS = ["akb_layout_sizes", "akb_cache_reset", "akb_append", "akb_attention_workspace", "akb_workspace_init", "akb_attention_path", "akb_attention_join", "akb_attention", "akb_evict_workspace", "akb_evict",
-               "akb_attention_shared_workspace", "akb_attention_shared", "akb_append_rotated", "akb_fork", "akb_truncate", "akb_unpack"]
+               "akb_attention_shared_workspace", "akb_attention_shared", "akb_attention_shared_path", "akb_append_rotated", "akb_fork", "akb_truncate", "akb_unpack"]
 AKB_TB, AKB_MAX_G = 64, 16
 AKB_DTYPES = {torch.float16: 0, torch.bfloat16: 1}
 
@@ -185,6 +185,8 @@ def lib() -> C.CDLL:
         L.akb_attention_shared.restype = C.c_int
         L.akb_attention_shared.argtypes = [C.POINTER(akb_cache), C.POINTER(akb_cache), C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.POINTER(akb_params), C.c_int32,
                                            C.c_void_p, C.c_size_t, C.c_void_p]
+        L.akb_attention_shared_path.restype = C.c_int32
+        L.akb_attention_shared_path.argtypes = [C.POINTER(akb_shape), C.POINTER(akb_shape), C.c_int32, C.c_int32, C.c_int32, C.POINTER(C.c_int32)]
         L.akb_append_rotated.restype = C.c_int
         L.akb_append_rotated.argtypes = [C.POINTER(akb_cache), C.POINTER(akb_tokens), C.c_void_p, C.c_int32, C.c_void_p, C.POINTER(akb_rotary), C.c_void_p]
         L.akb_fork.restype = C.c_int
@@ -701,6 +703,14 @@ def akb_attention_shared(prefix: BlockCache, cache: BlockCache, q: torch.Tensor,
     p = cache.params(scale, 0 if out.dtype == torch.float32 else 1, 0, max_len)
     _check(lib().akb_attention_shared(prefix.ref(), cache.ref(), _ptr(q), _ptr(n_q), n, _ptr(out), p, prefix_max_len, _ptr(ws), _nbytes(ws), _stream()))
     return out
+
+
+def akb_attention_shared_path(Bp: int, B: int, Hq: int, Hkv: int, D: int, P: int, Ncap: int, n: int = 1, max_len: int = 0, prefix_max_len: int = 0) -> tuple[int, int, int]:
+    """(1, 2 or 3: walks over prefixes by row groups of 32, of 128, one walk over prefix and own tokens; parts of a prefix walk, of an own walk): what akb_attention_shared takes
+    for Bp prefixes of capacity P and B sequences of capacity Ncap."""
+    parts = (C.c_int32 * 2)()
+    path = lib().akb_attention_shared_path(C.byref(akb_shape(Bp, Hq, Hkv, D, P, 0)), C.byref(akb_shape(B, Hq, Hkv, D, Ncap, 0)), n, max_len, prefix_max_len, parts)
+    return int(path), parts[0], parts[1]
 
 
 def _projected(t: torch.Tensor | None, cache: BlockCache, n: int, heads: int) -> tuple:

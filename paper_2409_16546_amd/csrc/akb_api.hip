@@ -224,6 +224,14 @@ akv_status akb_attention_shared(const akb_cache* prefix, const akb_cache* cache,
     return hip_result(akb::launch_shared(*prefix, prefix_max_len > 0 ? prefix_max_len : f.Ncap, a, static_cast<hipStream_t>(stream)), "shared attention launch");
 }
 
+int32_t akb_attention_shared_path(const akb_shape* prefix, const akb_shape* shape, int32_t n, int32_t max_len, int32_t prefix_max_len, int32_t* parts)
+{
+    if (!prefix || !shape || !shape_ok(*prefix) || !shape_ok(*shape) || !shares_ok(*prefix, *shape) || n < 1 || n > shape->Ncap || max_len < 0 || max_len > shape->Ncap ||
+        prefix_max_len < 0 || prefix_max_len > prefix->Ncap)
+        return 0;
+    return akb::shared_path(*prefix, *shape, n, max_len > 0 ? max_len : shape->Ncap, prefix_max_len > 0 ? prefix_max_len : prefix->Ncap, parts);
+}
+
 akv_status akb_append_rotated(const akb_cache* cache, const akb_tokens* tokens, const int32_t* n_new, int32_t n, uint16_t* q_out, const akb_rotary* rotary,
                               void* stream)
 {
@@ -237,6 +245,7 @@ akv_status akb_append_rotated(const akb_cache* cache, const akb_tokens* tokens, 
     if (r.rot > 0 && !r.inv_freq) return fail(AKV_EINVAL, "inv_freq is NULL");
     if (r.base && (r.n_base < 1 || s.B % r.n_base != 0)) return fail(AKV_EINVAL, "n_base = %d does not divide B = %d", r.n_base, s.B);
     if ((r.q_norm || r.k_norm) && !(std::isfinite(r.eps) && r.eps >= 0.f)) return fail(AKV_EINVAL, "eps is negative or not finite");
+    if ((size_t(n) + 126) / AKB_TB * s.Hkv >= size_t(1) << 23) return fail(AKV_EINVAL, "%d tokens of %d KV heads: 2^23 blocks or more of a sequence", n, s.Hkv);
     if (n == 0) return AKV_OK;
     if (!x.k || !x.v) return fail(AKV_EINVAL, "k / v is NULL");
     if (!x.q != !q_out) return fail(AKV_EINVAL, "one of q and q_out is NULL, the other is not");

@@ -36,6 +36,7 @@ int attention_path(const akb_shape& s, int n, int max_len, int32_t* parts);   //
 int attention_join(const akb_shape& s, int n, int max_len);                    // akb_attention_join
 hipError_t launch_attention(const AttentionArgs& a, hipStream_t st);
 size_t shared_workspace(const akb_shape& prefix, const akb_shape& s, int n);
+int shared_path(const akb_shape& prefix, const akb_shape& s, int n, int max_len, int prefix_max_len, int32_t* parts);   // akb_attention_shared_path
 hipError_t launch_shared(const akb_cache& prefix, int prefix_max_len, const AttentionArgs& a, hipStream_t st);
 bool append_ticketed(const akb_shape& s, int n);   // the appends' workgroups move the lengths themselves
 hipError_t launch_append_lens(const akb_cache& c, const int32_t* n_new, int n, hipStream_t st);   // otherwise: behind them

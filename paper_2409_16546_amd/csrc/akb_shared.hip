@@ -263,6 +263,14 @@ size_t shared_workspace(const akb_shape& f, const akb_shape& s, int n)
     return total;
 }
 
+int shared_path(const akb_shape& f, const akb_shape& s, int n, int max_len, int prefix_max_len, int32_t* parts)
+{
+    const SharedPlan p = plan(f, s, n, max_len, prefix_max_len);
+    if (parts)
+        for (int i = 0; i < 2; ++i) parts[i] = p.splits[p.one_walk ? 1 : i];
+    return p.one_walk ? 3 : (p.tiles[0] > 2 ? 2 : 1);
+}
+
 template <class T, int D> static hipError_t launch(const StepArgs& a, const SharedPlan& p, unsigned items, hipStream_t st)
 {
     auto go = [&](auto f32, auto b16) {
@@ -302,6 +310,7 @@ hipError_t launch_shared(const akb_cache& prefix, int prefix_max_len, const Atte
     StepArgs r{{side(0, prefix, per), side(1, a.c, 1)}, 0, a.q, a.n_q, a.n, G, a.out_dtype, a.out, a.c2};
     r.items = unsigned(prefix.shape.B) * s.Hkv * p.groups[0] * p.splits[0];
     const unsigned items = r.items + unsigned(s.B) * s.Hkv * p.groups[1] * p.splits[1];
+    if (items >= 1u << 24) return hipErrorInvalidConfiguration;   // (a launch has fewer than 2^32 threads)
     if (s.dtype == AKB_FP16) return s.D == 64 ? launch<Fp16, 64>(r, p, items, st) : launch<Fp16, 128>(r, p, items, st);
     return s.D == 64 ? launch<Bf16, 64>(r, p, items, st) : launch<Bf16, 128>(r, p, items, st);
 }
