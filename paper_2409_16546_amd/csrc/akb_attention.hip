@@ -113,7 +113,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void rows_kernel(RowArgs a)
         st[k].init(row < m * G ? a.q + place(row) : nullptr, row_limit(a, row, G, m, len), lane);
     }
     float* logits = RT == 1 && a.logits ? a.logits + bh * min(a.n * G, 16) * c.shape.Ncap : nullptr;
-    walk_rows<T, D, EXACT, RT, NT>(c, bh, st, lo, hi, len, all_see, a.c2, lane, wave, logits, rows);
+    walk_rows<T, D, EXACT, RT, NT, kWaves>(c, bh, st, lo, hi, len, all_see, a.c2, lane, wave, logits, rows);
     const int part = part_floats(rows, D);
     const __amdgpu_buffer_rsrc_t parts = akv::make_rsrc(a.parts + size_t(w - split) * part_floats(min(n * G, kRows), D), uint32_t(splits) * part * 4u);
 #pragma unroll

@@ -114,18 +114,18 @@ __device__ __forceinline__ void store_logits(float* block, const f32x4_t (&s)[4]
     for (int t = 0; t < 4; ++t) *reinterpret_cast<f32x4_t*>(block + (t * rows + row) * 16 + 4 * (lane >> 4)) = s[t];
 }
 
-// Blocks lo .. hi - 1 of (sequence, KV head) bh, which has len tokens, for RT tiles of 16 rows, `all_see` tokens of which every row sees: wave w takes every fourth block.
+// Blocks lo + at, lo + at + STEP, .. below hi of (sequence, KV head) bh, which has len tokens, for RT tiles of 16 rows, `all_see` tokens of which every row sees.
 // logits: where the products are left for the score (one tile of `rows` rows), or NULL.
-template <class T, int D, bool EXACT, int RT, bool NT>
-__device__ __forceinline__ void walk_rows(const akb_cache& c, size_t bh, RowState<T, D> (&st)[RT], int lo, int hi, int len, int all_see, float c2, int lane, int wave, float* logits,
+template <class T, int D, bool EXACT, int RT, bool NT, int STEP>
+__device__ __forceinline__ void walk_rows(const akb_cache& c, size_t bh, RowState<T, D> (&st)[RT], int lo, int hi, int len, int all_see, float c2, int lane, int at, float* logits,
                                           int rows)
 {
     const int whole = min(hi, len / kTB);   // blocks in 8 bits
     const size_t block0 = bh * (c.shape.Ncap / kTB);
-    int blk = lo + wave;
+    int blk = lo + at;
     KCodes<D, NT> kc;
     if (blk < whole) kc.load(c, block0 + blk, lane);
-    for (; blk < whole; blk += kWaves) {
+    for (; blk < whole; blk += STEP) {
         VCodes<D, NT> vc;
         vc.load(c, block0 + blk, lane);
         const float k_scale = pow2(int8_t(kc.e)), v_scale = pow2(int8_t(kc.e >> 8)), unit = weight_bits<T>(v_scale >= pow2(kLargeExp));
@@ -141,7 +141,7 @@ __device__ __forceinline__ void walk_rows(const akb_cache& c, size_t bh, RowStat
                 for (int k = 0; k < RT; ++k) s[k][t] = T::mfma16(x, st[k].q[i], s[k][t]);
             }
         }
-        if (blk + kWaves < whole) kc.load(c, block0 + blk + kWaves, lane);
+        if (blk + STEP < whole) kc.load(c, block0 + blk + STEP, lane);
         if (RT == 1 && logits) store_logits(logits + size_t(blk) * kTB * rows, s[0], rows, lane & 15, lane);
         const bool masked = (blk + 1) * kTB > all_see;
         u32x4_t ph[RT][2], pl[RT][2], pr[RT][2];

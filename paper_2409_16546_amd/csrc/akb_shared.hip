@@ -24,6 +24,7 @@ struct StepArgs {
     int n, G, out_dtype;
     void* out;
     float c2;
+    int solo;           // an own walk is a wave's alone
 };
 // rows of a row group of TILES tiles (8: the prompt walk)
 constexpr int tile_rows(int tiles) { return 16 * tiles; }
@@ -41,7 +42,8 @@ struct StepRow {
 };
 __device__ __forceinline__ int queries(const StepArgs& a, int b) { return a.n_q ? min(max(a.n_q[b], 0), a.n) : a.n; }
 
-template <class T, int D, bool EXACT, int TILES, bool PREFIX>
+// SOLO: by this wave alone, which meets no other
+template <class T, int D, bool EXACT, int TILES, bool PREFIX, bool SOLO>
 __device__ __forceinline__ void step_walk(const StepArgs& a, unsigned item, char* lds)
 {
     const Side& s = a.side[PREFIX ? 0 : 1];
@@ -84,8 +86,23 @@ __device__ __forceinline__ void step_walk(const StepArgs& a, unsigned item, char
             st[k].init(q, limit, lane);
             if (__any(limit < len)) all_see = 0;
         }
-        walk_rows<T, D, EXACT, TILES, false>(c, pair, st, lo, hi, len, all_see, a.c2, lane, wave, nullptr, 0);
+        walk_rows<T, D, EXACT, TILES, false, SOLO ? 1 : kWaves>(c, pair, st, lo, hi, len, all_see, a.c2, lane, SOLO ? 0 : wave, nullptr, 0);
         const int rows = min(tile_rows(TILES), all_rows - row0);
+        if (SOLO) {
+#pragma unroll
+            for (int k = 0; k < TILES; ++k) {
+                const int r = 16 * k + (lane & 15);
+                const float z = akv::add_lane32(akv::add_lane16(st[k].z));
+                if (r >= rows) continue;
+                if (lane < 16) {
+                    part[2 * r] = st[k].m;
+                    part[2 * r + 1] = z;
+                }
+#pragma unroll
+                for (int i = 0; i < D / 16; ++i) *reinterpret_cast<f32x4_t*>(part + part_head(tile_rows(TILES)) + r * D + 16 * i + 4 * (lane >> 4)) = st[k].o[i];
+            }
+            return;
+        }
 #pragma unroll
         for (int k = 0; k < TILES; ++k) {
             if (16 * k >= rows) break;
@@ -156,9 +173,12 @@ __global__ __launch_bounds__(64 * kWaves, 2) void step_kernel(StepArgs a)
             const unsigned x = w % akv::kXcds, i = w / akv::kXcds;
             w = (x + akv::kXcds * (i / per_pair)) * per_pair + i % per_pair;
         }
-        step_walk<T, D, EXACT, PREFIX_TILES, true>(a, w, lds);
+        step_walk<T, D, EXACT, PREFIX_TILES, true, false>(a, w, lds);
+    } else if (a.solo) {
+        const unsigned item = (w - a.items) * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        if (item < unsigned(a.side[1].c.shape.B) * a.side[1].c.shape.Hkv * a.side[1].groups) step_walk<T, D, EXACT, OWN_TILES, false, true>(a, item, lds);
     } else {
-        step_walk<T, D, EXACT, OWN_TILES, false>(a, w - a.items, lds);
+        step_walk<T, D, EXACT, OWN_TILES, false, false>(a, w - a.items, lds);
     }
 }
 
@@ -206,6 +226,7 @@ __global__ __launch_bounds__(256) void step_join_kernel(StepArgs a, int prefix_r
 // How a call is cut.
 struct SharedPlan {
     bool one_walk;              // prefix and own blocks by one walk
+    bool solo;                  // an own walk is a wave's alone
     int tiles[2], groups[2], splits[2];
     size_t parts[2], total;     // offsets into the workspace, its size
 };
@@ -229,22 +250,24 @@ static SharedPlan plan(const akb_shape& f, const akb_shape& s, int n, int max_le
     }
     // Parts: a walk is cut so that each kind makes about one workgroup per compute unit (and no part is shorter than a block per wave): two prefix walks on a unit take from each other most of what they
     // gain, and own walks fill the second place.  Both kinds to fill both places / one each, us: 16 x 64 heads 13000 + 3001 tokens 80 / 59, 4 x 32 heads 32768 + 100 21.3 / 19.1, 8 x 8
-    // heads 8192 + 2000 17.8 / 15.5, 8 prefixes of 8 x 32 heads 8192 + 500 43 / 38.  Row walks of more than about 30 us at that (1.9 us per four blocks) are cut further: 64 x 32 heads 32768 + 1000 68 / 62.6.
-    // Prefix walks of many rows take the prompt walk, which turns a block once for 128 of them, unless its parts were short: 640 rows 66.9 / 58.9 us, 1024 49.2 / 47.1, but 256 62.6 / 65.7 and 26.3 / 27.1
-    // (row walk / prompt walk).
+    // heads 8192 + 2000 17.8 / 15.5, 8 prefixes of 8 x 32 heads 8192 + 500 43 / 38.  Row walks that take some 30 us at that (1.9 us per four blocks) are cut further: 64 x 32 heads 32768 + 1000 68 / 62.6, 20 x
+    // 11 rows of 4 heads 4000 + 100 41 / 34.
+    // Prefix walks of many rows take the prompt walk, which turns a block once for 128 of them; row walk / prompt walk, us: 256 rows 62.6 / 65.7 and 26.3 / 27.1, 440 34.2 / 36.0, 640 66.9 / 58.9, 816 over
+    // 163 tokens 38.0 / 30.9, 1024 49.2 / 47.1, 1440 38.7 / 37.9.
     const long units = slots / 2;
     for (int i = 0; i < 2; ++i) {
         constexpr int kPromptTiles = kPromptRows / 16;
-        const long prompt_walks = pairs[i] * ((rows[i] + kPromptRows - 1) / kPromptRows);
-        const bool prompt = i == 0 && rows[i] > 384 && blocks[i] >= 12 * cut_into(prompt_walks, blocks[i], units);
+        const bool prompt = i == 0 && rows[i] > 512;
         p.tiles[i] = prompt ? kPromptTiles : (i == 1 && rows[i] <= 16 ? 1 : 2);
         p.groups[i] = int((rows[i] + tile_rows(p.tiles[i]) - 1) / tile_rows(p.tiles[i]));
         const long walks = pairs[i] * p.groups[i];
-        const bool longer = i == 0 && !prompt && walks * blocks[i] > units * 64;
+        const bool longer = i == 0 && !prompt && walks * blocks[i] > units * 48;
         p.splits[i] = int(cut_into(walks, blocks[i], longer ? units * 7 / 4 : units));
         p.parts[i] = at;
         at += align256(size_t(walks) * p.splits[i] * part_floats(tile_rows(p.tiles[i]), s.D) * sizeof(float));
     }
+    // Own walks of few blocks that are more than run at a time, one to a wave: 256 x 32 heads 4096 + 200 tokens 48.5 / 44, 120 x 64 heads of D = 64 2753 + 5 34 / 30 us; but 16 x 32 heads 8192 + 250 16.2 / 19.5
+    p.solo = long(pairs[1]) * p.groups[1] > slots && blocks[1] <= 4;
     p.total = at;
     return p;
 }
@@ -307,9 +330,9 @@ hipError_t launch_shared(const akb_cache& prefix, int prefix_max_len, const Atte
         return p.splits[1] > 1 ? launch_join(r, kPromptRows, st) : hipSuccess;
     }
     auto side = [&](int i, const akb_cache& c, int per) { return Side{c, per, p.groups[i], p.splits[i], reinterpret_cast<float*>(a.ws + p.parts[i])}; };
-    StepArgs r{{side(0, prefix, per), side(1, a.c, 1)}, 0, a.q, a.n_q, a.n, G, a.out_dtype, a.out, a.c2};
+    StepArgs r{{side(0, prefix, per), side(1, a.c, 1)}, 0, a.q, a.n_q, a.n, G, a.out_dtype, a.out, a.c2, p.solo ? 1 : 0};
     r.items = unsigned(prefix.shape.B) * s.Hkv * p.groups[0] * p.splits[0];
-    const unsigned items = r.items + unsigned(s.B) * s.Hkv * p.groups[1] * p.splits[1];
+    const unsigned own = unsigned(s.B) * s.Hkv * p.groups[1] * p.splits[1], items = r.items + (p.solo ? (own + kWaves - 1) / kWaves : own);
     if (items >= 1u << 24) return hipErrorInvalidConfiguration;   // (a launch has fewer than 2^32 threads)
     if (s.dtype == AKB_FP16) return s.D == 64 ? launch<Fp16, 64>(r, p, items, st) : launch<Fp16, 128>(r, p, items, st);
     return s.D == 64 ? launch<Bf16, 64>(r, p, items, st) : launch<Bf16, 128>(r, p, items, st);

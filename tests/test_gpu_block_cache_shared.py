@@ -82,6 +82,10 @@ LARGE = [  # dtype, out, D, prefixes, sequences, Hq, Hkv, P, N, n: against 64 bi
     (B16, B16, 64, 1, 100, 16, 1, 30000, 64, 1),
     (F16, F32, 128, 1, 1, 8, 1, 66000, 500, 2),
     (F16, F16, 128, 8, 8, 12, 4, 300, 900, 100),
+    (B16, F32, 128, 1, 20, 32, 8, 3500, 200, 9),       # prompt walks over the prefix, row walks over own tokens
+    (F16, F16, 64, 2, 40, 40, 8, 700, 130, 7),
+    (F16, F32, 64, 2, 140, 8, 8, 200, 150, 5),         # own walks by a wave alone, in one tile of rows
+    (B16, B16, 128, 3, 180, 24, 8, 100, 200, 7),       # ... in two
 ]
 
 
