@@ -10,6 +10,7 @@
 
 namespace akb {
 
+constexpr int kApart = 4;   // query heads of a workgroup of their own
 struct TurnArgs {
     akb_cache c;
     akb_tokens x;
@@ -18,8 +19,8 @@ struct TurnArgs {
     int n;
     uint16_t* q_out;
     int ticketed;
-    // Workgroups of a sequence: `blocks` x KV heads, each of which has 64 tokens of a KV head and, unless `apart`, of its query heads; where apart, as many for the query
-    // heads; where the tokens are few, `rows` that have 16 rows each
+    // Workgroups of a sequence: `blocks` x KV heads, each of which has 64 tokens of a KV head and, unless `apart`, of its query heads; where apart, as many for every
+    // kApart of the query heads (`apart` parts); where the tokens are few, `rows` that have 16 rows each
     int blocks, apart, rows;
 };
 typedef double f64x2_t __attribute__((ext_vector_type(2)));
@@ -53,25 +54,36 @@ __device__ __forceinline__ f64x2_t cos_sin(double place, float freq)
 // Which pair each of a thread's eight channels belongs to, and where the other channel of it is.  NEXT: pairs of neighbours (akb_rotary.pairs).
 template <int D, bool NEXT> struct Pairs {
     int first, step;      // number of the first channel's pair; how many octets (lanes) further the partners are
-    int lane;
+    int partner;          // four times their lane
     bool any;
     uint32_t minus;       // sign bit where these channels are the first of their pairs, which take their partners times -sin (NEXT: every other one is)
-    __device__ __forceinline__ Pairs(int rot, int oct, int lane_) : lane(lane_)
+    __device__ __forceinline__ Pairs(int rot, int oct, int lane)
     {
         const int half = rot / 16;   // octets
         const bool low = oct < half;
         any = oct * 8 < rot;
         step = !any || NEXT ? 0 : (low ? half : -half);
+        partner = 4 * (lane + step);
         first = !any ? 0 : (NEXT ? oct * 4 : (low ? oct : oct - half) * 8);
         minus = low ? 0x80000000u : 0u;
     }
     // a partner's number with the sign that its sine has
     __device__ __forceinline__ float signed_for(int e, float v) const { return NEXT ? (e & 1 ? v : -v) : bits_float(float_bits(v) ^ minus); }
+    __device__ __forceinline__ uint32_t other(uint32_t w) const { return uint32_t(__builtin_amdgcn_ds_bpermute(partner, int(w))); }
+    __device__ __forceinline__ double other(double v) const
+    {
+        const u32x2_t w = __builtin_bit_cast(u32x2_t, v);
+        const uint32_t lo = w.x, hi = w.y;
+        return __builtin_bit_cast(double, u32x2_t{other(lo), other(hi)});
+    }
     __device__ __forceinline__ u32x4_t others(const u32x4_t& x) const
     {
         u32x4_t p;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) p[k] = NEXT ? x[k] >> 16 | x[k] << 16 : uint32_t(__shfl(int(x[k]), lane + step));
+        for (int k = 0; k < 4; ++k) {
+            const uint32_t w = x[k];
+            p[k] = NEXT ? w >> 16 | w << 16 : other(w);
+        }
         return p;
     }
 };
@@ -138,10 +150,10 @@ __global__ __launch_bounds__(2 * D, NEXT ? 3 : 4) void append_rotated_kernel(Tur
     __shared__ u32x4_t norm_s[2][D / 8];   // the norms' weights, of queries and of keys
     const akb_cache& c = a.c;
     const int tid = threadIdx.x, lane = tid & 63, b = blockIdx.y;
-    const int Hkv = c.shape.Hkv, walks = a.blocks * Hkv, Ncap = c.shape.Ncap, G = c.shape.Hq / Hkv, n = a.n;
+    const int Hkv = c.shape.Hkv, walks = a.blocks * Hkv, Ncap = c.shape.Ncap, n = a.n;
     const bool behind = int(blockIdx.x) >= walks, in_rows = behind && a.rows > 0;
     // (a head's blocks one behind the other: the heads of a block beside each other 162 us of 4 x 8192 tokens for 151)
-    const int walk = behind ? blockIdx.x - walks : blockIdx.x, h = walk / a.blocks, j = walk % a.blocks;
+    const int walk = behind ? blockIdx.x - walks : blockIdx.x, h = walk / a.blocks % Hkv, j = walk % a.blocks;
     const int len = seq_len(c, b), cnt = a.n_new ? min(max(a.n_new[b], 0), n) : n;
     if (cnt == 0) return;
     if (len + cnt > Ncap) {   // the sequence is left unchanged
@@ -175,7 +187,7 @@ __global__ __launch_bounds__(2 * D, NEXT ? 3 : 4) void append_rotated_kernel(Tur
             if (NEXT) {
                 cs[2 * e] = cs[2 * e + 1] = made[e];
             } else {
-                const f64x2_t other = {__shfl(made[e][0], lane + pairs.step), __shfl(made[e][1], lane + pairs.step)};
+                const f64x2_t other = {pairs.other(made[e][0]), pairs.other(made[e][1])};
                 cs[e] = pairs.minus ? made[e] : other;
                 cs[4 + e] = pairs.minus ? other : made[e];
             }
@@ -230,6 +242,7 @@ __global__ __launch_bounds__(2 * D, NEXT ? 3 : 4) void append_rotated_kernel(Tur
     };
     // The new tokens among the 64 from w0 on: keys to LDS (for a complete block) or to the tail; queries to q_out
     auto turn_rows = [&](int w0, bool keys, bool to_tail, bool queries) {
+        const int G = c.shape.Hq / Hkv, part = behind ? walk / walks * kApart : 0, head0 = h * G + part, heads = behind ? min(kApart, G - part) : G;   // the query heads
         const int begin = max(had - w0, 0), end = min(total - w0, kTB) - 1;
         if (begin / 16 != end / 16) {   // (otherwise nothing is turned on)
             if (tid < a.r.rot / 2) on_s[tid] = cos_sin(16.0, a.r.inv_freq[tid]);
@@ -243,7 +256,7 @@ __global__ __launch_bounds__(2 * D, NEXT ? 3 : 4) void append_rotated_kernel(Tur
         auto fetch = [&](int t, int g0) {   // the query rows of some heads
 #pragma unroll
             for (int g = 0; g < kHeads; ++g)
-                q[g] = fresh(t) && g0 + g < G ? get(a.x.q + b * a.x.q_seq + (t - had) * a.x.q_token + (h * G + g0 + g) * D + at.oct * 8) : u32x4_t{0, 0, 0, 0};
+                q[g] = fresh(t) && g0 + g < heads ? get(a.x.q + b * a.x.q_seq + (t - had) * a.x.q_token + (head0 + g0 + g) * D + at.oct * 8) : u32x4_t{0, 0, 0, 0};
         };
         auto fetch_key = [&](int t) {
             if (keys) k = fresh(t) ? get(a.x.k + b * a.x.k_seq + (t - had) * a.x.k_token + h * D + at.oct * 8) : u32x4_t{0, 0, 0, 0};
@@ -270,14 +283,14 @@ __global__ __launch_bounds__(2 * D, NEXT ? 3 : 4) void append_rotated_kernel(Tur
                 for (int g0 = 0;;) {
 #pragma unroll
                     for (int g = 0; g < kHeads; ++g) {
-                        if (g0 + g >= G) break;
+                        if (g0 + g >= heads) break;
                         const u32x4_t z = turn_query_by(q[g], cw, sw);
                         if (!mine) continue;
-                        u32x4_t* out = reinterpret_cast<u32x4_t*>(a.q_out + ((bh * G + g0 + g) * n + (t - had)) * D + at.oct * 8);
+                        u32x4_t* out = reinterpret_cast<u32x4_t*>(a.q_out + ((size_t(b) * c.shape.Hq + head0 + g0 + g) * n + (t - had)) * D + at.oct * 8);
                         if (NT) __builtin_nontemporal_store(z, out);
                         else *out = z;
                     }
-                    if ((g0 += kHeads) >= G) break;
+                    if ((g0 += kHeads) >= heads) break;
                     fetch(t, g0);
                 }
             }
@@ -372,14 +385,16 @@ hipError_t launch_append_rotated(const akb_cache& c, const akb_tokens& x, const 
     const int blocks = (kTB - 1 + n + kTB - 1) / kTB;
     // Few tokens: row by row, 16 to a workgroup, which leaves little to any: 64 sequences of one token 22 / 12 us
     const int rows = n <= kFewTokens ? (n * (c.shape.Hq + 2 * c.shape.Hkv) + 15) / 16 : 0;
-    // Workgroups of two waves (D = 64) that fit the card in a round or two leave the query heads to others: chunks of 777 tokens of 6 sequences, 4 x 4 heads 25.1 / 19.4 us; of four waves no
-    // gain (2 x 8 heads at D = 128 24.9 / 25.7)
-    const bool apart = rows == 0 && q_out && c.shape.D == 64 && long(blocks) * c.shape.Hkv * c.shape.B <= 1024;
-    const dim3 grid(blocks * c.shape.Hkv * (apart ? 2 : 1) + rows, c.shape.B);
+    // Where they are few, workgroups of two waves (D = 64) and those of many query heads leave the query heads to others: chunks of 777 tokens of 6 sequences, 4 x 4 heads of D = 64 25.1 / 19.4 us; 2 KV heads
+    // of 16 at D = 128, 2 sequences 47 / 22 us, and 144 tokens 33 / 14; 8 of 16, 2048 tokens 74 / 58; but 8 of 8, 8 sequences of 777 62.7 / 68.7, and with four heads no gain (2 x 8 24.9 / 25.7)
+    const int G = c.shape.Hq / c.shape.Hkv;
+    const long walks = long(blocks) * c.shape.Hkv * c.shape.B;
+    const int apart = rows == 0 && q_out && (c.shape.D == 64 ? walks <= 1024 : (G > kApart && walks <= 512)) ? (G + kApart - 1) / kApart : 0;
+    const dim3 grid(blocks * c.shape.Hkv * (1 + apart) + rows, c.shape.B);
     const bool ticketed = append_ticketed(c.shape, n);
     // as in the append: large calls pass the last-level cache by
     const bool streamed = (size_t(q_out ? 2 * c.shape.Hq : 0) + 2 * size_t(c.shape.Hkv)) * c.shape.B * n * c.shape.D * 2 > (size_t(128) << 20);
-    const TurnArgs a{c, x, r, n_new, n, q_out, ticketed ? 1 : 0, blocks, apart ? 1 : 0, rows};
+    const TurnArgs a{c, x, r, n_new, n, q_out, ticketed ? 1 : 0, blocks, apart, rows};
     auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(2 * c.shape.D), 0, st, a); };
     auto pick = [&](auto type, auto width) {
         using T = decltype(type);
