@@ -38,7 +38,7 @@
  *
  * Conventions: those of akv.h (device pointers owned by the caller unless named "host", nothing is allocated or
  * synchronised, work is enqueued on the caller's stream, akv_status / akv_last_error(), 16-byte alignment of every
- * device array, lens, flags, n_new and n_q 4 bytes).  Every call enqueues kernels only and can be captured into a HIP graph.
+ * device array; lens, flags, n_new, n_q, parents, upto, keep, base and inv_freq 4 bytes).  Every call enqueues kernels only and can be captured into a HIP graph.
  * Inputs of tokens that are stored must be finite; an infinity or a NaN is stored as a NaN in 8 bits and reaches every
  * query row of its head whose tile holds it.  What lies behind a sequence's length, behind n_new[b] rows of k_new and v_new
  * or behind n_q[b] rows of q may be anything.

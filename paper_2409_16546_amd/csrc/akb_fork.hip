@@ -5,24 +5,32 @@ namespace akb {
 
 constexpr int kThreads = 256;
 
-// One side of block `block` of c as the 16-bit tail `bh` of d holds it: 16 codes become 32 bytes per thread and turn, in the orders that both already have (K: a token's run
-// of channels; V: a channel's tokens).
-template <class T, int D> __device__ __forceinline__ void block_to_tail(const akb_cache& c, size_t block, const akb_cache& d, size_t bh, bool is_v, int tid)
-{
-    const float s = pow2(c.exps[block * 2 + (is_v ? 1 : 0)]);
-    const uint8_t* from = (is_v ? c.v8 : c.k8) + block * (kTB * D);
-    uint16_t* to = (is_v ? d.v_tail : d.k_tail) + bh * kTB * D;
-    u32x4_t w[D * 4 / kThreads];
+// One side of a block on its way to a 16-bit tail: 16 codes become 32 bytes per thread and turn, in the orders that both already have (K: a token's run of channels; V: a
+// channel's tokens)
+template <class T, int D> struct TailSide {
+    static constexpr int kTurns = D * 4 / kThreads;
+    u32x4_t w[kTurns];
+    int e;
+    __device__ __forceinline__ void load(const akb_cache& c, size_t block, bool is_v, int tid)
+    {
+        const u32x4_t* from = reinterpret_cast<const u32x4_t*>((is_v ? c.v8 : c.k8) + block * (kTB * D));
 #pragma unroll
-    for (int k = 0; k < D * 4 / kThreads; ++k) w[k] = reinterpret_cast<const u32x4_t*>(from)[tid + k * kThreads];
-#pragma unroll
-    for (int k = 0; k < D * 4 / kThreads; ++k) {
-        const int p = tid + k * kThreads, run = p >> 2, token = run / (16 * (D / 64)) * 16 + run % 16, i = run / 16 % (D / 64);   // k8: [4][D / 64][16] runs of 64 channels
-        u32x4_t* out = reinterpret_cast<u32x4_t*>(to + (is_v ? p * 16 : token * D + i * 64 + (p & 3) * 16));
-        out[0] = cvt8<T>(w[k][0], w[k][1], s);
-        out[1] = cvt8<T>(w[k][2], w[k][3], s);
+        for (int k = 0; k < kTurns; ++k) w[k] = from[tid + k * kThreads];
+        e = c.exps[block * 2 + (is_v ? 1 : 0)];
     }
-}
+    __device__ __forceinline__ void store(const akb_cache& d, size_t bh, bool is_v, int tid) const
+    {
+        const float s = pow2(e);
+        uint16_t* to = (is_v ? d.v_tail : d.k_tail) + bh * kTB * D;
+#pragma unroll
+        for (int k = 0; k < kTurns; ++k) {
+            const int p = tid + k * kThreads, run = p >> 2, token = run / (16 * (D / 64)) * 16 + run % 16, i = run / 16 % (D / 64);   // k8: [4][D / 64][16] runs of 64 channels
+            u32x4_t* out = reinterpret_cast<u32x4_t*>(to + (is_v ? p * 16 : token * D + i * 64 + (p & 3) * 16));
+            out[0] = cvt8<T>(w[k][0], w[k][1], s);
+            out[1] = cvt8<T>(w[k][2], w[k][3], s);
+        }
+    }
+};
 
 // `pieces` of 16 bytes, PER of them per thread and turn, all asked for before the first is stored
 template <int PER, bool NT> __device__ __forceinline__ void copy(const uint8_t* from, uint8_t* to, int pieces, int tid)
@@ -67,8 +75,11 @@ __global__ __launch_bounds__(kThreads) void fork_kernel(akb_cache c, akb_cache d
     if (is_v && c.score && d.score)
         for (int t = first * kTB + tid; t < min(len, (first + chunk) * kTB); t += kThreads) d.score[to * d.shape.Ncap + t] = c.score[from * c.shape.Ncap + t];
     if (len % kTB && whole >= first && whole < first + chunk) {   // the incomplete block
-        if (whole < had / kTB) block_to_tail<T, D>(c, from0 + whole, d, to, is_v, tid);
-        else copy<2, false>(reinterpret_cast<const uint8_t*>((is_v ? c.v_tail : c.k_tail) + from * kTB * D), reinterpret_cast<uint8_t*>((is_v ? d.v_tail : d.k_tail) + to * kTB * D), kTB * D / 8, tid);
+        if (whole < had / kTB) {
+            TailSide<T, D> s;
+            s.load(c, from0 + whole, is_v, tid);
+            s.store(d, to, is_v, tid);
+        } else copy<2, false>(reinterpret_cast<const uint8_t*>((is_v ? c.v_tail : c.k_tail) + from * kTB * D), reinterpret_cast<uint8_t*>((is_v ? d.v_tail : d.k_tail) + to * kTB * D), kTB * D / 8, tid);
     }
 }
 
@@ -104,10 +115,17 @@ __global__ __launch_bounds__(kThreads) void truncate_kernel(akb_cache c, const i
         c.flags[AKV_NFLAGS + b] = 0;
         c.lens[b] = len;
     }
-    for (int h = h0; h < min(h0 + heads, c.shape.Hkv); ++h) {
-        const size_t bh = size_t(b) * c.shape.Hkv + h, block = bh * (c.shape.Ncap / kTB) + blk;
-        block_to_tail<T, D>(c, block, c, bh, false, tid);
-        block_to_tail<T, D>(c, block, c, bh, true, tid);
+    const int end = min(h0 + heads, c.shape.Hkv);
+    for (int h = h0; h < end; h += 2) {   // two heads, both sides, at a time: all their codes are asked for before the first is stored
+        TailSide<T, D> s[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const size_t bh = size_t(b) * c.shape.Hkv + min(h + (i >> 1), end - 1);
+            s[i].load(c, bh * (c.shape.Ncap / kTB) + blk, i & 1, tid);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (h + (i >> 1) < end) s[i].store(c, size_t(b) * c.shape.Hkv + h + (i >> 1), i & 1, tid);
     }
 }
 

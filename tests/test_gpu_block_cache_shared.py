@@ -180,6 +180,20 @@ def test_the_prefix_is_what_a_cache_of_all_the_tokens_gives(A):
     R.assert_attention(b, ref, eps, mag, B16, "two")
 
 
+@pytest.mark.parametrize("n", [1, 5, 30])
+def test_a_query_that_is_not_finite_stays_with_its_row(A, n):
+    """Rows of many sequences lie in one tile: a NaN or an infinity in one is in no other's result."""
+    p, pr, c, cr = caches(A, 1, 20, 32, 8, 128, 2000, 100, B16, [2000], [100 - 4 * b for b in range(20)], n)
+    q = R.tokens(20, 32, n, 128, B16, 2, "plain").to(DEV)
+    want = A.akb_attention_shared(p, c, q).clone()
+    q[3, 5, n // 2, 7], q[17, 0, 0, 100] = float("nan"), float("inf")
+    got = A.akb_attention_shared(p, c, q)
+    same = (got == want).all(dim=-1)
+    bad = torch.zeros_like(same)
+    bad[3, 5, n // 2] = bad[17, 0, 0] = True
+    assert same[~bad].all() and torch.isnan(got[3, 5, n // 2]).all()
+
+
 def test_two_calls_at_once_on_a_prefix(A):
     """Two batches on two streams, one prefix, a workspace each; and a workspace of NaN bits, prepared, gives the same."""
     p, pr, c0, cr0 = caches(A, 1, 6, 16, 4, 128, 3000, 200, F16, [3000], [200, 3, 77, 64, 1, 130], 4)
