@@ -125,14 +125,14 @@ template <class T, int D> __device__ __forceinline__ double norm_scale(const u32
     y = y * fma(-0.5 * m * y, y, 1.5);
     return y * fma(-0.5 * m * y, y, 1.5);
 }
-// .. and in 32, unless the squares of some row of the wave have none there (far)
+// .. and in 32, unless this row's have none there (far: the same in all of its lanes)
 template <class T, int D> __device__ __forceinline__ float norm_scale32(const u32x4_t& x, float eps, bool& far)
 {
     float sum = 0.f;
 #pragma unroll
     for (int e = 0; e < 8; ++e) sum = fmaf(channel<T>(x, e), channel<T>(x, e), sum);
     sum = row_sum<D>(sum);
-    far = __any(!(sum > 0x1p-100f && sum < 0x1p120f));
+    far = !(sum > 0x1p-100f && sum < 0x1p120f);
     if (far) return float(norm_scale<T, D>(x, eps));
     return __builtin_amdgcn_rsqf(fmaf(sum, 1.f / D, eps));
 }

@@ -232,6 +232,7 @@ struct SharedPlan {
 };
 // parts of each of `walks` walks that make up about `target` workgroups
 static long cut_into(long walks, long blocks, long target) { return std::max(1L, std::min((target + walks / 2) / walks, (blocks + kWaves - 1) / kWaves)); }
+constexpr int kRowWalkRows = 512;  // over a prefix, up to which row walks have them
 constexpr int kOneWalkRows = 96;   // of a sequence, from which on one walk goes over both
 static SharedPlan plan(const akb_shape& f, const akb_shape& s, int n, int max_len, int prefix_max_len)
 {
@@ -257,7 +258,7 @@ static SharedPlan plan(const akb_shape& f, const akb_shape& s, int n, int max_le
     const long units = slots / 2;
     for (int i = 0; i < 2; ++i) {
         constexpr int kPromptTiles = kPromptRows / 16;
-        const bool prompt = i == 0 && rows[i] > 512;
+        const bool prompt = i == 0 && rows[i] > kRowWalkRows;
         p.tiles[i] = prompt ? kPromptTiles : (i == 1 && rows[i] <= 16 ? 1 : 2);
         p.groups[i] = int((rows[i] + tile_rows(p.tiles[i]) - 1) / tile_rows(p.tiles[i]));
         const long walks = pairs[i] * p.groups[i];
@@ -272,20 +273,19 @@ static SharedPlan plan(const akb_shape& f, const akb_shape& s, int n, int max_le
     return p;
 }
 // For calls of up to n query tokens: no kind of call needs more than this, whatever its number of tokens up to n and its bounds of the lengths.  Parts of walks that are
-// cut are fewer than 2 slots, of 128 rows or fewer; a walk that is not cut has its rows, filled up to a row group.
+// cut are fewer than 2 slots; a walk that is not cut has its rows, filled up to a row group.
 size_t shared_workspace(const akb_shape& f, const akb_shape& s, int n)
 {
-    const size_t slots = 2 * size_t(akv::compute_units()), G = s.Hq / s.Hkv, per = s.B / f.B;
-    const size_t seq_rows = std::min(size_t(std::max(n, 1)) * G, size_t(kOneWalkRows));   // (beyond, no more is needed)
-    size_t total = align256(attention_tickets());
-    const size_t pairs[2] = {size_t(f.B) * s.Hkv, size_t(s.B) * s.Hkv}, rows[2] = {per * seq_rows, seq_rows};
+    const size_t slots = 2 * size_t(akv::compute_units()), G = s.Hq / s.Hkv, rows_all = size_t(std::max(n, 1)) * G, seq_rows = std::min(rows_all, size_t(kOneWalkRows));
+    const size_t front = align256(attention_tickets()), pairs[2] = {size_t(f.B) * s.Hkv, size_t(s.B) * s.Hkv}, rows[2] = {size_t(s.B / f.B) * seq_rows, seq_rows};
+    size_t step = front;
     for (int i = 0; i < 2; ++i) {
-        const size_t cut = 2 * slots * part_floats(kPromptRows, s.D), whole = pairs[i] * ((rows[i] + kPromptRows - 1) / kPromptRows) * part_floats(kPromptRows, s.D);
-        total += align256(std::max(cut, whole) * sizeof(float));
+        const int tile = i == 0 && rows[i] > size_t(kRowWalkRows) ? kPromptRows : 32;
+        step += align256(std::max(2 * slots, pairs[i] * ((rows[i] + tile - 1) / tile)) * part_floats(tile, s.D) * sizeof(float));
     }
-    return total;
+    const size_t one = rows_all >= size_t(kOneWalkRows) ? front + align256(2 * slots * part_floats(kPromptRows, s.D) * sizeof(float)) : 0;
+    return std::max(step, one);
 }
-
 int shared_path(const akb_shape& f, const akb_shape& s, int n, int max_len, int prefix_max_len, int32_t* parts)
 {
     const SharedPlan p = plan(f, s, n, max_len, prefix_max_len);

@@ -175,3 +175,24 @@ def test_in_a_graph_that_is_replayed(A, n, B):
         torch.cuda.synchronize()
         assert torch.equal(outs[0], outs[1]) and torch.equal(caches[0].lens, caches[1].lens), f"replay {turn}"
         assert all(torch.equal(x, y) for x, y in zip(A.akb_unpack(caches[0]), A.akb_unpack(caches[1]))), f"replay {turn}"
+
+
+@pytest.mark.parametrize("n", [3, 100])
+def test_a_row_does_not_depend_on_its_neighbours(A, n):
+    """Heads of zeros, of the largest numbers, and tokens that are left out change no other row's bits."""
+    x = R.tokens(1, 6, n, 128, B16, 5, "plain").transpose(1, 2).contiguous().to(DEV)
+    w = weight(128, B16, 3)
+
+    def run(x, n_new=None):
+        c = A.BlockCache.allocate(1, 6, 6, 128, 128, B16)
+        out = A.akb_append_rotated(c, x, x, x, inv_freq=freqs(128), q_norm=w, k_norm=w, n_new=i32(n_new))
+        return out, A.akb_unpack(c)[0][:, :, :n]
+    want, keys = run(x)
+    y = x.clone()
+    y[0, 1, 2], y[0, 0, 5], y[0, 2, 0] = 0, 3e38, 1e-38
+    got, _ = run(y)
+    same = torch.ones(1, 6, n, dtype=torch.bool)
+    same[0, 2, 1] = same[0, 5, 0] = same[0, 0, 2] = False
+    assert torch.equal(got[same], want[same]) and not torch.equal(got[~same], want[~same])
+    less, _ = run(x, [n - 1])
+    assert torch.equal(less[:, :, :n - 1], want[:, :, :n - 1])
