@@ -736,8 +736,8 @@ def akb_append_rotated(cache: BlockCache, q: torch.Tensor | None, k: torch.Tenso
     for t in (base, n_new):
         assert t is None or (t.dtype == torch.int32 and t.dim() == 1)
     assert n_new is None or n_new.shape == (cache.B,)
-    x = akb_tokens()
-    (x.q, x.q_seq, x.q_token), (x.k, x.k_seq, x.k_token), (x.v, x.v_seq, x.v_token) = _projected(q, cache, n, cache.Hq), _projected(k, cache, n, cache.Hkv), _projected(v, cache, n, cache.Hkv)
+    (qp, *qs), (kp, *ks), (vp, *vs) = _projected(q, cache, n, cache.Hq), _projected(k, cache, n, cache.Hkv), _projected(v, cache, n, cache.Hkv)
+    x = akb_tokens(qp, kp, vp, *qs, *ks, *vs)
     if q is not None and q_out is None:
         q_out = (torch.empty if n_new is None else torch.zeros)(cache.B, cache.Hq, n, cache.D, dtype=cache.dtype, device=q.device)
     assert q_out is None or (q_out.dtype == cache.dtype and q_out.shape == (cache.B, cache.Hq, n, cache.D))

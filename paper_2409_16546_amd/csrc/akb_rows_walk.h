@@ -65,13 +65,18 @@ template <class T, int D> struct RowState {
     {
         float mx = -__builtin_inff();
         const int seen = limit - first - 4 * (lane >> 4);   // counted from the lane's first token
+        if (masked) {
+            asm volatile("");   // (a branch: few blocks are masked, and without it all are asked, 50 instructions of some 180)
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (16 * t + r >= seen) s[t][r] = -__builtin_inff();
+        }
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                if (masked && 16 * t + r >= seen) s[t][r] = -__builtin_inff();
-                mx = fmaxf(mx, s[t][r]);
-            }
+            for (int r = 0; r < 4; ++r) mx = fmaxf(mx, s[t][r]);
         mx = max_lane32(max_lane16(mx));
         const float now = fmaf(mx, c2, -unit);
         if (__any(now > m + kSlackBits)) {
@@ -128,7 +133,9 @@ __device__ __forceinline__ void walk_rows(const akb_cache& c, size_t bh, RowStat
     for (; blk < whole; blk += STEP) {
         VCodes<D, NT> vc;
         vc.load(c, block0 + blk, lane);
-        const float k_scale = pow2(int8_t(kc.e)), v_scale = pow2(int8_t(kc.e >> 8)), unit = weight_bits<T>(v_scale >= pow2(kLargeExp));
+        uint32_t e = kc.e;
+        asm volatile("" : "+v"(e));   // (known to be the same in all lanes, it would be moved to a scalar register where it is asked for, and the codes that are asked for before it waited for there)
+        const float k_scale = pow2(int8_t(e)), v_scale = pow2(int8_t(e >> 8)), unit = weight_bits<T>(v_scale >= pow2(kLargeExp));
         f32x4_t s[RT][4];
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
