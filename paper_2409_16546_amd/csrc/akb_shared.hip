@@ -230,10 +230,19 @@ struct SharedPlan {
     int tiles[2], groups[2], splits[2];
     size_t parts[2], total;     // offsets into the workspace, its size
 };
-// parts of each of `walks` walks that make up about `target` workgroups
-static long cut_into(long walks, long blocks, long target) { return std::max(1L, std::min((target + walks / 2) / walks, (blocks + kWaves - 1) / kWaves)); }
-constexpr int kRowWalkRows = 512;  // over a prefix, up to which row walks have them
+// Parts of each of `walks` walks: one workgroup or more per unit, two at most, and of those the numbers at which the unit with the most has the least
+static long cut_into(long walks, long blocks, long units)
+{
+    long best = (units + walks - 1) / walks;
+    for (long s = best + 1; walks * s <= 2 * units; ++s)
+        if ((walks * s + units - 1) / units * best < (walks * best + units - 1) / units * s) best = s;
+    return std::max(1L, std::min(best, blocks / kWaves));
+}
 constexpr int kOneWalkRows = 96;   // of a sequence, from which on one walk goes over both
+// Whether a prefix's rows are the prompt walks', which turn a block once for 128 rows: where row walks, of 32 rows each, would be more than run at a time and do not all fall into one tile.  Row walk /
+// prompt walk, us: 256 rows over 32768 tokens 56 / 66, 512 over 16384 45.5 / 57.8, 640 over 13000 59.1 / 58.6, 1024 over 4096 40.0 / 44.8 (256 row walks); but 816 over 163 34.2 / 27.8 (624), 1600 over 1000
+// 57.0 / 48.6 (800), 100 over 2000 136.9 / 123.9 (1280), and 64 over 2000 171.6 / 181 (1280).
+static bool prompt_walks(long pairs, long rows, long slots) { return rows > 96 && pairs * ((rows + 31) / 32) > slots; }
 static SharedPlan plan(const akb_shape& f, const akb_shape& s, int n, int max_len, int prefix_max_len)
 {
     SharedPlan p = {};
@@ -249,21 +258,17 @@ static SharedPlan plan(const akb_shape& f, const akb_shape& s, int n, int max_le
         p.total = at + align256(size_t(2 * slots) * part_floats((int)std::min(seq_rows, long(kPromptRows)), s.D) * sizeof(float));
         return p;
     }
-    // Parts: a walk is cut so that each kind makes about one workgroup per compute unit (and no part is shorter than a block per wave): two prefix walks on a unit take from each other most of what they
-    // gain, and own walks fill the second place.  Both kinds to fill both places / one each, us: 16 x 64 heads 13000 + 3001 tokens 80 / 59, 4 x 32 heads 32768 + 100 21.3 / 19.1, 8 x 8
-    // heads 8192 + 2000 17.8 / 15.5, 8 prefixes of 8 x 32 heads 8192 + 500 43 / 38.  Row walks that take some 30 us at that (1.9 us per four blocks) are cut further: 64 x 32 heads 32768 + 1000 68 / 62.6, 20 x
-    // 11 rows of 4 heads 4000 + 100 41 / 34.
-    // Prefix walks of many rows take the prompt walk, which turns a block once for 128 of them; row walk / prompt walk, us: 256 rows 62.6 / 65.7 and 26.3 / 27.1, 440 34.2 / 36.0, 640 66.9 / 58.9, 816 over
-    // 163 tokens 38.0 / 30.9, 1024 49.2 / 47.1, 1440 38.7 / 37.9.
+    // Parts: both kinds make one workgroup per compute unit where that shares the work out evenly, and no part is shorter than a block per wave: two prefix walks on a unit take from each other most of
+    // what they gain, and own walks fill the second place.  Both kinds to fill both places / one each, us: 16 x 64 heads 13000 + 3001 tokens 80 / 59, 4 x 32 heads 32768 + 100 21.3 / 19.1, 8 x 8
+    // heads 8192 + 2000 17.8 / 15.5, 8 prefixes of 8 x 32 heads 8192 + 500 43 / 38, 64 x 32 heads 32768 + 1000 63.7 / 56.3.  160 row walks over 13000 tokens, in two / three: 54 / 46.5; 192 prompt
+    // walks, whole / in two: 89 / 80.5.  Own walks of five blocks, in two / whole: 13.7 / 12.0.
     const long units = slots / 2;
     for (int i = 0; i < 2; ++i) {
-        constexpr int kPromptTiles = kPromptRows / 16;
-        const bool prompt = i == 0 && rows[i] > kRowWalkRows;
-        p.tiles[i] = prompt ? kPromptTiles : (i == 1 && rows[i] <= 16 ? 1 : 2);
+        const bool prompt = i == 0 && prompt_walks(pairs[i], rows[i], slots);
+        p.tiles[i] = prompt ? kPromptRows / 16 : (i == 1 && rows[i] <= 16 ? 1 : 2);
         p.groups[i] = int((rows[i] + tile_rows(p.tiles[i]) - 1) / tile_rows(p.tiles[i]));
         const long walks = pairs[i] * p.groups[i];
-        const bool longer = i == 0 && !prompt && walks * blocks[i] > units * 48;
-        p.splits[i] = int(cut_into(walks, blocks[i], longer ? units * 7 / 4 : units));
+        p.splits[i] = int(cut_into(walks, blocks[i], units));
         p.parts[i] = at;
         at += align256(size_t(walks) * p.splits[i] * part_floats(tile_rows(p.tiles[i]), s.D) * sizeof(float));
     }
@@ -280,7 +285,7 @@ size_t shared_workspace(const akb_shape& f, const akb_shape& s, int n)
     const size_t front = align256(attention_tickets()), pairs[2] = {size_t(f.B) * s.Hkv, size_t(s.B) * s.Hkv}, rows[2] = {size_t(s.B / f.B) * seq_rows, seq_rows};
     size_t step = front;
     for (int i = 0; i < 2; ++i) {
-        const int tile = i == 0 && rows[i] > size_t(kRowWalkRows) ? kPromptRows : 32;
+        const int tile = i == 0 && prompt_walks(long(pairs[i]), long(rows[i]), long(slots)) ? kPromptRows : 32;
         step += align256(std::max(2 * slots, pairs[i] * ((rows[i] + tile - 1) / tile)) * part_floats(tile, s.D) * sizeof(float));
     }
     const size_t one = rows_all >= size_t(kOneWalkRows) ? front + align256(2 * slots * part_floats(kPromptRows, s.D) * sizeof(float)) : 0;

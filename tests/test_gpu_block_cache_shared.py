@@ -86,6 +86,9 @@ LARGE = [  # dtype, out, D, prefixes, sequences, Hq, Hkv, P, N, n: against 64 bi
     (F16, F16, 64, 2, 40, 40, 8, 700, 130, 7),
     (F16, F32, 64, 2, 140, 8, 8, 200, 150, 5),         # own walks by a wave alone, in one tile of rows
     (B16, B16, 128, 3, 180, 24, 8, 100, 200, 7),       # ... in two
+    (B16, F32, 128, 3, 150, 32, 8, 900, 90, 4),        # prompt walks over the prefix, one tile of own rows
+    (F16, F16, 64, 2, 60, 32, 8, 1200, 70, 12),        # ... two tiles
+    (B16, F32, 128, 5, 125, 64, 16, 333, 10, 2),       # ... walks that are not cut
 ]
 
 
