@@ -64,7 +64,7 @@ __device__ __forceinline__ void step_walk(const StepArgs& a, unsigned item, char
     const int nb = (keys + kTB - 1) / kTB, lo = (int)(long(nb) * split / s.splits), hi = (int)(long(nb) * (split + 1) / s.splits);
     // where a row's query lies (NULL: nobody's), and the tokens that it sees
     auto row_of = [&](int row, int& limit) -> const uint16_t* {
-        limit = PREFIX ? len : 0;   // (a row that nobody wants: no mask on its account)
+        limit = len;   // (a row that nobody wants: no mask on its account)
         if (row >= all_rows) return nullptr;
         const StepRow r(a, s, first_b, row);
         const int m = queries(a, r.b);
