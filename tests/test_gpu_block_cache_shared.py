@@ -89,6 +89,10 @@ LARGE = [  # dtype, out, D, prefixes, sequences, Hq, Hkv, P, N, n: against 64 bi
     (B16, F32, 128, 3, 150, 32, 8, 900, 90, 4),        # prompt walks over the prefix, one tile of own rows
     (F16, F16, 64, 2, 60, 32, 8, 1200, 70, 12),        # ... two tiles
     (B16, F32, 128, 5, 125, 64, 16, 333, 10, 2),       # ... walks that are not cut
+    (F16, F32, 64, 8, 560, 32, 8, 130, 66, 1),         # ... of each type and head size
+    (F16, F16, 128, 8, 560, 32, 8, 70, 200, 1),
+    (B16, F32, 64, 8, 88, 64, 8, 250, 100, 3),
+    (F16, F32, 128, 8, 88, 64, 8, 190, 40, 3),
 ]
 
 
