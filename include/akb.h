@@ -205,8 +205,9 @@ akv_status akb_append_rotated(const akb_cache *cache, const akb_tokens *tokens, 
  * Copy sequences: sequence j of dst becomes the first min(lens of the parent, upto[j]) tokens of its parent, sequence parents[j] of src.  parents: device
  * int32 [dst B]; a number outside 0..src B - 1 leaves sequence j as it was.  NULL: every sequence its own (dst B = src B).  upto: device int32 [dst B], or NULL for all
  * tokens.  Complete blocks are copied as they are; where a copy ends inside one, its tail takes that block's values (which rounds nothing: they are numbers
- * of the 16-bit type), all 64 of them; scores are copied where both have one.  A sequence whose length would exceed dst's Ncap is left unchanged and dst's
- * flags[AKV_FLAG_OVERFLOW] is incremented.  dst has src's Hkv, D and dtype, and shares no memory with src, which is not written.
+ * of the 16-bit type), all 64 of them.  Where dst has scores, the copied tokens' are src's, or 0 where src has none
+ * (as the appends set them).  A sequence whose length would exceed dst's Ncap is left unchanged and dst's flags[AKV_FLAG_OVERFLOW] is incremented.  dst has src's Hkv, D
+ * and dtype, and shares no memory with src, which is not written.
  */
 akv_status akb_fork(const akb_cache *src, const akb_cache *dst, const int32_t *parents, const int32_t *upto, void *stream);
 

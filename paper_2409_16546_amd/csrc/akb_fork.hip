@@ -72,8 +72,9 @@ __global__ __launch_bounds__(kThreads) void fork_kernel(akb_cache c, akb_cache d
         copy<4, NT>((is_v ? c.v8 : c.k8) + (from0 + first) * (kTB * D), (is_v ? d.v8 : d.k8) + (to0 + first) * (kTB * D), n * (kTB * D / 16), tid);
         if (!is_v && tid < 2 * n) d.exps[(to0 + first) * 2 + tid] = c.exps[(from0 + first) * 2 + tid];
     }
-    if (is_v && c.score && d.score)
-        for (int t = first * kTB + tid; t < min(len, (first + chunk) * kTB); t += kThreads) d.score[to * d.shape.Ncap + t] = c.score[from * c.shape.Ncap + t];
+    if (is_v && d.score)   // (from a cache without scores: of tokens that no weight has been counted for, as the appends store them)
+        for (int t = first * kTB + tid; t < min(len, (first + chunk) * kTB); t += kThreads)
+            d.score[to * d.shape.Ncap + t] = c.score ? c.score[from * c.shape.Ncap + t] : 0.f;
     if (len % kTB && whole >= first && whole < first + chunk) {   // the incomplete block
         if (whole < had / kTB) {
             TailSide<T, D> s;

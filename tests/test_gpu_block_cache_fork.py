@@ -52,6 +52,29 @@ def test_fork(A, dtype, D, parents, upto):
     R.assert_same_tokens(A, c, ref, "the source is as it was")
 
 
+@pytest.mark.parametrize("N,W", [(320, 1), (4096, 9)])   # copies in runs of blocks, and streamed block by block
+def test_fork_from_a_cache_without_scores(A, N, W):
+    """The copied tokens have no weight yet, whatever the sequence that they replace had; what is behind them stays; eviction then keeps the tokens that were attended."""
+    H, D = 16, 128
+    c, d = A.BlockCache.allocate(2, H, H, D, N, F16), A.BlockCache.allocate(2 * W, H, H, D, N, F16, score=True)
+    lens = [N - 20, 130]
+    A.akb_append(c, *(R.tokens(2, H, N - 20, D, F16, s, "plain").to(DEV) for s in (1, 2)), i32(lens))
+    parents, upto = [b % 2 for b in range(2 * W)], [N - 64 * b - 1 for b in range(2 * W)]
+    d.score.fill_(7.0)
+    A.akb_fork(c, d, i32(parents), i32(upto))
+    score, L = d.score.view(2 * W, H, N), d.lens.tolist()
+    assert L == [min(lens[a], u) for a, u in zip(parents, upto)]
+    for b in range(2 * W):
+        assert not score[b, :, :L[b]].any() and (score[b, :, L[b]:] == 7.0).all(), b
+    d.reserve(1, keep=64)
+    A.akb_attention(d, R.tokens(2 * W, H, 1, D, F16, 3, "plain").to(DEV), accumulate=True)
+    e, kept = A.BlockCache.allocate(2 * W, H, H, D, 64, F16, score=True), torch.zeros(2 * W, H, 64, dtype=torch.int32, device=DEV)
+    A.akb_evict(d, e, 64, 0, kept=kept)
+    for b in (0, 2 * W - 1):
+        want = score[b, :, :L[b]].sort(dim=1, descending=True, stable=True).indices[:, :64].sort(dim=1).values
+        assert torch.equal(kept[b].long(), want)
+
+
 def test_fork_into_caches_of_other_sizes(A):
     c, ref = pair(A, 2, 2, 2, 64, 1024, F16)
     put(A, c, ref, 1000, 1, [1000, 130])
