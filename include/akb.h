@@ -178,7 +178,8 @@ typedef struct akb_rotary {
     const uint16_t *q_norm, *k_norm; /* device [D] of the shape's type: w; NULL: not normed (each by itself)               */
     const float *inv_freq;           /* device [rot / 2]                                                                   */
     const int32_t *base;             /* device [n_base], or NULL: token i of sequence b stands at base[b / (B / n_base)] +
-                                        lens[b] + i: lengths of shared prefixes, counts of evicted tokens                  */
+                                        lens[b] + i: lengths of shared prefixes, counts of evicted tokens; not in the
+                                        memory of the cache's own lens, which the call moves                               */
     int32_t n_base;                  /* divides B                                                                          */
     int32_t rot;                     /* the first rot channels turn: a multiple of 16, 0..D                                */
     int32_t pairs;                   /* 0: pair j is channels (j, j + rot / 2); 1: channels (2 j, 2 j + 1)                 */
@@ -207,7 +208,7 @@ akv_status akb_append_rotated(const akb_cache *cache, const akb_tokens *tokens, 
  * tokens.  Complete blocks are copied as they are; where a copy ends inside one, its tail takes that block's values (which rounds nothing: they are numbers
  * of the 16-bit type), all 64 of them.  Where dst has scores, the copied tokens' are src's, or 0 where src has none
  * (as the appends set them).  A sequence whose length would exceed dst's Ncap is left unchanged and dst's flags[AKV_FLAG_OVERFLOW] is incremented.  dst has src's Hkv, D
- * and dtype, and shares no memory with src, which is not written.
+ * and dtype, and shares no memory with src, which is not written; parents shares none with dst's lens (upto may be them).
  */
 akv_status akb_fork(const akb_cache *src, const akb_cache *dst, const int32_t *parents, const int32_t *upto, void *stream);
 

@@ -57,6 +57,12 @@ void sizes_of(const akb_shape& s, akb_sizes* out)
 // sequences of shape s that go on from those of f
 bool shares_ok(const akb_shape& f, const akb_shape& s) { return s.B % f.B == 0 && s.Hq == f.Hq && s.Hkv == f.Hkv && s.D == f.D && s.dtype == f.dtype; }
 
+bool overlap(const void* p, size_t n, const void* q, size_t m)
+{
+    const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
+    return p && q && n && m && a < b + m && b < a + n;
+}
+
 // whether src and dst share memory (scores where dst's is written)
 bool share_memory(const akb_cache& src, const akb_cache& dst)
 {
@@ -66,10 +72,8 @@ bool share_memory(const akb_cache& src, const akb_cache& dst)
     const struct { const void *p; size_t n; } from[] = {{src.k8, a.k8}, {src.v8, a.v8}, {src.exps, a.exps}, {src.k_tail, a.k_tail}, {src.v_tail, a.v_tail}, {src.score, src.score ? a.score : 0}, {src.lens, a.lens}},
                  to[] = {{dst.k8, b.k8}, {dst.v8, b.v8}, {dst.exps, b.exps}, {dst.k_tail, b.k_tail}, {dst.v_tail, b.v_tail}, {dst.score, dst.score ? b.score : 0}, {dst.lens, b.lens}};
     for (const auto& x : from)
-        for (const auto& y : to) {
-            const uintptr_t xp = reinterpret_cast<uintptr_t>(x.p), yp = reinterpret_cast<uintptr_t>(y.p);
-            if (x.n && y.n && xp < yp + y.n && yp < xp + x.n) return true;
-        }
+        for (const auto& y : to)
+            if (overlap(x.p, x.n, y.p, y.n)) return true;
     return false;
 }
 
@@ -244,6 +248,7 @@ akv_status akb_append_rotated(const akb_cache* cache, const akb_tokens* tokens, 
     if (r.rot < 0 || r.rot > s.D || r.rot % 16 != 0) return fail(AKV_EINVAL, "rot = %d is no multiple of 16 in 0..D", r.rot);
     if (r.rot > 0 && !r.inv_freq) return fail(AKV_EINVAL, "inv_freq is NULL");
     if (r.base && (r.n_base < 1 || s.B % r.n_base != 0)) return fail(AKV_EINVAL, "n_base = %d does not divide B = %d", r.n_base, s.B);
+    if (overlap(r.base, size_t(r.n_base) * sizeof(int32_t), cache->lens, size_t(s.B) * sizeof(int32_t))) return fail(AKV_EINVAL, "base shares memory with the lens that the call moves");
     if ((r.q_norm || r.k_norm) && !(std::isfinite(r.eps) && r.eps >= 0.f)) return fail(AKV_EINVAL, "eps is negative or not finite");
     if ((size_t(n) + 126) / AKB_TB * s.Hkv >= size_t(1) << 23) return fail(AKV_EINVAL, "%d tokens of %d KV heads: 2^23 blocks or more of a sequence", n, s.Hkv);
     if (n == 0) return AKV_OK;
@@ -270,6 +275,7 @@ akv_status akb_fork(const akb_cache* src, const akb_cache* dst, const int32_t* p
     if (!parents && s.B != d.B) return fail(AKV_EINVAL, "parents is NULL and src and dst differ: B %d/%d", s.B, d.B);
     if (!aligned(parents, 4) || !aligned(upto, 4)) return fail(AKV_EINVAL, "parents and upto must be 4-byte aligned");
     if (share_memory(*src, *dst)) return fail(AKV_EINVAL, "src and dst share memory");
+    if (overlap(parents, size_t(d.B) * sizeof(int32_t), dst->lens, size_t(d.B) * sizeof(int32_t))) return fail(AKV_EINVAL, "parents shares memory with dst's lens");
     return hip_result(akb::launch_fork(*src, *dst, parents, upto, static_cast<hipStream_t>(stream)), "fork launch");
 }
 

@@ -166,6 +166,18 @@ def test_rotated_append_is_refused(A, refused):
     refused(call(c=wide, n=1 << 22, rot=64, n_base=1), "2^23")
 
 
+def test_places_and_parents_in_lengths_that_a_call_moves_are_refused(A, refused):
+    """Workgroups read them after others may have moved the lengths."""
+    L, r = A.lib(), C.byref
+    shape = A.akb_shape(6, 8, 4, 128, 256, 0)
+    cache, to = A.akb_cache(shape, **ADDR), A.akb_cache(shape, **OTHER)
+    tokens = A.akb_tokens(X, X, X, 4096, 2048, 4096, 2048, 4096, 2048)
+    for base, n_base in ((ADDR["lens"], 6), (ADDR["lens"] + 20, 1), (ADDR["lens"] - 4, 2)):
+        refused(L.akb_append_rotated(r(cache), r(tokens), None, 2, OUT, r(A.akb_rotary(None, None, Q, base, n_base, 128, 0, 0.0)), None), "base shares memory")
+    for parents in (OTHER["lens"], OTHER["lens"] + 20, OTHER["lens"] - 20):
+        refused(L.akb_fork(r(cache), r(to), parents, None, None), "parents shares memory")
+
+
 def test_copies_and_cuts_are_refused(A, refused):
     L, r = A.lib(), C.byref
     shape = (2, 8, 4, 128, 256, 0)

@@ -75,6 +75,17 @@ def test_fork_from_a_cache_without_scores(A, N, W):
         assert torch.equal(kept[b].long(), want)
 
 
+def test_copies_up_to_the_lengths_that_the_destination_had(A):
+    """upto may be dst's own lens, which the call moves."""
+    c, ref = pair(A, 7, 4, 2, 128, 320, F16)
+    put(A, c, ref, 300, 1, LENS)
+    d, want = pair(A, 7, 4, 2, 128, 320, F16)
+    put(A, d, want, 130, 7, had := [130, 5, 64, 0, 1, 100, 65])
+    A.akb_fork(c, d, i32([0, 0, 0, 4, 2, 6, 0]), d.lens)
+    S.fork(ref, want, [0, 0, 0, 4, 2, 6, 0], had)
+    R.assert_same_tokens(A, d, want)
+
+
 def test_fork_into_caches_of_other_sizes(A):
     c, ref = pair(A, 2, 2, 2, 64, 1024, F16)
     put(A, c, ref, 1000, 1, [1000, 130])
