@@ -202,6 +202,11 @@ typedef struct akb_tokens {
 akv_status akb_append_rotated(const akb_cache *cache, const akb_tokens *tokens, const int32_t *n_new, int32_t n, uint16_t *q_out, const akb_rotary *rotary,
                               void *stream);
 
+/* How akb_append_rotated shares out n tokens, with queries or without: 1 = row by row, 2 = a workgroup per (block, KV head) with its query heads, 3 = the query heads in
+ * workgroups of their own.  how: NULL, or a host pointer that receives two numbers: 1 where the call passes the last-level cache by, 1 where the workgroups move the lengths (0: a
+ * launch behind).  Host computation; 0 on a bad shape. */
+int32_t akb_append_rotated_path(const akb_shape *shape, int32_t n, int32_t queries, int32_t *how);
+
 /*
  * Copy sequences: sequence j of dst becomes the first min(lens of the parent, upto[j]) tokens of its parent, sequence parents[j] of src.  parents: device
  * int32 [dst B]; a number outside 0..src B - 1 leaves sequence j as it was.  NULL: every sequence its own (dst B = src B).  upto: device int32 [dst B], or NULL for all

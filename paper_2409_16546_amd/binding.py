@@ -29,7 +29,7 @@ EXPORTS = ["akv_version", "akv_last_error", "akv_layout_sizes", "akv_cache_reset
            "akw_layout_sizes", "akw_workspace_init", "akw_pack", "akw_unpack", "akw_gemv"]
 AKW_MAX_B = 4
 AKB_EXPORTS = ["akb_layout_sizes", "akb_cache_reset", "akb_append", "akb_attention_workspace", "akb_workspace_init", "akb_attention_path", "akb_attention_join", "akb_attention", "akb_evict_workspace", "akb_evict",
-               "akb_attention_shared_workspace", "akb_attention_shared", "akb_attention_shared_path", "akb_append_rotated", "akb_fork", "akb_truncate", "akb_unpack"]
+               "akb_attention_shared_workspace", "akb_attention_shared", "akb_attention_shared_path", "akb_append_rotated", "akb_append_rotated_path", "akb_fork", "akb_truncate", "akb_unpack"]
 AKB_TB, AKB_MAX_G = 64, 16
 AKB_DTYPES = {torch.float16: 0, torch.bfloat16: 1}
 
@@ -189,6 +189,8 @@ def lib() -> C.CDLL:
         L.akb_attention_shared_path.argtypes = [C.POINTER(akb_shape), C.POINTER(akb_shape), C.c_int32, C.c_int32, C.c_int32, C.POINTER(C.c_int32)]
         L.akb_append_rotated.restype = C.c_int
         L.akb_append_rotated.argtypes = [C.POINTER(akb_cache), C.POINTER(akb_tokens), C.c_void_p, C.c_int32, C.c_void_p, C.POINTER(akb_rotary), C.c_void_p]
+        L.akb_append_rotated_path.restype = C.c_int32
+        L.akb_append_rotated_path.argtypes = [C.POINTER(akb_shape), C.c_int32, C.c_int32, C.POINTER(C.c_int32)]
         L.akb_fork.restype = C.c_int
         L.akb_fork.argtypes = [C.POINTER(akb_cache), C.POINTER(akb_cache), C.c_void_p, C.c_void_p, C.c_void_p]
         L.akb_truncate.restype = C.c_int
@@ -745,6 +747,14 @@ def akb_append_rotated(cache: BlockCache, q: torch.Tensor | None, k: torch.Tenso
     r = akb_rotary(_ptr(q_norm), _ptr(k_norm), _ptr(inv_freq), _ptr(base), 0 if base is None else base.numel(), 0 if inv_freq is None else 2 * inv_freq.numel(), int(pairs), eps)
     _check(lib().akb_append_rotated(cache.ref(), C.byref(x), _ptr(n_new), n, _ptr(q_out), C.byref(r), _stream()))
     return q_out
+
+
+def akb_append_rotated_path(B: int, Hq: int, Hkv: int, D: int, Ncap: int, n: int, queries: bool = True) -> tuple[int, bool, bool]:
+    """(1, 2 or 3: row by row, a workgroup per block and KV head with its query heads, query heads in workgroups of their own; whether it passes the last-level cache by;
+    whether its workgroups move the lengths): how akb_append_rotated shares out n tokens."""
+    how = (C.c_int32 * 2)()
+    path = lib().akb_append_rotated_path(C.byref(akb_shape(B, Hq, Hkv, D, Ncap, 0)), n, int(queries), how)
+    return int(path), bool(how[0]), bool(how[1])
 
 
 def akb_fork(src: BlockCache, dst: BlockCache, parents: torch.Tensor | None = None, upto: torch.Tensor | None = None) -> None:

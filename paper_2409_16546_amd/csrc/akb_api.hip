@@ -63,6 +63,9 @@ bool overlap(const void* p, size_t n, const void* q, size_t m)
     return p && q && n && m && a < b + m && b < a + n;
 }
 
+// a sequence's blocks that an append of n projected tokens can touch, by KV head: its workgroups have fewer than 2^32 threads
+bool rotated_blocks_ok(const akb_shape& s, int n) { return (size_t(n) + 126) / AKB_TB * s.Hkv < size_t(1) << 23; }
+
 // whether src and dst share memory (scores where dst's is written)
 bool share_memory(const akb_cache& src, const akb_cache& dst)
 {
@@ -250,7 +253,7 @@ akv_status akb_append_rotated(const akb_cache* cache, const akb_tokens* tokens, 
     if (r.base && (r.n_base < 1 || s.B % r.n_base != 0)) return fail(AKV_EINVAL, "n_base = %d does not divide B = %d", r.n_base, s.B);
     if (overlap(r.base, size_t(r.n_base) * sizeof(int32_t), cache->lens, size_t(s.B) * sizeof(int32_t))) return fail(AKV_EINVAL, "base shares memory with the lens that the call moves");
     if ((r.q_norm || r.k_norm) && !(std::isfinite(r.eps) && r.eps >= 0.f)) return fail(AKV_EINVAL, "eps is negative or not finite");
-    if ((size_t(n) + 126) / AKB_TB * s.Hkv >= size_t(1) << 23) return fail(AKV_EINVAL, "%d tokens of %d KV heads: 2^23 blocks or more of a sequence", n, s.Hkv);
+    if (!rotated_blocks_ok(s, n)) return fail(AKV_EINVAL, "%d tokens of %d KV heads: 2^23 blocks or more of a sequence", n, s.Hkv);
     if (n == 0) return AKV_OK;
     if (!x.k || !x.v) return fail(AKV_EINVAL, "k / v is NULL");
     if (!x.q != !q_out) return fail(AKV_EINVAL, "one of q and q_out is NULL, the other is not");
@@ -264,6 +267,12 @@ akv_status akb_append_rotated(const akb_cache* cache, const akb_tokens* tokens, 
         if (q_out && i.p < q_out + size_t(s.B) * s.Hq * n * s.D && q_out < i.p + i.seq * (s.B - 1) + i.token * (n - 1) + int64_t(i.heads) * s.D)
             return fail(AKV_EINVAL, "q_out shares memory with the tokens");
     return hip_result(akb::launch_append_rotated(*cache, x, n_new, n, q_out, r, static_cast<hipStream_t>(stream)), "append launch");
+}
+
+int32_t akb_append_rotated_path(const akb_shape* shape, int32_t n, int32_t queries, int32_t* how)
+{
+    if (!shape || !shape_ok(*shape) || n < 1 || n > shape->Ncap || !rotated_blocks_ok(*shape, n)) return 0;
+    return akb::rotated_path(*shape, n, queries != 0, how);
 }
 
 akv_status akb_fork(const akb_cache* src, const akb_cache* dst, const int32_t* parents, const int32_t* upto, void* stream)

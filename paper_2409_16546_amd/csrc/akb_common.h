@@ -40,6 +40,7 @@ int shared_path(const akb_shape& prefix, const akb_shape& s, int n, int max_len,
 hipError_t launch_shared(const akb_cache& prefix, int prefix_max_len, const AttentionArgs& a, hipStream_t st);
 bool append_ticketed(const akb_shape& s, int n);   // the appends' workgroups move the lengths themselves
 hipError_t launch_append_lens(const akb_cache& c, const int32_t* n_new, int n, hipStream_t st);   // otherwise: behind them
+int rotated_path(const akb_shape& s, int n, bool queries, int32_t* how);   // akb_append_rotated_path
 hipError_t launch_append_rotated(const akb_cache& c, const akb_tokens& x, const int32_t* n_new, int n, uint16_t* q_out, const akb_rotary& r, hipStream_t st);
 hipError_t launch_fork(const akb_cache& src, const akb_cache& dst, const int32_t* parents, const int32_t* upto, hipStream_t st);
 hipError_t launch_truncate(const akb_cache& c, const int32_t* keep, hipStream_t st);

@@ -380,34 +380,54 @@ __global__ __launch_bounds__(2 * D, NEXT ? 3 : 4) void append_rotated_kernel(Tur
 }
 
 constexpr int kFewTokens = 8;
-hipError_t launch_append_rotated(const akb_cache& c, const akb_tokens& x, const int32_t* n_new, int n, uint16_t* q_out, const akb_rotary& r, hipStream_t st)
+// How a call is shared out
+struct RotatedPlan {
+    int blocks, rows, apart;   // TurnArgs
+    bool ticketed, streamed;
+};
+static RotatedPlan plan(const akb_shape& s, int n, bool queries)
 {
-    const int blocks = (kTB - 1 + n + kTB - 1) / kTB;
+    RotatedPlan p;
+    p.blocks = (kTB - 1 + n + kTB - 1) / kTB;
     // Few tokens: row by row, 16 to a workgroup, which leaves little to any: 64 sequences of one token 22 / 12 us
-    const int rows = n <= kFewTokens ? (n * (c.shape.Hq + 2 * c.shape.Hkv) + 15) / 16 : 0;
+    p.rows = n <= kFewTokens ? (n * (s.Hq + 2 * s.Hkv) + 15) / 16 : 0;
     // Where they are few, workgroups of two waves (D = 64) and those of many query heads leave the query heads to others: chunks of 777 tokens of 6 sequences, 4 x 4 heads of D = 64 25.1 / 19.4 us; 2 KV heads
     // of 16 at D = 128, 2 sequences 47 / 22 us, and 144 tokens 33 / 14; 8 of 16, 2048 tokens 74 / 58; but 8 of 8, 8 sequences of 777 62.7 / 68.7, and with four heads no gain (2 x 8 24.9 / 25.7)
-    const int G = c.shape.Hq / c.shape.Hkv;
-    const long walks = long(blocks) * c.shape.Hkv * c.shape.B;
-    const int apart = rows == 0 && q_out && (c.shape.D == 64 ? walks <= 1024 : (G > kApart && walks <= 512)) ? (G + kApart - 1) / kApart : 0;
-    const dim3 grid(blocks * c.shape.Hkv * (1 + apart) + rows, c.shape.B);
-    const bool ticketed = append_ticketed(c.shape, n);
+    const int G = s.Hq / s.Hkv;
+    const long walks = long(p.blocks) * s.Hkv * s.B;
+    p.apart = p.rows == 0 && queries && (s.D == 64 ? walks <= 1024 : (G > kApart && walks <= 512)) ? (G + kApart - 1) / kApart : 0;
+    p.ticketed = append_ticketed(s, n);
     // as in the append: large calls pass the last-level cache by
-    const bool streamed = (size_t(q_out ? 2 * c.shape.Hq : 0) + 2 * size_t(c.shape.Hkv)) * c.shape.B * n * c.shape.D * 2 > (size_t(128) << 20);
-    const TurnArgs a{c, x, r, n_new, n, q_out, ticketed ? 1 : 0, blocks, apart, rows};
+    p.streamed = (size_t(queries ? 2 * s.Hq : 0) + 2 * size_t(s.Hkv)) * s.B * n * s.D * 2 > (size_t(128) << 20);
+    return p;
+}
+int rotated_path(const akb_shape& s, int n, bool queries, int32_t* how)
+{
+    const RotatedPlan p = plan(s, n, queries);
+    if (how) {
+        how[0] = p.streamed;
+        how[1] = p.ticketed;
+    }
+    return p.rows ? 1 : (p.apart ? 3 : 2);
+}
+hipError_t launch_append_rotated(const akb_cache& c, const akb_tokens& x, const int32_t* n_new, int n, uint16_t* q_out, const akb_rotary& r, hipStream_t st)
+{
+    const RotatedPlan p = plan(c.shape, n, q_out != nullptr);
+    const dim3 grid(p.blocks * c.shape.Hkv * (1 + p.apart) + p.rows, c.shape.B);
+    const TurnArgs a{c, x, r, n_new, n, q_out, p.ticketed ? 1 : 0, p.blocks, p.apart, p.rows};
     auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(2 * c.shape.D), 0, st, a); };
     auto pick = [&](auto type, auto width) {
         using T = decltype(type);
         constexpr int D = decltype(width)::value;
-        if (r.pairs) streamed ? launch(append_rotated_kernel<T, D, true, true>) : launch(append_rotated_kernel<T, D, true, false>);
-        else streamed ? launch(append_rotated_kernel<T, D, false, true>) : launch(append_rotated_kernel<T, D, false, false>);
+        if (r.pairs) p.streamed ? launch(append_rotated_kernel<T, D, true, true>) : launch(append_rotated_kernel<T, D, true, false>);
+        else p.streamed ? launch(append_rotated_kernel<T, D, false, true>) : launch(append_rotated_kernel<T, D, false, false>);
     };
     using D64 = std::integral_constant<int, 64>;
     using D128 = std::integral_constant<int, 128>;
     if (c.shape.dtype == AKB_FP16) c.shape.D == 64 ? pick(Fp16(), D64()) : pick(Fp16(), D128());
     else c.shape.D == 64 ? pick(Bf16(), D64()) : pick(Bf16(), D128());
     if (hipError_t e = hipGetLastError()) return e;
-    return ticketed ? hipSuccess : launch_append_lens(c, n_new, n, st);
+    return p.ticketed ? hipSuccess : launch_append_lens(c, n_new, n, st);
 }
 
 }  // namespace akb

@@ -120,6 +120,27 @@ def test_the_gpu_tests_reach_every_kernel(A):
     assert {(s[0], s[3]) for s in seen} == {(1, False), (1, True), (2, False), (2, True), (3, False)}, seen
 
 
+def test_the_gpu_tests_reach_every_rotated_append(A):
+    """Each kernel (type, head size, order of pairs, past the last-level cache or not) and each way to share a call out, with lengths moved by either means where both occur."""
+    from test_gpu_block_cache_rotated_paths import LENS, PATHS
+    kernels, ways = set(), set()
+    for dtype, D, B, Hq, Hkv, n, _, _, _, pairs in PATHS:
+        path, streamed, ticketed = A.akb_append_rotated_path(B, Hq, Hkv, D, (max(LENS) + n + 63) // 64 * 64, n)
+        kernels.add((dtype, D, pairs, streamed))
+        ways.add((D, path, streamed))
+        ways.add((path, ticketed))
+        if path == 3:
+            ways.add((D, "apart", -(-Hq // Hkv // 4), Hq // Hkv % 4 == 0))
+    both = (False, True)
+    assert kernels == {(t, D, p, s) for t in (torch.float16, torch.bfloat16) for D in (64, 128) for p in both for s in both}
+    assert ways >= {(D, path, s) for D in (64, 128) for path in (1, 2, 3) for s in both} | {(path, t) for path in (1, 2, 3) for t in both}, ways
+    assert {w[2:] for w in ways if w[:2] == (128, "apart")} >= {(2, False), (2, True), (3, False), (4, True)} and len({w for w in ways if w[:2] == (64, "apart")}) >= 3, ways
+    good = (6, 8, 4, 128, 256)
+    assert A.akb_append_rotated_path(*good, 1)[0] == 1 and A.akb_append_rotated_path(*good, 9, False)[0] == 2
+    for bad in ((*good, 0), (*good, 257), (6, 8, 3, 128, 256, 1), (1, 256, 256, 64, 1 << 22, 1 << 22)):
+        assert A.akb_append_rotated_path(*bad)[0] == 0, bad
+
+
 def test_rotated_append_is_refused(A, refused):
     L, r = A.lib(), C.byref
     shape = A.akb_shape(6, 8, 4, 128, 256, 0)
