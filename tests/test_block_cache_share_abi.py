@@ -120,6 +120,17 @@ def test_the_gpu_tests_reach_every_kernel(A):
     assert {(s[0], s[3]) for s in seen} == {(1, False), (1, True), (2, False), (2, True), (3, False)}, seen
 
 
+def test_the_gpu_tests_reach_every_kernel_of_shared_attention(A):
+    from test_gpu_block_cache_shared_kernels import FORMS, KERNELS
+    up, ways = lambda x: (x + 63) // 64 * 64, []
+    for Bp, B, Hq, Hkv, P, N, n in FORMS:
+        for D in (64, 128):
+            path, a, _ = A.akb_attention_shared_path(Bp, B, Hq, Hkv, D, up(P), up(N), n)
+            ways.append((D, path, a > 1 if path == 3 else n * (Hq // Hkv) > 16))
+    assert set(ways) == {(D, path, x) for D in (64, 128) for path in (1, 2, 3) for x in (False, True)}
+    assert len(KERNELS) == 2 * 2 * len(ways)   # each of them in both types, with both results
+
+
 def test_the_gpu_tests_reach_every_rotated_append(A):
     """Each kernel (type, head size, order of pairs, past the last-level cache or not) and each way to share a call out, with lengths moved by either means where both occur."""
     from test_gpu_block_cache_rotated_paths import LENS, PATHS

@@ -75,6 +75,26 @@ def test_fork_from_a_cache_without_scores(A, N, W):
         assert torch.equal(kept[b].long(), want)
 
 
+@pytest.mark.parametrize("dtype", [F16, B16], ids=["fp16", "bf16"])
+@pytest.mark.parametrize("D", [64, 128])
+def test_copies_that_pass_the_cache_by(A, dtype, D):
+    """More than 128 MiB: blocks one at a time, stored with the non-temporal hint."""
+    H, N, L = 16, 4096, [4000, 131, 64, 4096]
+    c, d = (A.BlockCache.allocate(B, H, H, D, N, dtype, score=True) for B in (4, 18))
+    A.akb_append(c, *(R.tokens(4, H, N, D, dtype, s, "plain").to(DEV) for s in (1, 2)), i32(L))
+    c.score.copy_(torch.rand(c.score.shape, generator=torch.Generator().manual_seed(3)))
+    d.score.fill_(7.0)
+    parents, upto = [b % 4 for b in range(18)], [(1 << 30, 4032, 65, 2049, 1)[b % 5] for b in range(18)]
+    A.akb_fork(c, d, i32(parents), i32(upto))
+    lens = [min(L[a], u) for a, u in zip(parents, upto)]
+    assert d.lens.tolist() == lens
+    sides, scores = list(zip(A.akb_unpack(c), A.akb_unpack(d))), [x.score.view(x.B, H, N) for x in (c, d)]
+    for b, (a, m) in enumerate(zip(parents, lens)):
+        for src, dst in sides:
+            assert torch.equal(dst[b, :, :m], src[a, :, :m]), b
+        assert torch.equal(scores[1][b, :, :m], scores[0][a, :, :m]) and (scores[1][b, :, m:] == 7.0).all(), b
+
+
 def test_copies_up_to_the_lengths_that_the_destination_had(A):
     """upto may be dst's own lens, which the call moves."""
     c, ref = pair(A, 7, 4, 2, 128, 320, F16)
