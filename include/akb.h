@@ -173,7 +173,8 @@ akv_status akb_attention_shared(const akb_cache *prefix, const akb_cache *cache,
  * two numbers, the parts that a walk over a prefix and one over own tokens are cut into (3: twice those of the one walk).  Host computation; 0 on bad shapes. */
 int32_t akb_attention_shared_path(const akb_shape *prefix, const akb_shape *shape, int32_t n, int32_t max_len, int32_t prefix_max_len, int32_t *parts);
 
-/* How keys and queries are normed and turned (above): with angles made in binary64, keys in binary64 and queries in binary32, each result rounded once, to the 16-bit type. */
+/* How keys and queries are normed and turned (above): with angles made in binary64; keys in binary64, rounded to binary32 and then to the 16-bit type (each to nearest);
+ * queries in binary32, with sine and cosine rounded to it, and rounded once, to the 16-bit type. */
 typedef struct akb_rotary {
     const uint16_t *q_norm, *k_norm; /* device [D] of the shape's type: w; NULL: not normed (each by itself)               */
     const float *inv_freq;           /* device [rot / 2]                                                                   */

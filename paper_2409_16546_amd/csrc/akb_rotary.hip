@@ -1,9 +1,10 @@
 // Tokens from a model's projections into the block-scaled 8-bit cache: norms per head, rotary positions, the append (rules and layout: include/akb.h).
 //
-// Keys are normed and turned in 64 bits and rounded once, to the 16-bit type: their largest number decides a block's exponent, and a number next to a border would get another
-// code where 32 bits round twice.  Queries are normed and turned in 32 bits, by the same angles.
-// Bound by memory where it is large (4 x 8192 tokens of 32 + 16 heads: 738 MB in 151 us, 4.9 TB/s, what a plain copy of as much in as out reaches; without norms and with 16
-// channels turned 147), by the chain of loads, sums and stores of a workgroup where it is small.
+// Keys are normed and turned in 64 bits, rounded to binary32 and from there to the 16-bit type: their largest number decides a block's exponent, and in 32 bits throughout one key
+// in some thousand came out as another 16-bit number.  (What the step between costs: a key whose binary32 number is the middle of two 16-bit ones, one in some 2^13 in binary16 and
+// 2^16 in bfloat16, may be off by 2^-25 of itself more than half a step.)  Queries are normed and turned in 32 bits, by the same angles, sine and cosine rounded to binary32.
+// Bound by memory where it is large (4 x 8192 tokens of 32 + 16 heads: 738 MB in 151 to 163 us by the card, 4.5 to 4.9 TB/s, where a plain copy moves 5.1 in and out; without norms
+// and with 16 channels turned 147), by the chain of loads, sums and stores of a workgroup where it is small.
 // A row (a token of a head) lies in D / 8 lanes, eight channels in each; a workgroup has a block's 64 tokens, 16 rows at a time.  Sine and cosine are made by their power series
 // for a thread's first token (half of them by the lane of the other channels of the pairs), and turned on by 16 tokens, in 64 bits, for the next.
 #include "akb_pack.h"
@@ -389,15 +390,24 @@ static RotatedPlan plan(const akb_shape& s, int n, bool queries)
 {
     RotatedPlan p;
     p.blocks = (kTB - 1 + n + kTB - 1) / kTB;
-    // Few tokens: row by row, 16 to a workgroup, which leaves little to any: 64 sequences of one token 22 / 12 us
+    // Few tokens: row by row, 16 to a workgroup, which leaves little to any.  Otherwise / row by row, us, the copy that sets the lengths with them, 32 heads on 8 at D = 128 where not
+    // said otherwise.  One token: 64 sequences 14.0 / 13.7, of 64 heads 20.7 / 13.3, 256 sequences 25.0 / 16.9.  Eight: 23.8 / 23.6, 25.5 / 25.1, 52.1 / 49.2, at D = 64 17.3 / 18.6.
+    // Nine: 23.1 / 24.7, 26.7 / 28.4, 54.1 / 52.2, 17.9 / 18.8.  Twelve: 24.1 / 27.8, 27.9 / 31.6, 57.9 / 68.5, 21.1 / 21.2.  (Four sequences: 13.2 to 13.8 all of them.)
     p.rows = n <= kFewTokens ? (n * (s.Hq + 2 * s.Hkv) + 15) / 16 : 0;
-    // Where they are few, workgroups of two waves (D = 64) and those of many query heads leave the query heads to others: chunks of 777 tokens of 6 sequences, 4 x 4 heads of D = 64 25.1 / 19.4 us; 2 KV heads
-    // of 16 at D = 128, 2 sequences 47 / 22 us, and 144 tokens 33 / 14; 8 of 16, 2048 tokens 74 / 58; but 8 of 8, 8 sequences of 777 62.7 / 68.7, and with four heads no gain (2 x 8 24.9 / 25.7)
+    // Where they are few, workgroups of two waves (D = 64) and those of many query heads leave the query heads to others.  Beside / apart, us, by the workgroups that have KV heads.
+    // D = 64, 200 tokens: groups of four, 500 28.1 / 22.0, 1020 31.8 / 28.6, 1200 35.6 / 30.2, 1600 36.3 / 36.4, 2400 49.2 / 54.8 (777 tokens: 1008 31.3 / 28.6, 1176 33.9 / 34.3); of
+    // eight, 1020 42.2 / 36.5, 2400 66.8 / 72.4; of one, 900 24.7 / 24.8, 1020 25.9 / 26.8, 1600 29.2 / 33.9.  D = 128, 200 tokens: groups of eight, 240 37.3 / 30.6, 500 39.7 / 35.4,
+    // 640 48.3 / 42.9, 800 54.4 / 53.6, 1200 66.3 / 72.5; of five, 120 29.5 / 23.4, 480 32.4 / 33.2, 640 34.3 / 36.6; of sixteen, 777 tokens, 504 82.0 / 69.4, 784 96.4 / 97.2.  Groups of
+    // four at D = 128 stay beside: 24 workgroups of two sequences 24.9 / 25.7, though 120 to 400 of six to twenty gain, 28.5 / 25.4, and lose again from 640 on, 31.5 / 31.6, 800 33.2 / 38.0.
     const int G = s.Hq / s.Hkv;
     const long walks = long(p.blocks) * s.Hkv * s.B;
     p.apart = p.rows == 0 && queries && (s.D == 64 ? walks <= 1024 : (G > kApart && walks <= 512)) ? (G + kApart - 1) / kApart : 0;
+    // The append's line.  Tickets / a launch behind, us: one block, 512 workgroups 14.1 / 16.9, 640 14.1 / 17.0, 1024 14.2 / 16.9 (32 sequences of 32 KV heads 17.8 / 16.8); two or more,
+    // 288 31.0 / 31.6, 29.3 / 29.3, at D = 64 with query heads apart 24.0 / 20.4, 384 15.4 / 17.1 (five tokens), 31.4 / 32.1, 30.6 / 30.4, 23.2 / 19.8, 512 16.9 / 16.9, 32.7 / 32.4.
     p.ticketed = append_ticketed(s, n);
-    // as in the append: large calls pass the last-level cache by
+    // As in the append: tensors of more than half of the last-level cache are read and written with the non-temporal hint.  Plain / with it, us, 32 heads on 8 at D = 128; one set of
+    // tensors used again and again, 96 MB 31.4 / 35.4, 128 36.9 / 41.6, 160 39.4 / 46.3, 256 73.4 / 74.4, 512 140 / 136; four sets in turn, which no cache holds, 48 26.3 / 28.9, 64
+    // 32.9 / 31.9, 96 38.1 / 35.5, 128 44.4 / 42.0, 160 50.1 / 47.7, 512 141 / 138: by where the projection left them the line would be at 64 or at 256.
     p.streamed = (size_t(queries ? 2 * s.Hq : 0) + 2 * size_t(s.Hkv)) * s.B * n * s.D * 2 > (size_t(128) << 20);
     return p;
 }

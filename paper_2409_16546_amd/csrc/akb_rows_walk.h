@@ -66,7 +66,7 @@ template <class T, int D> struct RowState {
         float mx = -__builtin_inff();
         const int seen = limit - first - 4 * (lane >> 4);   // counted from the lane's first token
         if (masked) {
-            asm volatile("");   // (a branch: few blocks are masked, and without it all are asked, 50 instructions of some 180)
+            asm volatile("");   // (a branch: without it all blocks are asked, 50 instructions of some 180; few are masked where the caller knows what every row sees)
 #pragma unroll
             for (int t = 0; t < 4; ++t)
 #pragma unroll

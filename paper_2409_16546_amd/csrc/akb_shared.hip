@@ -62,7 +62,7 @@ __device__ __forceinline__ void step_walk(const StepArgs& a, unsigned item, char
         keys = max(len - m + last.token + 1, 0);
     }
     const int nb = (keys + kTB - 1) / kTB, lo = (int)(long(nb) * split / s.splits), hi = (int)(long(nb) * (split + 1) / s.splits);
-    // where a row's query lies (NULL: nobody's), and the tokens that it sees
+    // where a row's query lies (NULL: nobody's, behind its sequence's n_q: it is multiplied with its tile all the same), and the tokens that it sees
     auto row_of = [&](int row, int& limit) -> const uint16_t* {
         limit = len;   // (a row that nobody wants: no mask on its account)
         if (row >= all_rows) return nullptr;
@@ -78,6 +78,8 @@ __device__ __forceinline__ void step_walk(const StepArgs& a, unsigned item, char
         float(*m_s)[kTileRows] = reinterpret_cast<float(*)[kTileRows]>(lds + sizeof(float) * kWaves * kTileRows * (D + 4));
         float(*z_s)[kTileRows] = m_s + kWaves;
         RowState<T, D> st[TILES];
+        // (0 as soon as rows differ: all blocks of own walks of several query tokens are asked about then.  Until the least of the limits no block need be; 16 x 64 heads of 5 and 12
+        // query tokens over 3001 own ones 32.6 / 32.0 and 39.4 / 39.4 us, 64 x 32 of 20 over 500 behind 2000 85.9 / 85.2)
         int all_see = len;
 #pragma unroll
         for (int k = 0; k < TILES; ++k) {
@@ -238,7 +240,11 @@ static long cut_into(long walks, long blocks, long units)
         if ((walks * s + units - 1) / units * best < (walks * best + units - 1) / units * s) best = s;
     return std::max(1L, std::min(best, blocks / kWaves));
 }
-constexpr int kOneWalkRows = 96;   // of a sequence, from which on one walk goes over both
+// Rows of a sequence from which on one walk goes over both.  Walks of their own / one walk, us, at 64, 96, 128, 136 and 256 rows: 16 sequences of 500 tokens behind 8192, 32 heads on 8,
+// 36.8 / 53.4, 52.3 / 57.4, 65.8 / 65.7, 70.5 / 92.5, 122.9 / 105.0; 16 of 3001 behind 13000, 64 on 8, 67.2 / 100.6, 102.9 / 107.3, 132.1 / 123.4, 141.5 / 196.6, 266.8 / 222.7; eight of eight
+// behind 2000 73.3 / 75.5, 96.2 / 79.6, 126.7 / 88.6, 138.8 / 147.8, 238.1 / 159.6; two of four behind 20000 45.7 / 67.0, 65.3 / 73.1, 76.0 / 83.9, 112.3 / 118.4, 129.5 / 133.9.  The one walk fills
+// each sequence's rows up to a multiple of 128, the others a prefix's rows to a multiple of 128 and a sequence's to one of 32.
+constexpr int kOneWalkRows = 96;
 // Whether a prefix's rows are the prompt walks', which turn a block once for 128 rows: where row walks, of 32 rows each, would be more than run at a time and do not all fall into one tile.  Row walk /
 // prompt walk, us: 256 rows over 32768 tokens 56 / 66, 512 over 16384 45.5 / 57.8, 640 over 13000 59.1 / 58.6, 1024 over 4096 40.0 / 44.8 (256 row walks); but 816 over 163 34.2 / 27.8 (624), 1600 over 1000
 // 57.0 / 48.6 (800), 100 over 2000 136.9 / 123.9 (1280), and 64 over 2000 171.6 / 181 (1280).
@@ -314,6 +320,8 @@ template <class T, int D> static hipError_t launch(const StepArgs& a, const Shar
         const unsigned per_pair = (a.n * a.G + rows - 1) / rows, turns = per_pair * a.side[1].c.shape.B * a.side[1].c.shape.Hkv;
         hipLaunchKernelGGL(kernel, dim3(std::min(turns, 1u << 20)), dim3(256), 0, st, a, tile_rows(p.tiles[0]), tile_rows(p.tiles[1]), turns, per_pair);
     };
+    // A row's parts one after the other / by eight threads, us: 1 + 1 of them 50.2 / 73.0, 3 + 1 58.4 / 64.8, 4 + 1 38.5 / 41.3, 56.2 / 57.4 and 11.1 / 11.2, 8 + 2 23.0 / 23.0, 16 + 1 18.7 / 18.3,
+    // 16 + 2 22.6 / 21.3, 32 + 2 22.5 / 19.5, 117 + 1 23.7 / 13.6.
     if (p.splits[0] + p.splits[1] <= 8) join(step_join_kernel<T, D, 1>, 1024 / D);
     else join(step_join_kernel<T, D, 8>, 128 / D);
     return hipGetLastError();
