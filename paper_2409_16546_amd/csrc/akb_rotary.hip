@@ -126,15 +126,14 @@ template <class T, int D> __device__ __forceinline__ double norm_scale(const u32
     y = y * fma(-0.5 * m * y, y, 1.5);
     return y * fma(-0.5 * m * y, y, 1.5);
 }
-// .. and in 32, unless this row's have none there (far: the same in all of its lanes)
-template <class T, int D> __device__ __forceinline__ float norm_scale32(const u32x4_t& x, float eps, bool& far)
+// .. and in 32, unless this row's have none there (which is the same in all of its lanes)
+template <class T, int D> __device__ __forceinline__ float norm_scale32(const u32x4_t& x, float eps)
 {
     float sum = 0.f;
 #pragma unroll
     for (int e = 0; e < 8; ++e) sum = fmaf(channel<T>(x, e), channel<T>(x, e), sum);
     sum = row_sum<D>(sum);
-    far = !(sum > 0x1p-100f && sum < 0x1p120f);
-    if (far) return float(norm_scale<T, D>(x, eps));
+    if (!(sum > 0x1p-100f && sum < 0x1p120f)) return float(norm_scale<T, D>(x, eps));
     return __builtin_amdgcn_rsqf(fmaf(sum, 1.f / D, eps));
 }
 
@@ -225,19 +224,12 @@ __global__ __launch_bounds__(2 * D, NEXT ? 3 : 4) void append_rotated_kernel(Tur
     };
     auto turn_query_by = [&](const u32x4_t& q, const float (&cw)[8], const float (&sw)[8]) {
         const u32x4_t o = pairs.others(q);
-        bool far = false;
-        const float scale = a.r.q_norm ? norm_scale32<T, D>(q, a.r.eps, far) : 1.f;
+        const float scale = a.r.q_norm ? norm_scale32<T, D>(q, a.r.eps) : 1.f;
         float y[8];
-        if (far) {   // numbers that leave a product no room
 #pragma unroll
-            for (int e = 0; e < 8; ++e) y[e] = channel<T>(q, e) * scale * cw[e] + (pairs.any ? channel<T>(o, e) * scale * sw[e] : 0.f);
-        } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                y[e] = channel<T>(q, e) * cw[e];
-                if (pairs.any) y[e] = fmaf(channel<T>(o, e), sw[e], y[e]);
-                y[e] *= scale;
-            }
+        for (int e = 0; e < 8; ++e) {   // the scale first: a channel times its weight may have no room in 32 bits (bfloat16)
+            y[e] = channel<T>(q, e) * scale * cw[e];
+            if (pairs.any) y[e] = fmaf(channel<T>(o, e) * scale, sw[e], y[e]);
         }
         return u32x4_t{T::pack(y[0], y[1]), T::pack(y[2], y[3]), T::pack(y[4], y[5]), T::pack(y[6], y[7])};
     };

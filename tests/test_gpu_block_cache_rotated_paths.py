@@ -66,8 +66,8 @@ def turned(x, places, freq, w, eps, pairs):
 @pytest.mark.parametrize("queries", [True, False], ids=["", "keys"])
 def test_every_way_to_share_out_a_call(A, case, queries):
     """Queries, with u = 2^-24, relative to the sum of the addends' magnitudes: the root is of a sum of D squares (a lane's eight, each one rounding, and up to four sums
-    of lanes), the mean with eps (one more): 13 u, halved by the root, which is itself within 2 u (one unit in the last place): 8.5 u.  Sine and cosine rounded to binary32, times
-    a weight, times the channel, summed up, times the root: 5 u.  13.5 u, below the 16 u = 2^-20 that is allowed.  Then half a step of the type."""
+    of lanes), the mean with eps (one more): 13 u, halved by the root, which is itself within 2 u (one unit in the last place): 8.5 u.  Sine and cosine rounded to binary32 and times
+    a weight, the channel times the root, their product, the sum: 5 u.  13.5 u, below the 16 u = 2^-20 that is allowed.  Then half a step of the type."""
     dtype, D, B, Hq, Hkv, n, ragged, rot, norm, pairs = case
     print(case, flush=True)
     lens = [LENS[b % len(LENS)] for b in range(B)]
@@ -110,3 +110,25 @@ def test_every_way_to_share_out_a_call(A, case, queries):
         bound = half * want.abs() + 2.0 ** -20 * size * (1 + half) + (2.0 ** -25 if dtype == F16 else 1e-38)
         err = (out[b, :m].double() - want[0]).abs() / bound[0]
         assert not m or float(err.max()) <= 1.0, (b, float(err.max()))
+
+
+@pytest.mark.parametrize("D,pairs,n", [(128, False, 3), (128, True, 70), (64, False, 70), (64, True, 3), (128, False, 200)])
+def test_norm_weights_of_every_size(A, D, pairs, n):
+    """bfloat16 weights from 2^-100 to 2^100 on heads from 2^-48 to 2^58: a channel times its weight is beyond binary32 on either side where the normed number times it is not."""
+    g = torch.Generator().manual_seed(5)
+    H = 8
+    sizes = torch.exp2(torch.tensor([-48.0, -40, -20, 0, 20, 40, 50, 58])).view(1, 1, H, 1)
+    x = (torch.randn(2, n, H, D, generator=g) * sizes).to(B16).to(DEV)
+    w = (torch.exp2(torch.rand(D, generator=g) * 200 - 100) * torch.where(torch.rand(D, generator=g) < 0.5, -1.0, 1.0)).to(B16).to(DEV)
+    w[D // 3:D // 3 + 9] = 1.0   # and some that are not
+    freq, eps = freqs(D), 1e-37
+    c, d = (A.BlockCache.allocate(2, H, H, D, 256, B16) for _ in range(2))
+    out = A.akb_append_rotated(c, x, x, x, inv_freq=freq, q_norm=w, k_norm=w, eps=eps, pairs=pairs)
+    want, size = turned(x.double(), torch.arange(n, device=DEV).expand(2, n), freq, w, float(np.float32(eps)), pairs)
+    A.akb_append(d, want.float().to(B16).transpose(1, 2).contiguous(), x.transpose(1, 2).contiguous())
+    for got, stored in zip(A.akb_unpack(c), A.akb_unpack(d)):
+        assert torch.equal(got, stored)
+    half = 2.0 ** -8
+    err = (out.transpose(1, 2).double() - want).abs() / (half * want.abs() + 2.0 ** -20 * size * (1 + half) + 1e-38)
+    worst, finite = float(err.max()), bool(torch.isfinite(out).all())
+    assert finite and worst <= 1.0, worst
