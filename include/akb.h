@@ -177,7 +177,7 @@ int32_t akb_attention_shared_path(const akb_shape *prefix, const akb_shape *shap
  * queries in binary32, with sine and cosine rounded to it, and rounded once, to the 16-bit type. */
 typedef struct akb_rotary {
     const uint16_t *q_norm, *k_norm; /* device [D] of the shape's type: w; NULL: not normed (each by itself)               */
-    const float *inv_freq;           /* device [rot / 2]                                                                   */
+    const float *inv_freq;           /* device [rot / 2]; place inv_freq_j below 2^50 in magnitude (made in binary64)      */
     const int32_t *base;             /* device [n_base], or NULL: token i of sequence b stands at base[b / (B / n_base)] +
                                         lens[b] + i: lengths of shared prefixes, counts of evicted tokens; not in the
                                         memory of the cache's own lens, which the call moves                               */

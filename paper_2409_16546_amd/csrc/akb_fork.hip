@@ -88,9 +88,9 @@ hipError_t launch_fork(const akb_cache& src, const akb_cache& dst, const int32_t
 {
     // (a copy that ends with the source's capacity has no incomplete block; one that the destination has no room for is refused by the first workgroups)
     const int blocks = std::min(src.shape.Ncap, dst.shape.Ncap) / kTB;
-    // Copies that are more than half of the last-level cache are stored with the non-temporal hint and shared out by single blocks; smaller ones, which the next step reads, without it and in
-    // runs of eight.  Single blocks with the hint / eight without: one prompt of 8192 tokens to 16 sequences of 8 heads (268 MB) 40.8 / 60 us, 16 to 16 88 / 105; 64 sequences of up to 500
-    // tokens that change places (67 MB) 27.7 / 14.3, with the next step's attention 33.3 / 26.1.
+    // Copies that are more than half of the last-level cache are stored with the non-temporal hint and shared out by single blocks; smaller ones, which the next step reads,
+    // without it and in runs of eight.  Single blocks with the hint / eight without: one prompt of 8192 tokens to 16 sequences of 8 heads (268 MB) 40.8 / 60 us, 16 to 16 88
+    // / 105; 64 sequences of up to 500 tokens that change places (67 MB) 27.7 / 14.3, with the next step's attention 33.3 / 26.1.
     const bool streamed = size_t(dst.shape.B) * dst.shape.Hkv * blocks * kTB * dst.shape.D * 2 > (size_t(128) << 20);
     const int chunk = streamed ? 1 : 8;
     auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(2 * ((blocks + chunk - 1) / chunk), dst.shape.Hkv, dst.shape.B), dim3(kThreads), 0, st, src, dst, parents, upto, chunk); };

@@ -390,7 +390,8 @@ static RotatedPlan plan(const akb_shape& s, int n, bool queries)
     // D = 64, 200 tokens: groups of four, 500 28.1 / 22.0, 1020 31.8 / 28.6, 1200 35.6 / 30.2, 1600 36.3 / 36.4, 2400 49.2 / 54.8 (777 tokens: 1008 31.3 / 28.6, 1176 33.9 / 34.3); of
     // eight, 1020 42.2 / 36.5, 2400 66.8 / 72.4; of one, 900 24.7 / 24.8, 1020 25.9 / 26.8, 1600 29.2 / 33.9.  D = 128, 200 tokens: groups of eight, 240 37.3 / 30.6, 500 39.7 / 35.4,
     // 640 48.3 / 42.9, 800 54.4 / 53.6, 1200 66.3 / 72.5; of five, 120 29.5 / 23.4, 480 32.4 / 33.2, 640 34.3 / 36.6; of sixteen, 777 tokens, 504 82.0 / 69.4, 784 96.4 / 97.2.  Groups of
-    // four at D = 128 stay beside: 24 workgroups of two sequences 24.9 / 25.7, though 120 to 400 of six to twenty gain, 28.5 / 25.4, and lose again from 640 on, 31.5 / 31.6, 800 33.2 / 38.0.
+    // four at D = 128 stay beside: two sequences of eight KV heads 24.9 / 25.7, though 120 to 500 workgroups of four gain, 400 28.5 / 25.4, and lose again
+    // from 640 on, 31.5 / 31.6, 800 33.2 / 38.0.
     const int G = s.Hq / s.Hkv;
     const long walks = long(p.blocks) * s.Hkv * s.B;
     p.apart = p.rows == 0 && queries && (s.D == 64 ? walks <= 1024 : (G > kApart && walks <= 512)) ? (G + kApart - 1) / kApart : 0;

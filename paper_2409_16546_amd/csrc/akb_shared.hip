@@ -241,13 +241,13 @@ static long cut_into(long walks, long blocks, long units)
     return std::max(1L, std::min(best, blocks / kWaves));
 }
 // Rows of a sequence from which on one walk goes over both.  Walks of their own / one walk, us, at 64, 96, 128, 136 and 256 rows: 16 sequences of 500 tokens behind 8192, 32 heads on 8,
-// 36.8 / 53.4, 52.3 / 57.4, 65.8 / 65.7, 70.5 / 92.5, 122.9 / 105.0; 16 of 3001 behind 13000, 64 on 8, 67.2 / 100.6, 102.9 / 107.3, 132.1 / 123.4, 141.5 / 196.6, 266.8 / 222.7; eight of eight
-// behind 2000 73.3 / 75.5, 96.2 / 79.6, 126.7 / 88.6, 138.8 / 147.8, 238.1 / 159.6; two of four behind 20000 45.7 / 67.0, 65.3 / 73.1, 76.0 / 83.9, 112.3 / 118.4, 129.5 / 133.9.  The one walk fills
-// each sequence's rows up to a multiple of 128, the others a prefix's rows to a multiple of 128 and a sequence's to one of 32.
+// 36.8 / 53.4, 52.3 / 57.4, 65.8 / 65.7, 70.5 / 92.5, 122.9 / 105.0; 16 of 3001 behind 13000, 64 on 8, 67.2 / 100.6, 102.9 / 107.3, 132.1 / 123.4, 141.5 / 196.6, 266.8 / 222.7;
+// eight of eight behind 2000 73.3 / 75.5, 96.2 / 79.6, 126.7 / 88.6, 138.8 / 147.8, 238.1 / 159.6; two of four behind 20000 45.7 / 67.0, 65.3 / 73.1, 76.0 / 83.9, 112.3 / 118.4,
+// 129.5 / 133.9.  The one walk fills each sequence's rows up to a multiple of 128, the others a prefix's rows to a multiple of 128 and a sequence's to one of 32.
 constexpr int kOneWalkRows = 96;
-// Whether a prefix's rows are the prompt walks', which turn a block once for 128 rows: where row walks, of 32 rows each, would be more than run at a time and do not all fall into one tile.  Row walk /
-// prompt walk, us: 256 rows over 32768 tokens 56 / 66, 512 over 16384 45.5 / 57.8, 640 over 13000 59.1 / 58.6, 1024 over 4096 40.0 / 44.8 (256 row walks); but 816 over 163 34.2 / 27.8 (624), 1600 over 1000
-// 57.0 / 48.6 (800), 100 over 2000 136.9 / 123.9 (1280), and 64 over 2000 171.6 / 181 (1280).
+// Whether a prefix's rows are the prompt walks', which turn a block once for 128 rows: where row walks, of 32 rows each, would be more than run at a time and do not all fall
+// into one tile.  Row walk / prompt walk, us: 256 rows over 32768 tokens 56 / 66, 512 over 16384 45.5 / 57.8, 640 over 13000 59.1 / 58.6, 1024 over 4096 40.0 / 44.8 (256 row
+// walks); but 816 over 163 34.2 / 27.8 (624), 1600 over 1000 57.0 / 48.6 (800), 100 over 2000 136.9 / 123.9 (1280), and 64 over 2000 171.6 / 181 (1280).
 static bool prompt_walks(long pairs, long rows, long slots) { return rows > 96 && pairs * ((rows + 31) / 32) > slots; }
 static SharedPlan plan(const akb_shape& f, const akb_shape& s, int n, int max_len, int prefix_max_len)
 {
@@ -264,10 +264,10 @@ static SharedPlan plan(const akb_shape& f, const akb_shape& s, int n, int max_le
         p.total = at + align256(size_t(2 * slots) * part_floats((int)std::min(seq_rows, long(kPromptRows)), s.D) * sizeof(float));
         return p;
     }
-    // Parts: both kinds make one workgroup per compute unit where that shares the work out evenly, and no part is shorter than a block per wave: two prefix walks on a unit take from each other most of
-    // what they gain, and own walks fill the second place.  Both kinds to fill both places / one each, us: 16 x 64 heads 13000 + 3001 tokens 80 / 59, 4 x 32 heads 32768 + 100 21.3 / 19.1, 8 x 8
-    // heads 8192 + 2000 17.8 / 15.5, 8 prefixes of 8 x 32 heads 8192 + 500 43 / 38, 64 x 32 heads 32768 + 1000 63.7 / 56.3.  160 row walks over 13000 tokens, in two / three: 54 / 46.5; 192 prompt
-    // walks, whole / in two: 89 / 80.5.  Own walks of five blocks, in two / whole: 13.7 / 12.0.
+    // Parts: both kinds make one workgroup per compute unit where that shares the work out evenly, and no part is shorter than a block per wave: two prefix walks on a unit
+    // take from each other most of what they gain, and own walks fill the second place.  Both kinds to fill both places / one each, us: 16 x 64 heads 13000 + 3001 tokens 80
+    // / 59, 4 x 32 heads 32768 + 100 21.3 / 19.1, 8 x 8 heads 8192 + 2000 17.8 / 15.5, 8 prefixes of 8 x 32 heads 8192 + 500 43 / 38, 64 x 32 heads 32768 + 1000 63.7 / 56.3.
+    // 160 row walks over 13000 tokens, in two / three: 54 / 46.5; 192 prompt walks, whole / in two: 89 / 80.5.  Own walks of five blocks, in two / whole: 13.7 / 12.0.
     const long units = slots / 2;
     for (int i = 0; i < 2; ++i) {
         const bool prompt = i == 0 && prompt_walks(pairs[i], rows[i], slots);
@@ -278,7 +278,8 @@ static SharedPlan plan(const akb_shape& f, const akb_shape& s, int n, int max_le
         p.parts[i] = at;
         at += align256(size_t(walks) * p.splits[i] * part_floats(tile_rows(p.tiles[i]), s.D) * sizeof(float));
     }
-    // Own walks of few blocks that are more than run at a time, one to a wave: 256 x 32 heads 4096 + 200 tokens 48.5 / 44, 120 x 64 heads of D = 64 2753 + 5 34 / 30 us; but 16 x 32 heads 8192 + 250 16.2 / 19.5
+    // Own walks of few blocks that are more than run at a time, one to a wave: 256 x 32 heads 4096 + 200 tokens 48.5 / 44, 120 x 64 heads of D = 64 2753 + 5 34 / 30 us; but
+    // 16 x 32 heads 8192 + 250 16.2 / 19.5
     p.solo = long(pairs[1]) * p.groups[1] > slots && blocks[1] <= 4;
     p.total = at;
     return p;
@@ -320,8 +321,8 @@ template <class T, int D> static hipError_t launch(const StepArgs& a, const Shar
         const unsigned per_pair = (a.n * a.G + rows - 1) / rows, turns = per_pair * a.side[1].c.shape.B * a.side[1].c.shape.Hkv;
         hipLaunchKernelGGL(kernel, dim3(std::min(turns, 1u << 20)), dim3(256), 0, st, a, tile_rows(p.tiles[0]), tile_rows(p.tiles[1]), turns, per_pair);
     };
-    // A row's parts one after the other / by eight threads, us: 1 + 1 of them 50.2 / 73.0, 3 + 1 58.4 / 64.8, 4 + 1 38.5 / 41.3, 56.2 / 57.4 and 11.1 / 11.2, 8 + 2 23.0 / 23.0, 16 + 1 18.7 / 18.3,
-    // 16 + 2 22.6 / 21.3, 32 + 2 22.5 / 19.5, 117 + 1 23.7 / 13.6.
+    // A row's parts one after the other / by eight threads, us: 1 + 1 of them 50.2 / 73.0, 3 + 1 58.4 / 64.8, 4 + 1 38.5 / 41.3, 56.2 / 57.4 and 11.1 / 11.2, 8 + 2 23.0 /
+    // 23.0, 16 + 1 18.7 / 18.3, 16 + 2 22.6 / 21.3, 32 + 2 22.5 / 19.5, 117 + 1 23.7 / 13.6.
     if (p.splits[0] + p.splits[1] <= 8) join(step_join_kernel<T, D, 1>, 1024 / D);
     else join(step_join_kernel<T, D, 8>, 128 / D);
     return hipGetLastError();
